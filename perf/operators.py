@@ -108,8 +108,8 @@ def prepare(case, seed):
         s["rowwise"] = (q[:rows, 0::2] | q[:rows, 1::2] << 4).to(torch.uint8).contiguous()  # two neighbours a byte
         s["scale"], s["zero"] = scale[:rows].contiguous(), zero[:rows].to(torch.uint8).contiguous()
         # the weights as the library lays them out: words of 8 values in the order in which a warp takes 16 rows x 64 columns
-        v = q.view(high // 16, 2, 8, wide // 64, 4, 4, 2, 2)  # row tile, half, row, unit, t, step, pair, low/high
-        v = v.permute(0, 3, 2, 4, 5, 7, 6, 1).reshape(-1, 8)  # a word: low/high, pair, half
+        v = q.view(high // 16, 2, 8, wide // 64, 2, 4, 2, 2, 2)  # row tile, half, row, unit, step / 2, t, step % 2, pair, low/high
+        v = v.permute(0, 3, 2, 5, 4, 6, 8, 7, 1).reshape(-1, 8)  # a word: low/high, pair, half
         word = torch.zeros(v.shape[0], dtype=torch.int64, device="cuda")
         for j in range(8):
             word |= v[:, j] << (4 * j)
