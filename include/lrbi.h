@@ -309,6 +309,111 @@ LRBI_API lrbi_status lrbi_masked_gemm_dw(const lrbi_layout *layout, const uint16
                                          const uint32_t *ip, const uint32_t *iz, void *dW, int32_t dw_dtype,
                                          void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Around the pruned layers of a feed-forward block: layer norm, the nonlinearity, activations kept in 8 bits for the
+ * backward pass, and (further down) 4-bit weights for a few rows of activations.  (The paper has no counterpart to
+ * these calls: it retrains and serves whole networks, and they are what stands between two masked layers.)
+ *
+ * Matrices of these calls are [rows][cols] with unit column stride; element (r, c) is at data[r * stride + c], stride in
+ * elements and at least cols, so a slice of a wider array is passed as it is.  Each has its own element type (LRBI_Y_BF16
+ * or LRBI_Y_F32) and needs that type's alignment only; rows that start on 16-byte boundaries and a multiple of 8 columns
+ * are read and written in vectors.  rows may be 0 (nothing is read; gradients of parameters are written as zeros), cols
+ * is 1 .. LRBI_MAX_ROW_COLS.  All sums and statistics are fp32, each output is rounded once.  Outputs must not overlap
+ * inputs or one another.
+ * Results of a call have the same bits every time it is made on the same GPU model.
+ */
+#define LRBI_MAX_ROW_COLS (1 << 24)
+
+/*
+ * 8-bit copy ("checkpoint") of a matrix: columns are cut into groups of LRBI_CHECKPOINT_GROUP, and a group of a row has
+ *       top = max |x|,   scale = top / 127,   q = round_to_even(x * (127 / top))       (each step one fp32 operation)
+ * and stands for q * scale, so a value is off by at most top / 254 (and rounding).  A group whose top is below 2^-118 is kept
+ * as zeros (scale 0); a group that holds a NaN or an infinity has scale NaN and q = 0, and loads as NaN.
+ *   q      device, int8, [rows][lrbi_checkpoint_pitch(cols)], 16-byte aligned; bytes past the last column are written as 0
+ *   scale  device, fp32, [rows][lrbi_checkpoint_groups(cols)]
+ * lrbi_checkpoint_store writes the copy of x, lrbi_checkpoint_load writes what a copy stands for.
+ */
+#define LRBI_CHECKPOINT_GROUP 128
+LRBI_API int32_t lrbi_checkpoint_pitch(int32_t cols);  /* cols rounded up to 16; 0 for cols out of range  */
+LRBI_API int32_t lrbi_checkpoint_groups(int32_t cols); /* ceil(cols / LRBI_CHECKPOINT_GROUP)              */
+LRBI_API lrbi_status lrbi_checkpoint_store(const void *x, int32_t x_dtype, int64_t x_stride, int32_t rows, int32_t cols,
+                                           int8_t *q, float *scale, void *stream);
+LRBI_API lrbi_status lrbi_checkpoint_load(const int8_t *q, const float *scale, int32_t rows, int32_t cols, void *x,
+                                          int32_t x_dtype, int64_t x_stride, void *stream);
+
+/*
+ * Layer norm over the columns of each row:
+ *       mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),  y = (x - mean) * rstd * gamma + beta
+ *   gamma, beta   device, [cols], param_dtype each; beta may be NULL (no offset)
+ *   mean, rstd    device, fp32, [rows], for the backward pass; both or neither NULL
+ *   q, scale      8-bit copy of x, taken on the way; both or neither NULL
+ *
+ * lrbi_layer_norm_backward: with n = (x - mean) * rstd and g = dy * gamma,
+ *       dx = dres + rstd * (g - mean_c(g) - n * mean_c(g * n)),   dgamma = sum over rows of dy * n,   dbeta = sum of dy
+ *   x             the forward input, or NULL where its 8-bit copy q, scale is given: n is then taken from what the copy
+ *                 stands for, with the statistics that the forward pass saved (those of x itself)
+ *   dres          in dx's type, or NULL: the gradient that reaches x past the norm (the residual connection)
+ *   y             in dy's type, or NULL: n * gamma + beta, the forward result, restored for the weight gradient of the
+ *                 layer that it went into
+ *   dgamma, dbeta device, fp32, [cols]; either may be NULL
+ *   workspace     device, lrbi_layer_norm_backward_workspace(rows, cols) bytes, 16-byte aligned, scratch for the call
+ */
+LRBI_API lrbi_status lrbi_layer_norm(const void *x, int32_t x_dtype, int64_t x_stride, int32_t rows, int32_t cols,
+                                     const void *gamma, const void *beta, int32_t param_dtype, float eps, void *y,
+                                     int32_t y_dtype, int64_t y_stride, float *mean, float *rstd, int8_t *q, float *scale,
+                                     void *stream);
+LRBI_API size_t lrbi_layer_norm_backward_workspace(int32_t rows, int32_t cols);
+LRBI_API lrbi_status lrbi_layer_norm_backward(const void *dy, int32_t dy_dtype, int64_t dy_stride, const void *x,
+                                              int32_t x_dtype, int64_t x_stride, const int8_t *q, const float *scale,
+                                              int32_t rows, int32_t cols, const void *gamma, const void *beta,
+                                              int32_t param_dtype, const float *mean, const float *rstd, const void *dres,
+                                              int64_t dres_stride, void *dx, int32_t dx_dtype, int64_t dx_stride, void *y,
+                                              int64_t y_stride, float *dgamma, float *dbeta, void *workspace,
+                                              size_t workspace_bytes, void *stream);
+
+/*
+ * The nonlinearity between two layers: a = act(h), optionally with the 8-bit copy of h (q, scale: both or neither NULL).
+ *       LRBI_ACT_RELU max(h, 0)      LRBI_ACT_GELU h * Phi(h), Phi the normal distribution      LRBI_ACT_SILU h / (1 + exp(-h))
+ * lrbi_activation_backward: dh = da * act'(h), from h, or (h NULL) from its 8-bit copy; `a`, in da's type, or NULL,
+ * receives act(h) again, for the weight gradient of the layer that it went into.  At h = 0 relu has slope 0.
+ */
+enum { LRBI_ACT_RELU = 0, LRBI_ACT_GELU = 1, LRBI_ACT_SILU = 2 };
+LRBI_API lrbi_status lrbi_activation(const void *h, int32_t h_dtype, int64_t h_stride, int32_t rows, int32_t cols,
+                                     int32_t act, void *a, int32_t a_dtype, int64_t a_stride, int8_t *q, float *scale,
+                                     void *stream);
+LRBI_API lrbi_status lrbi_activation_backward(const void *da, int32_t da_dtype, int64_t da_stride, const void *h,
+                                              int32_t h_dtype, int64_t h_stride, const int8_t *q, const float *scale,
+                                              int32_t rows, int32_t cols, int32_t act, void *dh, int32_t dh_dtype,
+                                              int64_t dh_stride, void *a, int64_t a_stride, void *stream);
+
+/*
+ * 4-bit weights with a scale and a zero point for each group of columns of a row (groups of 32, 64 or 128):
+ *       W[o][i] = s[o][g] * (q[o][i] - z[o][g]),     q and z whole numbers 0 .. 15, s bf16,  g = i / group
+ * A weight that the index prunes is stored with q = z, which is exactly zero: the index is applied once, when the layer is
+ * quantised, and costs nothing afterwards.
+ *
+ * Layout (RT = ceil(rows / 16), U = ceil(cols / 64), G = ceil(cols / group)):
+ *   packed  device, uint32, [RT][U][32][4], 16-byte aligned.  Word (tile, u, 4 * g + t, s) holds eight values of rows
+ *           16 * tile + g and + g + 8; its bits 4j .. 4j + 3 are row g + 8 * (j & 1), column
+ *           64 * u + 32 * (s / 2) + 8 * t + 4 * (s & 1) + i with i = 2 * (j / 2 & 1) + j / 4.  Rows past the last hold anything; columns past the last hold their group's z
+ *           (where they belong to no group, anything).
+ *   meta    device, uint32, [RT][G][16]: row 16 * tile + r of group g has the bits of s in the upper half and z in the
+ *           lowest four bits of word (tile, g, r).
+ * lrbi_w4_quantize  W [rows][cols] bf16 -> packed, meta.  Over the kept weights of a group: lo = min(0, W), hi = max(0, W),
+ *           s = bf16((hi - lo) / 15), z = clamp(round(-lo / s)), q = clamp(round(W / s) + z), each step one fp32 operation,
+ *           rounding to nearest even, clamped to 0 .. 15.  A group without a non-zero kept weight has s = 0, z = 8; a kept
+ *           weight that is not finite gives s = NaN.  What the array holds at pruned places is not looked at.  ip, iz: the
+ *           layer's packed factors, or both NULL (nothing is pruned; only rows and cols of the layout are looked at).
+ * lrbi_w4_gemv  Y [batch][rows] (bf16 or fp32) = X W^T for X [batch][cols] bf16, contiguous, sums in fp32.  Made for a few
+ *           rows of X (up to 16 go through the weights together); batch may be 0.
+ */
+LRBI_API size_t lrbi_w4_packed_words(int32_t rows, int32_t cols);             /* RT*U*128; 0 if a size is out of range */
+LRBI_API size_t lrbi_w4_meta_words(int32_t rows, int32_t cols, int32_t group); /* RT*G*16; 0 also for other groups      */
+LRBI_API lrbi_status lrbi_w4_quantize(const lrbi_layout *layout, const uint16_t *W, const uint32_t *ip, const uint32_t *iz,
+                                      int32_t group, uint32_t *packed, uint32_t *meta, void *stream);
+LRBI_API lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, int32_t rows, int32_t cols, int32_t group,
+                                  const uint16_t *X, int32_t batch, void *Y, int32_t y_dtype, void *stream);
+
 /* Which kernel LRBI_ALGO_AUTO would run for this layout and batch (an LRBI_ALGO_* value). */
 LRBI_API int32_t lrbi_masked_gemm_choice(const lrbi_layout *layout, int32_t batch);
 

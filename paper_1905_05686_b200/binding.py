@@ -115,6 +115,34 @@ def lib():
         L.lrbi_nmf_workspace.restype = ctypes.c_size_t
         L.lrbi_nmf_update.argtypes = [lp, vp, vp, vp, i32, ctypes.c_float, vp, ctypes.c_size_t, vp]
         L.lrbi_nmf_update.restype = i32
+        i64, f32, sz = ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+        L.lrbi_checkpoint_pitch.argtypes = [i32]
+        L.lrbi_checkpoint_pitch.restype = i32
+        L.lrbi_checkpoint_groups.argtypes = [i32]
+        L.lrbi_checkpoint_groups.restype = i32
+        L.lrbi_checkpoint_store.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+        L.lrbi_checkpoint_store.restype = i32
+        L.lrbi_checkpoint_load.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp]
+        L.lrbi_checkpoint_load.restype = i32
+        L.lrbi_layer_norm.argtypes = [vp, i32, i64, i32, i32, vp, vp, i32, f32, vp, i32, i64, vp, vp, vp, vp, vp]
+        L.lrbi_layer_norm.restype = i32
+        L.lrbi_layer_norm_backward_workspace.argtypes = [i32, i32]
+        L.lrbi_layer_norm_backward_workspace.restype = sz
+        L.lrbi_layer_norm_backward.argtypes = [vp, i32, i64, vp, i32, i64, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, i64, vp, i32, i64,
+                                               vp, i64, vp, vp, vp, sz, vp]
+        L.lrbi_layer_norm_backward.restype = i32
+        L.lrbi_activation.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i64, vp, vp, vp]
+        L.lrbi_activation.restype = i32
+        L.lrbi_activation_backward.argtypes = [vp, i32, i64, vp, i32, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp, i64, vp]
+        L.lrbi_activation_backward.restype = i32
+        L.lrbi_w4_packed_words.argtypes = [i32, i32]
+        L.lrbi_w4_packed_words.restype = sz
+        L.lrbi_w4_meta_words.argtypes = [i32, i32, i32]
+        L.lrbi_w4_meta_words.restype = sz
+        L.lrbi_w4_quantize.argtypes = [lp, vp, vp, vp, i32, vp, vp, vp]
+        L.lrbi_w4_quantize.restype = i32
+        L.lrbi_w4_gemv.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, i32, vp]
+        L.lrbi_w4_gemv.restype = i32
         L.lrbi_launch_count.argtypes = []
         L.lrbi_launch_count.restype = ctypes.c_uint64
         L.lrbi_device_status.argtypes = [i32]
@@ -417,6 +445,262 @@ def lrbi_masked_gemm_static(layer, W: torch.Tensor, ip: torch.Tensor, iz: torch.
                                        _dev(Y, Y.dtype, "Y"), code, _stream_ptr(stream))
     if rc != OK:
         raise LrbiError(rc, "lrbi_masked_gemm_static")
+    return Y
+
+
+# ---------------------------------------------------------------------------------------------
+# Around the layers: layer norm, 8-bit copies, the nonlinearity, 4-bit weights
+# ---------------------------------------------------------------------------------------------
+CHECKPOINT_GROUP = 128
+ACTIVATIONS = {"relu": 0, "gelu": 1, "silu": 2}
+_DTYPE = {torch.bfloat16: Y_BF16, torch.float32: Y_F32}
+
+
+def _rows(t: torch.Tensor, what, like=None):
+    """(pointer, type code, row stride) of a [rows, cols] CUDA matrix with unit column stride."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or not t.is_cuda or t.dtype not in _DTYPE:
+        raise TypeError("%s must be a [rows, cols] CUDA tensor of bfloat16 or float32" % what)
+    if like is not None and (t.shape != like.shape or t.device != like.device):
+        raise ValueError("%s must have the shape and device of the call's input" % what)
+    rows, cols = t.shape
+    stride = t.stride(0) if rows > 1 else cols
+    if cols < 1 or (cols > 1 and t.stride(1) != 1) or stride < cols:
+        raise ValueError("%s must have unit column stride and rows that do not overlap" % what)
+    return t.data_ptr(), _DTYPE[t.dtype], stride
+
+
+def _params(gamma, beta, cols, device):
+    """(gamma pointer, beta pointer, type code)."""
+    for p, what in ((gamma, "gamma"), (beta, "beta")):
+        if p is None and what == "beta":
+            continue
+        if not isinstance(p, torch.Tensor) or p.dtype not in _DTYPE or not p.is_contiguous() or p.device != device:
+            raise TypeError("%s must be a contiguous bfloat16 or float32 tensor on the call's device" % what)
+        if p.numel() != cols or p.dtype != gamma.dtype:
+            raise ValueError("%s must hold one value per column, in gamma's type" % what)
+    return gamma.data_ptr(), None if beta is None else beta.data_ptr(), _DTYPE[gamma.dtype]
+
+
+def _statistics(t, rows, device, what):
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device or t.numel() != rows:
+        raise TypeError("%s must be a contiguous float32 tensor with one value per row" % what)
+    return t.data_ptr()
+
+
+def _call_stream(device, stream, *tensors):
+    """The stream's handle.  On a stream that is not the current one, what the call allocated is kept for that stream."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError("the call's tensors must be on the current CUDA device")
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _check(rc, what):
+    if rc != OK:
+        raise LrbiError(rc, what)
+
+
+class Checkpoint:
+    """A matrix kept in 8 bits: q [rows, pitch] int8, scale [rows, groups] float32 (one per CHECKPOINT_GROUP columns of a row)."""
+
+    __slots__ = ("q", "scale", "rows", "cols")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, rows: int, cols: int):
+        pitch, groups = (cols + 15) // 16 * 16, -(-cols // CHECKPOINT_GROUP)
+        if q.dtype != torch.int8 or scale.dtype != torch.float32 or not q.is_contiguous() or not scale.is_contiguous():
+            raise TypeError("q must be contiguous int8 and scale contiguous float32")
+        if q.shape != (rows, pitch) or scale.shape != (rows, groups) or q.device != scale.device or not q.is_cuda:
+            raise ValueError("q must be [rows, %d] and scale [rows, %d] on one CUDA device" % (pitch, groups))
+        self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "Checkpoint":
+        q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)
+        return cls(q, torch.empty((rows, -(-cols // CHECKPOINT_GROUP)), dtype=torch.float32, device=device), rows, cols)
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    @property
+    def nbytes(self):
+        return self.q.numel() + 4 * self.scale.numel()
+
+
+def _kept_or_rows(x, like, what):
+    """(pointer, type code, stride, q, scale) of a matrix or of its 8-bit copy."""
+    if isinstance(x, Checkpoint):
+        if x.shape != tuple(like.shape) or x.q.device != like.device:
+            raise ValueError("%s must have the shape and device of the call's input" % what)
+        return None, Y_BF16, x.cols, x.q.data_ptr(), x.scale.data_ptr()
+    return (*_rows(x, what, like), None, None)
+
+
+def lrbi_checkpoint_store(x: torch.Tensor, stream=None) -> Checkpoint:
+    """The 8-bit copy of x [rows, cols] (bf16 or fp32)."""
+    ptr, dtype, stride = _rows(x, "x")
+    rows, cols = x.shape
+    kept = Checkpoint.empty(rows, cols, x.device)
+    s = _call_stream(x.device, stream, kept.q, kept.scale)
+    _check(lib().lrbi_checkpoint_store(ptr, dtype, stride, rows, cols, kept.q.data_ptr(), kept.scale.data_ptr(), s), "lrbi_checkpoint_store")
+    return kept
+
+
+def lrbi_checkpoint_load(kept: Checkpoint, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """What an 8-bit copy stands for, as a new [rows, cols] tensor of `dtype`."""
+    if not isinstance(kept, Checkpoint):
+        raise TypeError("kept must be a Checkpoint")
+    x = torch.empty((kept.rows, kept.cols), dtype=dtype, device=kept.q.device)
+    ptr, code, stride = _rows(x, "x")
+    s = _call_stream(x.device, stream, x)
+    _check(lib().lrbi_checkpoint_load(kept.q.data_ptr(), kept.scale.data_ptr(), kept.rows, kept.cols, ptr, code, stride, s), "lrbi_checkpoint_load")
+    return x
+
+
+def lrbi_layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None = None, eps: float = 1e-5, y_dtype=None,
+                    checkpoint: bool = False, stream=None):
+    """Layer norm over the columns of x [rows, cols].  Returns (y, mean, rstd), and the 8-bit copy of x with checkpoint=True."""
+    ptr, dtype, stride = _rows(x, "x")
+    rows, cols = x.shape
+    dev = x.device
+    g, b, pt = _params(gamma, beta, cols, dev)
+    y = torch.empty((rows, cols), dtype=x.dtype if y_dtype is None else y_dtype, device=dev)
+    yp, yt, ys = _rows(y, "y")
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    kept = Checkpoint.empty(rows, cols, dev) if checkpoint else None
+    q, scale = (kept.q, kept.scale) if checkpoint else (None, None)
+    s = _call_stream(dev, stream, y, mean, q, scale)
+    _check(lib().lrbi_layer_norm(ptr, dtype, stride, rows, cols, g, b, pt, eps, yp, yt, ys, mean.data_ptr(), rstd.data_ptr(),
+                                 q.data_ptr() if checkpoint else None, scale.data_ptr() if checkpoint else None, s), "lrbi_layer_norm")
+    return (y, mean, rstd, kept) if checkpoint else (y, mean, rstd)
+
+
+def lrbi_layer_norm_backward(dy: torch.Tensor, x, gamma: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                             beta: torch.Tensor | None = None, dres: torch.Tensor | None = None, restore: bool = False, dx_dtype=None,
+                             stream=None):
+    """Gradients of the layer norm: x is the forward input or its Checkpoint.  Returns (dx, dgamma, dbeta), dgamma and dbeta in
+    fp32, and the forward result again with restore=True (in dy's type; pass the beta of the forward pass).  dres is added to dx."""
+    dyp, dyt, dys = _rows(dy, "dy")
+    rows, cols = dy.shape
+    dev = dy.device
+    xp, xt, xs, q, scale = _kept_or_rows(x, dy, "x")
+    g, b, pt = _params(gamma, beta, cols, dev)
+    m, r = _statistics(mean, rows, dev, "mean"), _statistics(rstd, rows, dev, "rstd")
+    if dx_dtype is None:
+        dx_dtype = dy.dtype if isinstance(x, Checkpoint) else x.dtype
+    rp, rs = None, cols
+    if dres is not None:
+        rp, rt, rs = _rows(dres, "dres", dy)
+        if dres.dtype != dx_dtype:
+            raise ValueError("dres must have dx's type")
+    dx = torch.empty((rows, cols), dtype=dx_dtype, device=dev)
+    dxp, dxt, dxs = _rows(dx, "dx")
+    y = torch.empty((rows, cols), dtype=dy.dtype, device=dev) if restore else None
+    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dev).unbind(0)
+    L = lib()
+    need = L.lrbi_layer_norm_backward_workspace(rows, cols)
+    work = torch.empty(need, dtype=torch.uint8, device=dev)
+    s = _call_stream(dev, stream, dx, y, dgamma, work)
+    _check(L.lrbi_layer_norm_backward(dyp, dyt, dys, xp, xt, xs, q, scale, rows, cols, g, b, pt, m, r, rp, rs, dxp, dxt, dxs,
+                                      y.data_ptr() if restore else None, cols, dgamma.data_ptr(), dbeta.data_ptr(), work.data_ptr(), need, s),
+           "lrbi_layer_norm_backward")
+    return (dx, dgamma, dbeta, y) if restore else (dx, dgamma, dbeta)
+
+
+def _act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
+    return ACTIVATIONS[act]
+
+
+def lrbi_activation(h: torch.Tensor, act: str, a_dtype=None, checkpoint: bool = False, stream=None):
+    """a = act(h) for act "relu", "gelu" or "silu".  Returns a, or (a, the 8-bit copy of h) with checkpoint=True."""
+    code = _act(act)
+    ptr, dtype, stride = _rows(h, "h")
+    rows, cols = h.shape
+    a = torch.empty((rows, cols), dtype=h.dtype if a_dtype is None else a_dtype, device=h.device)
+    ap, at, as_ = _rows(a, "a")
+    kept = Checkpoint.empty(rows, cols, h.device) if checkpoint else None
+    q, scale = (kept.q, kept.scale) if checkpoint else (None, None)
+    s = _call_stream(h.device, stream, a, q, scale)
+    _check(lib().lrbi_activation(ptr, dtype, stride, rows, cols, code, ap, at, as_, q.data_ptr() if checkpoint else None,
+                                 scale.data_ptr() if checkpoint else None, s), "lrbi_activation")
+    return (a, kept) if checkpoint else a
+
+
+def lrbi_activation_backward(da: torch.Tensor, h, act: str, restore: bool = False, dh_dtype=None, stream=None):
+    """dh = da * act'(h): h is the forward input or its Checkpoint.  Returns dh, or (dh, act(h) in da's type) with restore=True."""
+    code = _act(act)
+    dap, dat, das = _rows(da, "da")
+    rows, cols = da.shape
+    hp, ht, hs, q, scale = _kept_or_rows(h, da, "h")
+    dh = torch.empty((rows, cols), dtype=da.dtype if dh_dtype is None else dh_dtype, device=da.device)
+    dhp, dht, dhs = _rows(dh, "dh")
+    a = torch.empty((rows, cols), dtype=da.dtype, device=da.device) if restore else None
+    s = _call_stream(da.device, stream, dh, a)
+    _check(lib().lrbi_activation_backward(dap, dat, das, hp, ht, hs, q, scale, rows, cols, code, dhp, dht, dhs,
+                                          a.data_ptr() if restore else None, cols, s), "lrbi_activation_backward")
+    return (dh, a) if restore else dh
+
+
+class W4Weights:
+    """A layer's weights in 4 bits as the library lays them out (lrbi.h): packed and meta are int32 CUDA tensors."""
+
+    __slots__ = ("packed", "meta", "rows", "cols", "group")
+
+    def __init__(self, packed: torch.Tensor, meta: torch.Tensor, rows: int, cols: int, group: int):
+        if group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        tiles = -(-rows // 16)
+        for t, n, what in ((packed, tiles * -(-cols // 64) * 128, "packed"), (meta, tiles * -(-cols // group) * 16, "meta")):
+            _dev(t, torch.int32, what)
+            if t.numel() != n or t.device != packed.device:
+                raise ValueError("%s must hold %d words on one device" % (what, n))
+        self.packed, self.meta, self.rows, self.cols, self.group = packed, meta, rows, cols, group
+
+    @property
+    def nbytes(self):
+        return 4 * (self.packed.numel() + self.meta.numel())
+
+
+def lrbi_w4_quantize(layer, W: torch.Tensor, group: int = 128, ip: torch.Tensor | None = None, iz: torch.Tensor | None = None,
+                     stream=None) -> W4Weights:
+    """Quantises W [rows, cols] bf16 to 4 bits; with the layer's packed factors, pruned weights are exactly zero."""
+    lay = Layout.of(layer)
+    L = lib()
+    if tuple(W.shape) != (lay.rows, lay.cols):
+        raise ValueError("W shape does not match the layout")
+    if (ip is None) != (iz is None):
+        raise ValueError("ip and iz come together")
+    if ip is not None and (ip.numel() != L.lrbi_packed_ip_words(ctypes.byref(lay)) or iz.numel() != L.lrbi_packed_iz_words(ctypes.byref(lay))):
+        raise ValueError("packed factor sizes do not match the layout")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    w = _dev(W, torch.bfloat16, "W")
+    factors = [None if t is None else _dev(t, torch.int32, what) for t, what in ((ip, "ip"), (iz, "iz"))]
+    packed = torch.empty(L.lrbi_w4_packed_words(lay.rows, lay.cols), dtype=torch.int32, device=W.device)
+    meta = torch.empty(L.lrbi_w4_meta_words(lay.rows, lay.cols, group), dtype=torch.int32, device=W.device)
+    s = _call_stream(W.device, stream, packed, meta)
+    _check(L.lrbi_w4_quantize(ctypes.byref(lay), w, *factors, group, packed.data_ptr(), meta.data_ptr(), s), "lrbi_w4_quantize")
+    return W4Weights(packed, meta, lay.rows, lay.cols, group)
+
+
+def lrbi_w4_gemv(weights: W4Weights, X: torch.Tensor, y_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """Y [batch, rows] = X W^T for X [batch, cols] bf16 and 4-bit weights; made for a few rows of X."""
+    x = _dev(X, torch.bfloat16, "X")
+    if X.dim() != 2 or X.shape[1] != weights.cols or X.device != weights.packed.device:
+        raise ValueError("X must be [batch, cols] on the weights' device")
+    if y_dtype not in _DTYPE:
+        raise TypeError("y_dtype must be bfloat16 or float32")
+    batch = X.shape[0]
+    Y = torch.empty((batch, weights.rows), dtype=y_dtype, device=X.device)
+    s = _call_stream(X.device, stream, Y)
+    _check(lib().lrbi_w4_gemv(weights.packed.data_ptr(), weights.meta.data_ptr(), weights.rows, weights.cols, weights.group, x, batch,
+                              Y.data_ptr(), _DTYPE[y_dtype], s), "lrbi_w4_gemv")
     return Y
 
 

@@ -178,4 +178,51 @@ lrbi_status launch_threshold_pack(const Geo &g, const float *mp, const float *mz
 lrbi_status launch_index_cost(const Geo &g, const uint16_t *W, float theta, const uint32_t *ip, const uint32_t *iz,
                               lrbi_tile_cost *out, cudaStream_t s);
 
+
+// 8-bit copies: bytes of a row (padded to whole 16-byte vectors) and scales of a row.
+inline int checkpoint_pitch(int cols) { return (cols + 15) / 16 * 16; }
+inline int checkpoint_groups(int cols) { return (cols - 1) / LRBI_CHECKPOINT_GROUP + 1; }
+
+// Layer norm; null pointers for what a call does not have.
+struct NormArgs {
+    const void *x; long long x_stride; int x_dtype;      // input, or null where its 8-bit copy (q, scale) is given
+    const int8_t *q; const float *scale;
+    const void *gamma, *beta; int param_dtype;
+    float eps;
+    void *y; long long y_stride; int y_dtype;            // forward result; restored by the backward pass in dy's type
+    float *mean_out, *rstd_out;
+    int8_t *q_out; float *scale_out;
+    const void *dy; long long dy_stride; int dy_dtype;
+    const float *mean, *rstd;
+    const void *dres; long long dres_stride;             // in dx's type
+    void *dx; long long dx_stride; int dx_dtype;
+    float *dgamma, *dbeta;
+    int rows, cols;
+};
+size_t norm_backward_workspace(int rows, int cols);
+lrbi_status launch_layer_norm(const NormArgs &n, cudaStream_t s);
+lrbi_status launch_layer_norm_backward(const NormArgs &n, float *workspace, cudaStream_t s);
+
+// Activations and 8-bit copies.
+struct ActArgs {
+    const void *h; long long h_stride; int h_dtype;
+    const int8_t *q; const float *scale;
+    int act;
+    void *a; long long a_stride; int a_dtype;
+    int8_t *q_out; float *scale_out;
+    const void *da; long long da_stride; int da_dtype;
+    void *dh; long long dh_stride; int dh_dtype;
+    int rows, cols;
+};
+lrbi_status launch_checkpoint_store(const void *x, int dtype, long long stride, int rows, int cols, int8_t *q, float *scale, cudaStream_t s);
+lrbi_status launch_checkpoint_load(const int8_t *q, const float *scale, int rows, int cols, void *x, int dtype, long long stride, cudaStream_t s);
+lrbi_status launch_activation(const ActArgs &n, cudaStream_t s);
+lrbi_status launch_activation_backward(const ActArgs &n, cudaStream_t s);
+
+// 4-bit weights.
+lrbi_status launch_w4_gemv(const uint32_t *packed, const uint32_t *meta, int rows, int cols, int group, const uint16_t *X, int batch, void *Y,
+                           int y_dtype, cudaStream_t s);
+lrbi_status launch_w4_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int group, uint32_t *packed, uint32_t *meta,
+                               cudaStream_t s);
+
 }  // namespace lrbi
