@@ -2,12 +2,14 @@
 
 Every step of the path (decode, pruning, product) runs in the CUDA library; this module turns
 torch CUDA tensors into device pointers and checks return codes.  torch is used for device
-memory and streams.  If the library is not built, importing a compute function's first call
+memory and streams.  The calls made per layer and per token around the masked layers are marshalled by a small
+compiled module (_lrbi_torch.so) that calls the same C ABI.  If the library is not built, importing a compute function's first call
 raises: there is no CPU fallback.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 
 import numpy as np
@@ -17,6 +19,7 @@ from .synth import Layer
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblrbi.so")
+CALLS_PATH = os.path.join(_HERE, "_lrbi_torch.so")
 
 ALGO_AUTO, ALGO_GENERIC, ALGO_GEMV, ALGO_TENSOR, ALGO_DECODE_BALLOT, ALGO_DECODE_PLANES, ALGO_DECODE_PLANES_WIDE, ALGO_STREAM, ALGO_TENSOR_PAIR, ALGO_TENSOR_PAIR2, ALGO_TENSOR_PAIR192 = range(11)
 ALGO_NAMES = {0: "auto", 1: "generic", 2: "gemv", 3: "tensor", 4: "decode_ballot", 5: "decode_planes", 6: "decode_planes_wide", 7: "stream", 8: "tensor_pair", 9: "tensor_pair2", 10: "tensor_pair192"}
@@ -453,55 +456,22 @@ def lrbi_masked_gemm_static(layer, W: torch.Tensor, ip: torch.Tensor, iz: torch.
 # ---------------------------------------------------------------------------------------------
 CHECKPOINT_GROUP = 128
 ACTIVATIONS = {"relu": 0, "gelu": 1, "silu": 2}
-_DTYPE = {torch.bfloat16: Y_BF16, torch.float32: Y_F32}
+_calls = None
 
 
-def _rows(t: torch.Tensor, what, like=None):
-    """(pointer, type code, row stride) of a [rows, cols] CUDA matrix with unit column stride."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or not t.is_cuda or t.dtype not in _DTYPE:
-        raise TypeError("%s must be a [rows, cols] CUDA tensor of bfloat16 or float32" % what)
-    if like is not None and (t.shape != like.shape or t.device != like.device):
-        raise ValueError("%s must have the shape and device of the call's input" % what)
-    rows, cols = t.shape
-    stride = t.stride(0) if rows > 1 else cols
-    if cols < 1 or (cols > 1 and t.stride(1) != 1) or stride < cols:
-        raise ValueError("%s must have unit column stride and rows that do not overlap" % what)
-    return t.data_ptr(), _DTYPE[t.dtype], stride
-
-
-def _params(gamma, beta, cols, device):
-    """(gamma pointer, beta pointer, type code)."""
-    for p, what in ((gamma, "gamma"), (beta, "beta")):
-        if p is None and what == "beta":
-            continue
-        if not isinstance(p, torch.Tensor) or p.dtype not in _DTYPE or not p.is_contiguous() or p.device != device:
-            raise TypeError("%s must be a contiguous bfloat16 or float32 tensor on the call's device" % what)
-        if p.numel() != cols or p.dtype != gamma.dtype:
-            raise ValueError("%s must hold one value per column, in gamma's type" % what)
-    return gamma.data_ptr(), None if beta is None else beta.data_ptr(), _DTYPE[gamma.dtype]
-
-
-def _statistics(t, rows, device, what):
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or not t.is_contiguous() or t.device != device or t.numel() != rows:
-        raise TypeError("%s must be a contiguous float32 tensor with one value per row" % what)
-    return t.data_ptr()
-
-
-def _call_stream(device, stream, *tensors):
-    """The stream's handle.  On a stream that is not the current one, what the call allocated is kept for that stream."""
-    if device.index != torch.cuda.current_device():
-        raise ValueError("the call's tensors must be on the current CUDA device")
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return stream.cuda_stream
-
-
-def _check(rc, what):
-    if rc != OK:
-        raise LrbiError(rc, what)
+def _native():
+    """The module that checks tensors, allocates outputs and calls the C ABI (csrc/torch_calls.cpp); raises if it has not been built."""
+    global _calls
+    if _calls is None:
+        lib()
+        if not os.path.exists(CALLS_PATH):
+            raise RuntimeError("lrbi call module missing: %s (run paper_1905_05686_b200/build.py)" % CALLS_PATH)
+        spec = importlib.util.spec_from_file_location("_lrbi_torch", CALLS_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.set_error(LrbiError)
+        _calls = module
+    return _calls
 
 
 class Checkpoint:
@@ -522,6 +492,12 @@ class Checkpoint:
         q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)
         return cls(q, torch.empty((rows, -(-cols // CHECKPOINT_GROUP)), dtype=torch.float32, device=device), rows, cols)
 
+    @classmethod
+    def _of(cls, q, scale, rows, cols):
+        kept = object.__new__(cls)
+        kept.q, kept.scale, kept.rows, kept.cols = q, scale, rows, cols
+        return kept
+
     @property
     def shape(self):
         return (self.rows, self.cols)
@@ -532,119 +508,59 @@ class Checkpoint:
 
 
 def _kept_or_rows(x, like, what):
-    """(pointer, type code, stride, q, scale) of a matrix or of its 8-bit copy."""
-    if isinstance(x, Checkpoint):
-        if x.shape != tuple(like.shape) or x.q.device != like.device:
-            raise ValueError("%s must have the shape and device of the call's input" % what)
-        return None, Y_BF16, x.cols, x.q.data_ptr(), x.scale.data_ptr()
-    return (*_rows(x, what, like), None, None)
+    """(matrix, q, scale): a matrix, or its 8-bit copy."""
+    if not isinstance(x, Checkpoint):
+        return x, None, None
+    if like.dim() != 2 or x.rows != like.shape[0] or x.cols != like.shape[1]:
+        raise ValueError("%s must have the shape of the call's input" % what)
+    return None, x.q, x.scale
 
 
 def lrbi_checkpoint_store(x: torch.Tensor, stream=None) -> Checkpoint:
     """The 8-bit copy of x [rows, cols] (bf16 or fp32)."""
-    ptr, dtype, stride = _rows(x, "x")
-    rows, cols = x.shape
-    kept = Checkpoint.empty(rows, cols, x.device)
-    s = _call_stream(x.device, stream, kept.q, kept.scale)
-    _check(lib().lrbi_checkpoint_store(ptr, dtype, stride, rows, cols, kept.q.data_ptr(), kept.scale.data_ptr(), s), "lrbi_checkpoint_store")
-    return kept
+    q, scale = _native().checkpoint_store(x, stream)
+    return Checkpoint._of(q, scale, *x.shape)
 
 
 def lrbi_checkpoint_load(kept: Checkpoint, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
     """What an 8-bit copy stands for, as a new [rows, cols] tensor of `dtype`."""
     if not isinstance(kept, Checkpoint):
         raise TypeError("kept must be a Checkpoint")
-    x = torch.empty((kept.rows, kept.cols), dtype=dtype, device=kept.q.device)
-    ptr, code, stride = _rows(x, "x")
-    s = _call_stream(x.device, stream, x)
-    _check(lib().lrbi_checkpoint_load(kept.q.data_ptr(), kept.scale.data_ptr(), kept.rows, kept.cols, ptr, code, stride, s), "lrbi_checkpoint_load")
-    return x
+    return _native().checkpoint_load(kept.q, kept.scale, kept.rows, kept.cols, dtype, stream)
 
 
 def lrbi_layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None = None, eps: float = 1e-5, y_dtype=None,
                     checkpoint: bool = False, stream=None):
     """Layer norm over the columns of x [rows, cols].  Returns (y, mean, rstd), and the 8-bit copy of x with checkpoint=True."""
-    ptr, dtype, stride = _rows(x, "x")
-    rows, cols = x.shape
-    dev = x.device
-    g, b, pt = _params(gamma, beta, cols, dev)
-    y = torch.empty((rows, cols), dtype=x.dtype if y_dtype is None else y_dtype, device=dev)
-    yp, yt, ys = _rows(y, "y")
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
-    kept = Checkpoint.empty(rows, cols, dev) if checkpoint else None
-    q, scale = (kept.q, kept.scale) if checkpoint else (None, None)
-    s = _call_stream(dev, stream, y, mean, q, scale)
-    _check(lib().lrbi_layer_norm(ptr, dtype, stride, rows, cols, g, b, pt, eps, yp, yt, ys, mean.data_ptr(), rstd.data_ptr(),
-                                 q.data_ptr() if checkpoint else None, scale.data_ptr() if checkpoint else None, s), "lrbi_layer_norm")
-    return (y, mean, rstd, kept) if checkpoint else (y, mean, rstd)
+    out = _native().layer_norm(x, gamma, beta, eps, y_dtype, checkpoint, stream)
+    return (*out[:3], Checkpoint._of(out[3], out[4], *x.shape)) if checkpoint else out
 
 
 def lrbi_layer_norm_backward(dy: torch.Tensor, x, gamma: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
                              beta: torch.Tensor | None = None, dres: torch.Tensor | None = None, restore: bool = False, dx_dtype=None,
                              stream=None):
     """Gradients of the layer norm: x is the forward input or its Checkpoint.  Returns (dx, dgamma, dbeta), dgamma and dbeta in
-    fp32, and the forward result again with restore=True (in dy's type; pass the beta of the forward pass).  dres is added to dx."""
-    dyp, dyt, dys = _rows(dy, "dy")
-    rows, cols = dy.shape
-    dev = dy.device
-    xp, xt, xs, q, scale = _kept_or_rows(x, dy, "x")
-    g, b, pt = _params(gamma, beta, cols, dev)
-    m, r = _statistics(mean, rows, dev, "mean"), _statistics(rstd, rows, dev, "rstd")
-    if dx_dtype is None:
-        dx_dtype = dy.dtype if isinstance(x, Checkpoint) else x.dtype
-    rp, rs = None, cols
-    if dres is not None:
-        rp, rt, rs = _rows(dres, "dres", dy)
-        if dres.dtype != dx_dtype:
-            raise ValueError("dres must have dx's type")
-    dx = torch.empty((rows, cols), dtype=dx_dtype, device=dev)
-    dxp, dxt, dxs = _rows(dx, "dx")
-    y = torch.empty((rows, cols), dtype=dy.dtype, device=dev) if restore else None
-    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dev).unbind(0)
-    L = lib()
-    need = L.lrbi_layer_norm_backward_workspace(rows, cols)
-    work = torch.empty(need, dtype=torch.uint8, device=dev)
-    s = _call_stream(dev, stream, dx, y, dgamma, work)
-    _check(L.lrbi_layer_norm_backward(dyp, dyt, dys, xp, xt, xs, q, scale, rows, cols, g, b, pt, m, r, rp, rs, dxp, dxt, dxs,
-                                      y.data_ptr() if restore else None, cols, dgamma.data_ptr(), dbeta.data_ptr(), work.data_ptr(), need, s),
-           "lrbi_layer_norm_backward")
-    return (dx, dgamma, dbeta, y) if restore else (dx, dgamma, dbeta)
+    fp32, and the forward result again with restore=True (in dy's type; pass the beta of the forward pass).  dres is added to dx,
+    which has x's type, or dy's where x is a Checkpoint, unless dx_dtype says otherwise."""
+    return _native().layer_norm_backward(dy, *_kept_or_rows(x, dy, "x"), gamma, mean, rstd, beta, dres, restore, dx_dtype, stream)
 
 
 def _act(act):
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError("act must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
-    return ACTIVATIONS[act]
+    return code
 
 
 def lrbi_activation(h: torch.Tensor, act: str, a_dtype=None, checkpoint: bool = False, stream=None):
     """a = act(h) for act "relu", "gelu" or "silu".  Returns a, or (a, the 8-bit copy of h) with checkpoint=True."""
-    code = _act(act)
-    ptr, dtype, stride = _rows(h, "h")
-    rows, cols = h.shape
-    a = torch.empty((rows, cols), dtype=h.dtype if a_dtype is None else a_dtype, device=h.device)
-    ap, at, as_ = _rows(a, "a")
-    kept = Checkpoint.empty(rows, cols, h.device) if checkpoint else None
-    q, scale = (kept.q, kept.scale) if checkpoint else (None, None)
-    s = _call_stream(h.device, stream, a, q, scale)
-    _check(lib().lrbi_activation(ptr, dtype, stride, rows, cols, code, ap, at, as_, q.data_ptr() if checkpoint else None,
-                                 scale.data_ptr() if checkpoint else None, s), "lrbi_activation")
-    return (a, kept) if checkpoint else a
+    out = _native().activation(h, _act(act), a_dtype, checkpoint, stream)
+    return (out[0], Checkpoint._of(out[1], out[2], *h.shape)) if checkpoint else out
 
 
 def lrbi_activation_backward(da: torch.Tensor, h, act: str, restore: bool = False, dh_dtype=None, stream=None):
     """dh = da * act'(h): h is the forward input or its Checkpoint.  Returns dh, or (dh, act(h) in da's type) with restore=True."""
-    code = _act(act)
-    dap, dat, das = _rows(da, "da")
-    rows, cols = da.shape
-    hp, ht, hs, q, scale = _kept_or_rows(h, da, "h")
-    dh = torch.empty((rows, cols), dtype=da.dtype if dh_dtype is None else dh_dtype, device=da.device)
-    dhp, dht, dhs = _rows(dh, "dh")
-    a = torch.empty((rows, cols), dtype=da.dtype, device=da.device) if restore else None
-    s = _call_stream(da.device, stream, dh, a)
-    _check(lib().lrbi_activation_backward(dap, dat, das, hp, ht, hs, q, scale, rows, cols, code, dhp, dht, dhs,
-                                          a.data_ptr() if restore else None, cols, s), "lrbi_activation_backward")
-    return (dh, a) if restore else dh
+    return _native().activation_backward(da, *_kept_or_rows(h, da, "h"), _act(act), restore, dh_dtype, stream)
 
 
 class W4Weights:
@@ -684,24 +600,18 @@ def lrbi_w4_quantize(layer, W: torch.Tensor, group: int = 128, ip: torch.Tensor 
     factors = [None if t is None else _dev(t, torch.int32, what) for t, what in ((ip, "ip"), (iz, "iz"))]
     packed = torch.empty(L.lrbi_w4_packed_words(lay.rows, lay.cols), dtype=torch.int32, device=W.device)
     meta = torch.empty(L.lrbi_w4_meta_words(lay.rows, lay.cols, group), dtype=torch.int32, device=W.device)
-    s = _call_stream(W.device, stream, packed, meta)
-    _check(L.lrbi_w4_quantize(ctypes.byref(lay), w, *factors, group, packed.data_ptr(), meta.data_ptr(), s), "lrbi_w4_quantize")
+    if stream is not None:
+        packed.record_stream(stream)
+        meta.record_stream(stream)
+    rc = L.lrbi_w4_quantize(ctypes.byref(lay), w, *factors, group, packed.data_ptr(), meta.data_ptr(), _stream_ptr(stream))
+    if rc != OK:
+        raise LrbiError(rc, "lrbi_w4_quantize")
     return W4Weights(packed, meta, lay.rows, lay.cols, group)
 
 
 def lrbi_w4_gemv(weights: W4Weights, X: torch.Tensor, y_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
     """Y [batch, rows] = X W^T for X [batch, cols] bf16 and 4-bit weights; made for a few rows of X."""
-    x = _dev(X, torch.bfloat16, "X")
-    if X.dim() != 2 or X.shape[1] != weights.cols or X.device != weights.packed.device:
-        raise ValueError("X must be [batch, cols] on the weights' device")
-    if y_dtype not in _DTYPE:
-        raise TypeError("y_dtype must be bfloat16 or float32")
-    batch = X.shape[0]
-    Y = torch.empty((batch, weights.rows), dtype=y_dtype, device=X.device)
-    s = _call_stream(X.device, stream, Y)
-    _check(lib().lrbi_w4_gemv(weights.packed.data_ptr(), weights.meta.data_ptr(), weights.rows, weights.cols, weights.group, x, batch,
-                              Y.data_ptr(), _DTYPE[y_dtype], s), "lrbi_w4_gemv")
-    return Y
+    return _native().w4_gemv(weights.packed, weights.meta, weights.rows, weights.cols, weights.group, X, y_dtype, stream)
 
 
 class HostLayer:
