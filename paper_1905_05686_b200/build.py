@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblrbi.so")
 SOURCES = ["api.cu", "decode_kernels.cu", "gemv_kernels.cu", "gemm_tc.cu", "alg1_kernels.cu", "ranked_kernels.cu", "backward_kernels.cu", "nmf_kernels.cu",
-           "norm_kernels.cu", "keep_kernels.cu", "w4_kernels.cu", "api_block.cu"]
+           "norm_forward.cu", "norm_backward.cu", "keep_kernels.cu", "w4_kernels.cu", "api_block.cu"]
 CALLS = os.path.join(HERE, "_lrbi_torch.so")
 CALLS_SOURCE = os.path.join(CSRC, "torch_calls.cpp")
 

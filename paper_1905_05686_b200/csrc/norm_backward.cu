@@ -1,0 +1,520 @@
+// Layer norm, backward:  with n = (x - mean) * rstd and g = dy * gamma,
+//     dx = dres + rstd * (g - mean(g) - n * mean(g * n)),   dgamma = sum over rows of dy * n,   dbeta = sum of dy;
+// x as it was, or its 8-bit copy; optionally n * gamma + beta again, the forward result of that copy.
+//
+// A thread has the same columns in every row, so that the sums over rows stay in its registers; a group of threads has a
+// whole row, and takes R rows at a time, so that the sums over columns share their shuffles and one barrier.  Rows come
+// through a ring in shared memory, filled by asynchronous copies some rounds ahead, one block per SM.
+// Rows go round the groups in a fixed order, a block's groups and then the blocks are summed in order: the parameters'
+// gradients have the same bits in every run.
+#include <algorithm>
+#include <type_traits>
+
+#include "norm_common.cuh"
+
+namespace lrbi {
+
+struct NormBackward {
+    RowsIn dy, x, dres;    // dres.data null: nothing added; x unused when the copy is given
+    KeptIn kept;
+    Params p;
+    const float *mean, *rstd;
+    RowsOut dx, y;         // y.data null: the forward result is not restored
+    int dres_dtype;
+    float *part;           // [gridDim.x][2][pitch]: sums over the rows of a block
+    int rows, cols, pitch; // pitch: cols rounded up to whole chunks
+};
+
+template <bool STRIDED>
+__device__ __forceinline__ void add_residual(const NormBackward &a, long long row, int c, F2 (&v)[PAIRS])
+{
+    F2 r[PAIRS];
+    if (a.dres_dtype == LRBI_Y_BF16) { Raw<SRC_BF16, STRIDED> w; w.load(a.dres, KeptIn{}, row, c, a.cols); w.get(r); }
+    else { Raw<SRC_F32, STRIDED> w; w.load(a.dres, KeptIn{}, row, c, a.cols); w.get(r); }
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) v[i] = v[i] + r[i];
+}
+
+constexpr int BACK_THREADS = 512;
+
+// blockDim = (threads of a row, rows side by side).  A thread has NV chunks of R rows at a time and keeps its columns' sums
+// and their gamma in registers.  Vector rows come through a ring of STAGES rounds in shared memory, each thread copying what
+// it reads itself; strided rows are loaded into registers a round ahead.  What is left to bound it is the number of
+// instructions a value: addresses are one multiply-add each, and rounds that are whole check nothing.
+template <int DY, int SRC, int OUT, bool STRIDED, bool EXTRA, int NV, int R>
+__global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBackward a)
+{
+    constexpr int STAGES = 3, WARPS = BACK_THREADS / 32;
+    constexpr int DSIZE = DY == SRC_F32 ? 4 : 2, XSIZE = SRC == SRC_F32 ? 4 : SRC == SRC_BF16 ? 2 : 1, OSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
+    constexpr int DBYTES = CHUNK * DSIZE, XBYTES = SRC == SRC_KEPT ? 16 : CHUNK * XSIZE;     // of a chunk in the ring
+    extern __shared__ float4 shared[];          // the ring: [STAGES][R][NV][dy, x][threads]
+    __shared__ float part[2][2 * R * WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + threadIdx.x, id = 1 + threadIdx.y;
+    const float over = 1.f / (float)a.cols;
+    const int c0 = lane_column<STRIDED>(warp * SPAN, lane), apart = warps * SPAN;
+    const int left = a.cols - c0;               // columns from the thread's first one on
+    F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS], gamma[NV][PAIRS];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        load_param<STRIDED>(a.p.gamma, a.p, c0 + j * apart, a.cols, 0.f, gamma[j]);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) { dgamma[j][i] = f2(0.f); dbeta[j][i] = f2(0.f); }
+    }
+    const char *dy0 = static_cast<const char *>(a.dy.data) + c0 * DSIZE;
+    const char *x0 = SRC == SRC_KEPT ? reinterpret_cast<const char *>(a.kept.q + c0) : static_cast<const char *>(a.x.data) + c0 * XSIZE;
+    char *dx0 = static_cast<char *>(a.dx.data) + c0 * OSIZE, *y0 = static_cast<char *>(a.y.data) + c0 * DSIZE;
+    const char *res0 = static_cast<const char *>(a.dres.data) + c0 * OSIZE;
+    const uint32_t dy_row = (uint32_t)(a.dy.stride * DSIZE), x_row = SRC == SRC_KEPT ? (uint32_t)a.kept.pitch : (uint32_t)(a.x.stride * XSIZE);
+    const uint32_t dx_row = (uint32_t)(a.dx.stride * OSIZE), y_row = (uint32_t)(a.y.stride * DSIZE), res_row = (uint32_t)(a.dres.stride * OSIZE);
+    const uint32_t step = gridDim.x * blockDim.y * R, rows = (uint32_t)a.rows;
+    uint32_t row = (threadIdx.y * gridDim.x + blockIdx.x) * R;
+
+    char *ring = reinterpret_cast<char *>(shared);
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(shared);
+    const int chunk_bytes = (DBYTES + XBYTES) * threads, round_bytes = R * NV * chunk_bytes;
+    auto ask = [&](uint32_t first, int at) {    // vector rows
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (first + r < rows && j * apart < left) {
+                    const char *d = dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, *x = x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE;
+                    const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes, to_x = to + DBYTES * threads;
+#pragma unroll
+                    for (int i = 0; i < DBYTES / 16; ++i) copy_async(to + (i * threads + me) * 16, d + 16 * i, 16);
+                    if constexpr (SRC == SRC_KEPT) {
+                        copy_async(to_x + me * 8, x, 8);
+                        copy_async(to_x + threads * 8 + me * 4, a.kept.scale + (uint64_t)(first + r) * (uint32_t)a.kept.groups + (c0 + j * apart) / KEEP_GROUP, 4);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < XBYTES / 16; ++i) copy_async(to_x + (i * threads + me) * 16, x + 16 * i, 16);
+                    }
+                }
+        copies_asked();
+    };
+    Raw<DY, STRIDED> raw_dy[R][NV];
+    Raw<SRC, STRIDED> raw_x[R][NV];
+    auto take = [&](int at) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const char *from = ring + at * round_bytes + (r * NV + j) * chunk_bytes, *from_x = from + DBYTES * threads;
+                raw_dy[r][j].clear();
+                raw_x[r][j].clear();
+                if (j * apart < left) {
+#pragma unroll
+                    for (int i = 0; i < DBYTES / 16; ++i) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(from + (i * threads + me) * 16);
+                        uint32_t *w = raw_dy[r][j].w + (STRIDED ? 0 : 4 * i);
+                        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                    }
+                    if constexpr (SRC == SRC_KEPT) {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(from_x + me * 8);
+                        raw_x[r][j].w[0] = v.x;
+                        raw_x[r][j].w[1] = v.y;
+                        raw_x[r][j].scale[0] = *reinterpret_cast<const float *>(from_x + threads * 8 + me * 4);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < XBYTES / 16; ++i) {
+                            const uint4 v = *reinterpret_cast<const uint4 *>(from_x + (i * threads + me) * 16);
+                            uint32_t *w = raw_x[r][j].w + (STRIDED ? 0 : 4 * i);
+                            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                        }
+                    }
+                }
+            }
+    };
+    auto load = [&](uint32_t first) {           // strided rows
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int there = first + r < rows ? left - j * apart : 0;
+                raw_dy[r][j].load_at(dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, there);
+                if constexpr (SRC == SRC_KEPT) raw_x[r][j].load(a.x, a.kept, first + r, c0 + j * apart, first + r < rows ? a.cols : 0);
+                else raw_x[r][j].load_at(x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE, there);
+            }
+    };
+    float mean[R], rstd[R];                     // of the round to come
+    auto statistics = [&](uint32_t first) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = rstd[r] = 0.f;
+            if (first + r < rows) { mean[r] = __ldg(a.mean + first + r); rstd[r] = __ldg(a.rstd + first + r); }
+        }
+    };
+    int at = 0, turn = 0;
+    // One round; `whole`: all R rows are there.
+    auto round = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        if constexpr (!STRIDED) {
+            ask(row + (STAGES - 1) * step, at == 0 ? STAGES - 1 : at - 1);      // the place that the last round was taken from
+            copies_wait<STAGES - 1>();
+            take(at);
+            at = at + 1 == STAGES ? 0 : at + 1;
+        }
+        F2 g[R][NV][PAIRS], n[R][NV][PAIRS], scale[R];      // dy * gamma, and the normalised input
+        float both[2 * R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const F2 less = f2(-mean[r]);
+            scale[r] = f2(rstd[r]);
+            F2 sg = f2(0.f), sgn = f2(0.f);
+            if (!WHOLE && row + r >= rows) {
+                both[2 * r] = both[2 * r + 1] = 0.f;
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                F2 v[PAIRS], w[PAIRS];
+                raw_dy[r][j].get(v);            // zeros past the last column, in dy and in gamma
+                raw_x[r][j].get(w);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    w[i] = (w[i] + less) * scale[r];
+                    dgamma[j][i] = fma2(v[i], w[i], dgamma[j][i]);
+                    dbeta[j][i] = dbeta[j][i] + v[i];
+                    v[i] = v[i] * gamma[j][i];
+                    sg = sg + v[i];
+                    sgn = fma2(v[i], w[i], sgn);
+                    g[r][j][i] = v[i];
+                    n[r][j][i] = w[i];
+                }
+            }
+            both[2 * r] = sum2(sg);
+            both[2 * r + 1] = sum2(sgn);
+        }
+        if constexpr (STRIDED) load(row + step);
+        Raw<OUT, STRIDED> res[EXTRA ? R * NV : 1];          // the residual's gradient, under way during the sums
+        if constexpr (EXTRA) {
+            if (a.dres.data) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int j = 0; j < NV; ++j)
+                        res[r * NV + j].load_at(res0 + (uint64_t)(row + r) * res_row + j * apart * OSIZE, WHOLE || row + r < rows ? left - j * apart : 0);
+            }
+        }
+        statistics(row + step);
+        row_sums<2 * R, WARPS>(both, part[turn] + threadIdx.y * warps, lane, warp, warps, id);
+        turn ^= 1;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const F2 mg = f2(-both[2 * r] * over), mgn = f2(-both[2 * r + 1] * over);
+            if (!WHOLE && row + r >= rows) continue;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                F2 d[PAIRS];
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) d[i] = fma2(n[r][j][i], mgn, g[r][j][i] + mg) * scale[r];
+                if constexpr (EXTRA) {
+                    if (a.dres.data) {
+                        F2 w[PAIRS];
+                        res[r * NV + j].get(w);
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) d[i] = d[i] + w[i];
+                    }
+                }
+                store_at<OSIZE, STRIDED>(dx0 + (uint64_t)(row + r) * dx_row + j * apart * OSIZE, left - j * apart, d);
+                if constexpr (EXTRA) {
+                    if (a.y.data) {
+                        F2 beta[PAIRS];
+                        load_param<STRIDED>(a.p.beta, a.p, c0 + j * apart, a.cols, 0.f, beta);
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) d[i] = fma2(n[r][j][i], gamma[j][i], beta[i]);
+                        store_at<DSIZE, STRIDED>(y0 + (uint64_t)(row + r) * y_row + j * apart * DSIZE, left - j * apart, d);
+                    }
+                }
+            }
+        }
+    };
+    if constexpr (STRIDED) load(row);
+    else {
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) ask(row + i * step, i);
+    }
+    statistics(row);
+    for (; row + R <= rows; row += step) round(std::true_type());
+    if (R > 1 && row < rows) round(std::false_type());
+    if constexpr (!STRIDED) copies_wait<0>();
+
+    if (blockDim.y > 1) {           // rows side by side: add up their sums, in order
+        __syncthreads();            // no copy of any thread is under way any more
+        F2 *sums = reinterpret_cast<F2 *>(shared);     // [blockDim.y - 1][2][NV][PAIRS][blockDim.x]
+        const int each = 2 * NV * PAIRS * blockDim.x;
+        if (threadIdx.y > 0) {
+            F2 *to = sums + (threadIdx.y - 1) * each + threadIdx.x;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    to[(j * PAIRS + i) * blockDim.x] = dgamma[j][i];
+                    to[((NV + j) * PAIRS + i) * blockDim.x] = dbeta[j][i];
+                }
+        }
+        __syncthreads();
+        if (threadIdx.y > 0) return;
+        for (int y = 1; y < (int)blockDim.y; ++y) {
+            const F2 *from = sums + (y - 1) * each + threadIdx.x;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    dgamma[j][i] = dgamma[j][i] + from[(j * PAIRS + i) * blockDim.x];
+                    dbeta[j][i] = dbeta[j][i] + from[((NV + j) * PAIRS + i) * blockDim.x];
+                }
+        }
+    }
+    const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        store_chunk<STRIDED>(to, 0, c0 + j * apart, a.pitch, dgamma[j]);
+        store_chunk<STRIDED>(to, 1, c0 + j * apart, a.pitch, dbeta[j]);
+    }
+}
+
+// Rows of more columns than a thread can hold values of: NV chunks a thread, the sums over rows in registers, dy and x read
+// a second time (from L2) for the result.
+template <int DY, int SRC, bool STRIDED, int NV>
+__global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_again_kernel(NormBackward a)
+{
+    __shared__ float part[2][2 * (BACK_THREADS / 32)];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, apart = warps * SPAN;
+    const float over = 1.f / (float)a.cols;
+    const int c0 = lane_column<STRIDED>(warp * SPAN, lane);
+    F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) { dgamma[j][i] = f2(0.f); dbeta[j][i] = f2(0.f); }
+    Raw<DY, STRIDED> raw_dy[NV];
+    Raw<SRC, STRIDED> raw_x[NV];
+    auto load = [&](long long row) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            raw_dy[j].load(a.dy, a.kept, row, c0 + j * apart, a.cols);
+            raw_x[j].load(a.x, a.kept, row, c0 + j * apart, a.cols);
+        }
+    };
+    int turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        load(row);
+        const F2 less = f2(-__ldg(a.mean + row)), scale = f2(__ldg(a.rstd + row));
+        F2 dy[PAIRS], n[PAIRS], gamma[PAIRS], sg = f2(0.f), sgn = f2(0.f);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            load_param<STRIDED>(a.p.gamma, a.p, c0 + j * apart, a.cols, 0.f, gamma);
+            raw_dy[j].get(dy);
+            raw_x[j].get(n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                n[i] = (n[i] + less) * scale;
+                dgamma[j][i] = fma2(dy[i], n[i], dgamma[j][i]);
+                dbeta[j][i] = dbeta[j][i] + dy[i];
+                dy[i] = dy[i] * gamma[i];
+                sg = sg + dy[i];
+                sgn = fma2(dy[i], n[i], sgn);
+            }
+        }
+        float both[2] = {sum2(sg), sum2(sgn)};
+        row_sums<2, BACK_THREADS / 32>(both, part[turn], lane, warp, warps, 1);
+        const F2 mg = f2(-both[0] * over), mgn = f2(-both[1] * over);
+        load(row);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = c0 + j * apart;
+            load_param<STRIDED>(a.p.gamma, a.p, c, a.cols, 0.f, gamma);
+            raw_dy[j].get(dy);
+            raw_x[j].get(n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                n[i] = (n[i] + less) * scale;
+                dy[i] = fma2(n[i], mgn, fma2(dy[i], gamma[i], mg)) * scale;
+            }
+            if (a.dres.data) add_residual<STRIDED>(a, row, c, dy);
+            store_chunk<STRIDED>(a.dx, row, c, a.cols, dy);
+            if (a.y.data) {
+                F2 beta[PAIRS];
+                load_param<STRIDED>(a.p.beta, a.p, c, a.cols, 0.f, beta);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) n[i] = fma2(n[i], gamma[i], beta[i]);
+                store_chunk<STRIDED>(a.y, row, c, a.cols, n);
+            }
+        }
+    }
+    const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        store_chunk<STRIDED>(to, 0, c0 + j * apart, a.pitch, dgamma[j]);
+        store_chunk<STRIDED>(to, 1, c0 + j * apart, a.pitch, dbeta[j]);
+    }
+}
+
+// Rows beyond the registers of a block: sums over rows in memory, a thread's own columns; dy and x are read twice.
+template <int DY, int SRC, bool STRIDED>
+__global__ void __launch_bounds__(1024) norm_backward_wide_kernel(NormBackward a)
+{
+    __shared__ float part[2][2 * 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int span = warps * SPAN;
+    const float over = 1.f / (float)a.cols;
+    float *out = a.part + (long long)blockIdx.x * 2 * a.pitch;
+    for (int k = threadIdx.x; k < 2 * a.pitch; k += blockDim.x) out[k] = 0.f;
+    __syncthreads();
+    int turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const float mean = __ldg(a.mean + row), rstd = __ldg(a.rstd + row);
+        Raw<DY, STRIDED> raw_dy;
+        Raw<SRC, STRIDED> raw_x;
+        F2 dy[PAIRS], n[PAIRS], gamma[PAIRS], sg = f2(0.f), sgn = f2(0.f);
+        for (int c0 = warp * SPAN; c0 < a.cols; c0 += span) {
+            const int c = lane_column<STRIDED>(c0, lane);
+            raw_dy.load(a.dy, a.kept, row, c, a.cols);
+            raw_x.load(a.x, a.kept, row, c, a.cols);
+            load_param<STRIDED>(a.p.gamma, a.p, c, a.cols, 0.f, gamma);
+            raw_dy.get(dy);
+            raw_x.get(n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) n[i] = (n[i] + f2(-mean)) * f2(rstd);
+#pragma unroll
+            for (int e = 0; e < CHUNK; ++e) {      // this thread's columns alone
+                const int k = chunk_column<STRIDED>(c, e);
+                float d[2], x[2];
+                split(dy[e / 2], d[0], d[1]);
+                split(n[e / 2], x[0], x[1]);
+                if (k < a.cols) { out[k] = fmaf(d[e & 1], x[e & 1], out[k]); out[a.pitch + k] += d[e & 1]; }
+            }
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                dy[i] = dy[i] * gamma[i];
+                sg = sg + dy[i];
+                sgn = fma2(dy[i], n[i], sgn);
+            }
+        }
+        float both[2] = {sum2(sg), sum2(sgn)};
+        row_sums<2, 32>(both, part[turn], lane, warp, warps, 1);
+        const F2 mg = f2(-both[0] * over), mgn = f2(-both[1] * over);
+        for (int c0 = warp * SPAN; c0 < a.cols; c0 += span) {
+            const int c = lane_column<STRIDED>(c0, lane);
+            F2 beta[PAIRS];
+            raw_dy.load(a.dy, a.kept, row, c, a.cols);
+            raw_x.load(a.x, a.kept, row, c, a.cols);
+            load_param<STRIDED>(a.p.gamma, a.p, c, a.cols, 0.f, gamma);
+            raw_dy.get(dy);
+            raw_x.get(n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                n[i] = (n[i] + f2(-mean)) * f2(rstd);
+                dy[i] = fma2(n[i], mgn, fma2(dy[i], gamma[i], mg)) * f2(rstd);
+            }
+            if (a.dres.data) add_residual<STRIDED>(a, row, c, dy);
+            store_chunk<STRIDED>(a.dx, row, c, a.cols, dy);
+            if (a.y.data) {
+                load_param<STRIDED>(a.p.beta, a.p, c, a.cols, 0.f, beta);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) n[i] = fma2(n[i], gamma[i], beta[i]);
+                store_chunk<STRIDED>(a.y, row, c, a.cols, n);
+            }
+        }
+    }
+}
+
+// Sums the blocks' parts in order: 32 columns a block, 32 threads along the parts of each.
+__global__ void __launch_bounds__(1024) norm_param_sum_kernel(const float *__restrict__ part, int parts, int pitch, int cols, float *dgamma, float *dbeta)
+{
+    __shared__ float s[32][33];
+    const int k = blockIdx.x * 32 + threadIdx.x;
+    float v = 0.f;
+    if (k < 2 * pitch)
+        for (int p = threadIdx.y; p < parts; p += 32) v += part[(long long)p * 2 * pitch + k];
+    s[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    v = s[threadIdx.x][threadIdx.y];
+#pragma unroll
+    for (int j = 16; j; j >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, j);
+    const int at = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0) {
+        if (at < cols) { if (dgamma) dgamma[at] = v; }
+        else if (at >= pitch && at < pitch + cols && dbeta) dbeta[at - pitch] = v;
+    }
+}
+
+namespace {
+
+struct Shape { int threads, side, chunks, at_a_time; };   // threads of a row, rows side by side, chunks of a thread (0: wide), R
+
+Shape backward_shape(int cols)
+{
+    const int spans = (cols + SPAN - 1) / SPAN, most = BACK_THREADS / 32;
+    if (spans <= most) return {32 * spans, most / spans, 1, 2};
+    if (spans <= 2 * most) return {32 * ((spans + 1) / 2), 1, 2, 1};
+    if (spans <= 4 * most) return {32 * ((spans + 3) / 4), 1, 4, 1};
+    return {1024, 1, 0, 1};
+}
+
+int backward_grid(int rows, int cols)
+{
+    const Shape s = backward_shape(cols);
+    const long long rounds = ((long long)rows + s.at_a_time - 1) / s.at_a_time;
+    return (int)std::max(1LL, std::min((long long)NORM_SMS, rounds));
+}
+int backward_pitch(int cols) { return (cols + CHUNK - 1) / CHUNK * CHUNK; }
+
+template <int DY, int SRC, int OUT, bool STRIDED, int NV, int R>
+lrbi_status ring_launch(const NormBackward &a, const Shape &sh, int grid, cudaStream_t s)
+{
+    constexpr int bytes = CHUNK * (DY == SRC_F32 ? 4 : 2) + (SRC == SRC_KEPT ? 16 : CHUNK * (SRC == SRC_F32 ? 4 : 2));
+    const size_t ring = STRIDED ? 0 : (size_t)3 * R * NV * bytes * sh.threads * sh.side, sums = (size_t)(sh.side - 1) * 2 * NV * CHUNK * 4 * sh.threads;
+    const dim3 block(sh.threads, sh.side);
+    if (a.dres.data || a.y.data) return norm_launch(norm_backward_kernel<DY, SRC, OUT, STRIDED, true, NV, R>, grid, block, std::max(ring, sums), s, a);
+    return norm_launch(norm_backward_kernel<DY, SRC, OUT, STRIDED, false, NV, R>, grid, block, std::max(ring, sums), s, a);
+}
+
+template <int DY, int SRC, bool STRIDED>
+lrbi_status backward_launch(const NormBackward &a, int grid, cudaStream_t s)
+{
+    const Shape sh = backward_shape(a.cols);
+    const bool f32 = a.dx.dtype == LRBI_Y_F32;
+    if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, 2>(a, sh, grid, s);
+    if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
+    if (sh.chunks == 4) return norm_launch(norm_backward_again_kernel<DY, SRC, STRIDED, 4>, grid, dim3(sh.threads), 0, s, a);
+    return norm_launch(norm_backward_wide_kernel<DY, SRC, STRIDED>, grid, dim3(1024), 0, s, a);
+}
+
+}  // namespace
+
+size_t norm_backward_workspace(int rows, int cols) { return (size_t)backward_grid(std::max(rows, 1), cols) * 2 * backward_pitch(cols) * 4; }
+
+lrbi_status launch_layer_norm_backward(const NormArgs &n, float *workspace, cudaStream_t s)
+{
+    const int pitch = backward_pitch(n.cols), grid = backward_grid(std::max(n.rows, 1), n.cols);
+    const NormBackward a = {{n.dy, n.dy_stride}, {n.x, n.x_stride}, {n.dres, n.dres_stride}, {n.q, n.scale, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)},
+                            make_params(n), n.mean, n.rstd, {n.dx, n.dx_stride, n.dx_dtype}, {n.y, n.y_stride, n.dy_dtype},
+                            n.dx_dtype, workspace, n.rows, n.cols, pitch};
+    const bool strided = n.cols % CHUNK != 0 || !rows16(n.dy, n.dy_stride, n.dy_dtype) || (!n.q && !rows16(n.x, n.x_stride, n.x_dtype)) ||
+                       (n.dres && !rows16(n.dres, n.dres_stride, n.dx_dtype)) || !rows16(n.dx, n.dx_stride, n.dx_dtype) ||
+                       (n.y && !rows16(n.y, n.y_stride, n.dy_dtype));
+    const int src = n.q ? SRC_KEPT : n.x_dtype;
+    lrbi_status st;
+#define BACKWARD(DY, SRC) st = strided ? backward_launch<DY, SRC, true>(a, grid, s) : backward_launch<DY, SRC, false>(a, grid, s)
+    if (n.dy_dtype == LRBI_Y_BF16) {
+        if (src == SRC_BF16) BACKWARD(SRC_BF16, SRC_BF16);
+        else if (src == SRC_F32) BACKWARD(SRC_BF16, SRC_F32);
+        else BACKWARD(SRC_BF16, SRC_KEPT);
+    } else {
+        if (src == SRC_BF16) BACKWARD(SRC_F32, SRC_BF16);
+        else if (src == SRC_F32) BACKWARD(SRC_F32, SRC_F32);
+        else BACKWARD(SRC_F32, SRC_KEPT);
+    }
+#undef BACKWARD
+    if (st != LRBI_OK || (!n.dgamma && !n.dbeta)) return st;
+    norm_param_sum_kernel<<<(2 * pitch + 31) / 32, dim3(32, 32), 0, s>>>(workspace, grid, pitch, n.cols, n.dgamma, n.dbeta);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
+    count_launch();
+    return LRBI_OK;
+}
+
+}  // namespace lrbi

@@ -1,0 +1,378 @@
+// Layer norm over the columns of each row:  y = (x - mean) * rstd * gamma + beta, statistics in fp32, optionally an 8-bit
+// copy of x on the way.
+//
+// Memory is read once and written once: a row's values stay in registers, as they were loaded, between the two sums and the
+// result (the sum of squares is taken about the mean, from registers: no cancellation).  What bounds it then is the number
+// of instructions per value as much as memory, which is why a lane holds as much of a row as it can:
+//
+//   tall  many rows.  A warp has a row, or `warps` of them share one; a lane holds up to 16 chunks (bf16; 8 in fp32), the
+//         sums' shuffles are paid once per row, gamma and beta come from shared memory without bank conflicts, and warps
+//         run apart from one another, so that loads, arithmetic and stores of different rows overlap.
+//   row   few rows (less than two rows a warp for the whole GPU): latency counts, a block has a row, a lane one or two chunks.
+//   wide  rows beyond the registers of a block: read three times, mostly from L2.
+#include <algorithm>
+#include <atomic>
+
+#include "norm_common.cuh"
+
+namespace lrbi {
+
+// How bf16 values are unpacked: by 16 bits and a mask of the upper half.  Each use in a kernel has its own copy, which the
+// compiler takes for another one, and so unpacks the words anew: kept from one use to the next the values would take twice
+// the registers of the words (and were spilled).
+struct Unpack { uint32_t shift, mask; };
+
+struct NormForward {
+    RowsIn x;
+    Params p;
+    RowsOut y;
+    KeptOut kept;          // q null: no copy
+    float *mean, *rstd;    // both or neither
+    float eps;
+    int rows, cols;
+    int warps, each;       // tall: warps that share a row, chunks of each
+    Unpack use[3];
+};
+
+// The chunks of a lane of one row (or of the part of a row that a warp has: columns first .. end), chunk j in the span at
+// first + j * SPAN.
+template <int SRC, bool STRIDED, int K>
+struct Part {
+    static constexpr int SIZE = SRC == SRC_F32 ? 4 : 2, WORDS = Raw<SRC, STRIDED>::WORDS;
+    Raw<SRC, STRIDED> chunk[K];
+
+    // Strided: element by element from memory.  at: the lane's first column; spans that are whole are not checked.
+    __device__ __forceinline__ void load(const char *at, int c, int first, int end)
+    {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            const bool whole = first + (j + 1) * SPAN <= end;
+#pragma unroll
+            for (int e = 0; e < CHUNK; ++e) {
+                const char *p = at + (j * SPAN + 32 * e) * SIZE;
+                uint32_t v = 0;
+                if (whole || c + j * SPAN + 32 * e < end) v = SIZE == 4 ? __ldg(reinterpret_cast<const uint32_t *>(p)) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p));
+                chunk[j].w[e] = v;
+            }
+        }
+    }
+    __device__ __forceinline__ void put(int j, int i, const uint4 &v) { uint32_t *w = chunk[j].w + 4 * i; w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    __device__ __forceinline__ void get(int j, const Unpack &u, F2 (&v)[PAIRS]) const
+    {
+        const uint32_t *w = chunk[j].w;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            if constexpr (SIZE == 4) v[i] = f2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            else if constexpr (STRIDED) v[i] = f2(__uint_as_float(w[2 * i] << u.shift), __uint_as_float(w[2 * i + 1] << u.shift));
+            else v[i] = f2(__uint_as_float(w[i] << u.shift), __uint_as_float(w[i] & u.mask));
+        }
+    }
+};
+
+// Warps of a block, and blocks of an SM: as many registers as K chunks need.
+template <int SRC, bool STRIDED, int K>
+struct Tall {
+    static constexpr int WORDS = K * Raw<SRC, STRIDED>::WORDS;    // registers that hold a row's part
+    static constexpr int WARPS = WORDS >= 64 ? 16 : WORDS >= 32 ? 12 : 16, BLOCKS = WORDS >= 64 ? 1 : 2;
+};
+
+// blockDim = (32, warps of a row, rows of a block).  The next row (whole vectors) is copied to shared memory meanwhile.
+template <int SRC, int OUT, bool STRIDED, int K>
+__global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, STRIDED, K>::BLOCKS) norm_forward_tall_kernel(NormForward a)
+{
+    constexpr int WARPS = Tall<SRC, STRIDED, K>::WARPS, SIZE = SRC == SRC_F32 ? 4 : 2, VECTORS = CHUNK * SIZE / 16;
+    extern __shared__ float4 params[];   // [chunks of a row][gamma, gamma, beta, beta][32]: a lane's 8 columns as 4 vectors
+    __shared__ float part[WARPS][2][WARPS];
+    const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
+    const int first = warp * a.each * SPAN, end = min(first + a.each * SPAN, a.cols), c = lane_column<STRIDED>(first, lane);
+    long long row = (long long)blockIdx.x * blockDim.z + threadIdx.z;
+    const long long step = (long long)gridDim.x * blockDim.z;
+    // then [warps of the block][chunks of a warp][VECTORS][32]: the rows to come
+    uint4 *ahead = reinterpret_cast<uint4 *>(params) + ((a.cols + SPAN - 1) / SPAN * 4 + (threadIdx.z * warps + warp) * a.each * VECTORS) * 32 + lane;
+    auto ask = [&](long long r) {
+        if (r < a.rows) {
+            const char *from = static_cast<const char *>(a.x.data) + (r * a.x.stride + c) * SIZE;
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(ahead);
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (c + j * SPAN < end) {
+#pragma unroll
+                    for (int i = 0; i < VECTORS; ++i) copy_async(to + (j * VECTORS + i) * 512, from + j * SPAN * SIZE + 16 * i, 16);
+                }
+        }
+        copies_asked();
+    };
+    if (!STRIDED) ask(row);
+    for (int q = threadIdx.z * warps + warp; q * SPAN < a.cols; q += warps * blockDim.z) {
+        F2 v[PAIRS];
+        float f[CHUNK];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            load_param<STRIDED>(which ? a.p.beta : a.p.gamma, a.p, lane_column<STRIDED>(q * SPAN, lane), a.cols, which ? 0.f : 1.f, v);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
+            if (STRIDED) {
+#pragma unroll
+                for (int e = 0; e < CHUNK; ++e) reinterpret_cast<float *>(params + (q * 4 + which * 2) * 32)[32 * e + lane] = f[e];
+            } else {
+                params[(q * 4 + which * 2) * 32 + lane] = make_float4(f[0], f[1], f[2], f[3]);
+                params[(q * 4 + which * 2 + 1) * 32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
+            }
+        }
+    }
+    __syncthreads();
+    const float over = 1.f / (float)a.cols;
+    const float4 *own = params + warp * a.each * 4 * 32;
+    for (; row < a.rows; row += step) {
+        Part<SRC, STRIDED, K> x;
+        if constexpr (STRIDED) x.load(static_cast<const char *>(a.x.data) + (row * a.x.stride + c) * SIZE, c, first, end);
+        else {
+            copies_wait<0>();
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+#pragma unroll
+                for (int i = 0; i < VECTORS; ++i) x.put(j, i, c + j * SPAN < end ? ahead[(j * VECTORS + i) * 32] : make_uint4(0, 0, 0, 0));
+        }
+        F2 v[PAIRS], t = f2(0.f);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (STRIDED && first + j * SPAN >= end) break;       // the whole warp
+            x.get(j, a.use[0], v);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) t = t + v[i];
+        }
+        float s[1] = {sum2(t)};       // all of the row is in registers
+        if (!STRIDED) ask(row + step);
+        row_sums<1, WARPS>(s, part[threadIdx.z][0], lane, warp, warps, 1 + threadIdx.z);
+        const float mean = s[0] * over;
+        t = f2(0.f);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (STRIDED && first + j * SPAN >= end) break;
+            x.get(j, a.use[1], v);
+            const F2 less = f2(STRIDED || c + j * SPAN < end ? -mean : 0.f);      // zeros stay zeros past the last column
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) v[i] = v[i] + less;
+            if (STRIDED && first + (j + 1) * SPAN > end) cut<STRIDED>(v, c + j * SPAN, end);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) t = fma2(v[i], v[i], t);
+        }
+        s[0] = sum2(t);
+        row_sums<1, WARPS>(s, part[threadIdx.z][1], lane, warp, warps, 1 + threadIdx.z);
+        const float rstd = inverse_root(fmaf(s[0], over, a.eps));
+        if (a.mean && lane == 0 && warp == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+        constexpr int YSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
+        char *y = static_cast<char *>(a.y.data) + (row * a.y.stride + c) * YSIZE;
+        int8_t *q = a.kept.q + row * a.kept.pitch + c;
+        float *scale = a.kept.scale + row * a.kept.groups + first / KEEP_GROUP;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (first + j * SPAN < end) {
+                x.get(j, a.use[2], v);
+                if (a.kept.q) {
+                    uint32_t tops[STRIDED ? 2 : 1];
+                    x.chunk[j].tops(tops);
+                    keep_chunk<STRIDED>(q + j * SPAN, a.kept.pitch - c - j * SPAN, scale + j * (SPAN / KEEP_GROUP), a.kept.groups - first / KEEP_GROUP - j * (SPAN / KEEP_GROUP), v, tops);
+                }
+                F2 gamma[PAIRS], beta[PAIRS];
+                if constexpr (STRIDED) {
+                    const float *g = reinterpret_cast<const float *>(own + j * 4 * 32) + lane;
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) { gamma[i] = f2(g[64 * i], g[64 * i + 32]); beta[i] = f2(g[256 + 64 * i], g[256 + 64 * i + 32]); }
+                } else {
+                    const float4 *g = own + j * 4 * 32 + lane;
+                    const float4 g0 = g[0], g1 = g[32], b0 = g[64], b1 = g[96];
+                    gamma[0] = f2(g0.x, g0.y); gamma[1] = f2(g0.z, g0.w); gamma[2] = f2(g1.x, g1.y); gamma[3] = f2(g1.z, g1.w);
+                    beta[0] = f2(b0.x, b0.y); beta[1] = f2(b0.z, b0.w); beta[2] = f2(b1.x, b1.y); beta[3] = f2(b1.z, b1.w);
+                }
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[i] = fma2((v[i] + f2(-mean)) * f2(rstd), gamma[i], beta[i]);
+                store_at<YSIZE, STRIDED>(y + j * SPAN * YSIZE, STRIDED && first + (j + 1) * SPAN <= end ? SPAN : end - c - j * SPAN, v);
+            }
+        }
+    }
+    copies_wait<0>();
+}
+
+// blockDim = 32 * warps of a row; one row a block.
+template <int SRC, bool STRIDED, int NV>
+__global__ void __launch_bounds__(1024) norm_forward_row_kernel(NormForward a)
+{
+    __shared__ float part[2][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const long long row = blockIdx.x;
+    const float over = 1.f / (float)a.cols;
+    Raw<SRC, STRIDED> raw[NV];
+    int c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        c[j] = lane_column<STRIDED>((j * warps + warp) * SPAN, lane);
+        raw[j].load(a.x, KeptIn{}, row, c[j], a.cols);
+    }
+    F2 gamma[PAIRS], beta[PAIRS], v[NV][PAIRS], t = f2(0.f);
+    load_param<STRIDED>(a.p.gamma, a.p, c[0], a.cols, 1.f, gamma);
+    load_param<STRIDED>(a.p.beta, a.p, c[0], a.cols, 0.f, beta);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        raw[j].get(v[j]);
+        if (a.kept.q) {
+            uint32_t tops[STRIDED ? 2 : 1];
+            raw[j].tops(tops);
+            keep_chunk<STRIDED>(a.kept, row, (j * warps + warp) * SPAN, lane, v[j], tops);
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) t = t + v[j][i];
+    }
+    float s[1] = {sum2(t)};
+    row_sums<1, 32>(s, part[0], lane, warp, warps, 1);
+    const float mean = s[0] * over;
+    t = f2(0.f);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[j][i] = v[j][i] + f2(-mean);
+        cut<STRIDED>(v[j], c[j], a.cols);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) t = fma2(v[j][i], v[j][i], t);
+    }
+    s[0] = sum2(t);
+    row_sums<1, 32>(s, part[1], lane, warp, warps, 1);
+    const float rstd = inverse_root(fmaf(s[0], over, a.eps));
+    if (a.mean && threadIdx.x == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (j > 0) {
+            load_param<STRIDED>(a.p.gamma, a.p, c[j], a.cols, 1.f, gamma);
+            load_param<STRIDED>(a.p.beta, a.p, c[j], a.cols, 0.f, beta);
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[j][i] = fma2(v[j][i] * f2(rstd), gamma[i], beta[i]);
+        store_chunk<STRIDED>(a.y, row, c[j], a.cols, v[j]);
+    }
+}
+
+template <int SRC, bool STRIDED>
+__global__ void __launch_bounds__(1024) norm_forward_wide_kernel(NormForward a)
+{
+    __shared__ float part[2][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int span = warps * SPAN;
+    const float over = 1.f / (float)a.cols;
+    const long long row = blockIdx.x;
+    Raw<SRC, STRIDED> raw;
+    F2 v[PAIRS], t = f2(0.f);
+    for (int c0 = warp * SPAN; c0 < a.cols; c0 += span) {
+        raw.load(a.x, KeptIn{}, row, lane_column<STRIDED>(c0, lane), a.cols);
+        raw.get(v);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) t = t + v[i];
+    }
+    float s[1] = {sum2(t)};
+    row_sums<1, 32>(s, part[0], lane, warp, warps, 1);
+    const float mean = s[0] * over;
+    t = f2(0.f);
+    for (int c0 = warp * SPAN; c0 < a.cols; c0 += span) {
+        const int c = lane_column<STRIDED>(c0, lane);
+        raw.load(a.x, KeptIn{}, row, c, a.cols);
+        raw.get(v);
+        if (a.kept.q) {
+            uint32_t tops[STRIDED ? 2 : 1];
+            raw.tops(tops);
+            keep_chunk<STRIDED>(a.kept, row, c0, lane, v, tops);
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[i] = v[i] + f2(-mean);
+        cut<STRIDED>(v, c, a.cols);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) t = fma2(v[i], v[i], t);
+    }
+    s[0] = sum2(t);
+    row_sums<1, 32>(s, part[1], lane, warp, warps, 1);
+    const float rstd = inverse_root(fmaf(s[0], over, a.eps));
+    if (a.mean && threadIdx.x == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+    for (int c0 = warp * SPAN; c0 < a.cols; c0 += span) {
+        const int c = lane_column<STRIDED>(c0, lane);
+        F2 gamma[PAIRS], beta[PAIRS];
+        load_param<STRIDED>(a.p.gamma, a.p, c, a.cols, 1.f, gamma);
+        load_param<STRIDED>(a.p.beta, a.p, c, a.cols, 0.f, beta);
+        raw.load(a.x, KeptIn{}, row, c, a.cols);
+        raw.get(v);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[i] = fma2((v[i] + f2(-mean)) * f2(rstd), gamma[i], beta[i]);
+        store_chunk<STRIDED>(a.y, row, c, a.cols, v);
+    }
+}
+
+namespace {
+
+// Blocks of a kernel that an SM takes at once; asked once for each amount of shared memory that comes up.
+template <class Kernel>
+int blocks_per_sm(Kernel kernel, int threads, size_t smem)
+{
+    static std::atomic<uint64_t> known{0};     // threads, shared memory and the answer of the last question
+    const uint64_t key = (uint64_t)threads << 48 | (uint64_t)smem << 8, k = known.load(std::memory_order_relaxed);
+    if ((k & ~255ull) == key && k) return (int)(k & 255);
+    int n = 1;
+    if (smem > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
+    known.store(key | (uint64_t)n, std::memory_order_relaxed);
+    return n;
+}
+
+template <int SRC, int OUT, bool STRIDED, int K>
+lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
+{
+    using T = Tall<SRC, STRIDED, K>;
+    const size_t params = (size_t)((a.cols + SPAN - 1) / SPAN) * 4 * 512;
+    const size_t ahead = STRIDED ? 0 : (size_t)a.warps * a.each * (CHUNK * (SRC == SRC_F32 ? 4 : 2) / 16) * 512;      // of a row
+    int rows = T::WARPS / a.warps;
+    if (!STRIDED) rows = std::min<int>(rows, (int)((MOST_SHARED - params) / ahead));
+    const dim3 block(32, a.warps, std::max(1, rows));
+    const size_t smem = params + ahead * block.z;
+    auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, K>;
+    const long long need = ((long long)a.rows + block.z - 1) / block.z;
+    const int most = NORM_SMS * blocks_per_sm(kernel, 32 * block.y * block.z, smem);
+    return norm_launch(kernel, (int)std::min<long long>(need, most), block, smem, s, a);
+}
+
+template <int SRC, int OUT, bool STRIDED>
+lrbi_status forward_launch(NormForward a, cudaStream_t s)
+{
+    constexpr bool TWO = SRC == SRC_BF16 && !STRIDED;       // two values a register
+    const int spans = (a.cols + SPAN - 1) / SPAN;
+    // Chunks of a lane at most.  8: 24 warps an SM, 16384 x 4096 in 47 us (16 chunks, 16 warps: 49).  Rows beyond 8192 columns
+    // share more of an SM's memory between fewer blocks, and there 16 are better: 4000 x 16384 in 55 us (8: 69).
+    const int most = TWO && spans > 32 ? 16 : 8;
+    a.warps = (spans + most - 1) / most;
+    // Few rows leave most of the GPU idle with a warp each: then a block takes one.
+    const bool few = (long long)a.rows * a.warps < 4 * NORM_SMS;
+    if (spans > 64) return norm_launch(norm_forward_wide_kernel<SRC, STRIDED>, a.rows, dim3(1024), 0, s, a);
+    if (few) {
+        if (spans <= 32) return norm_launch(norm_forward_row_kernel<SRC, STRIDED, 1>, a.rows, dim3(32 * spans), 0, s, a);
+        return norm_launch(norm_forward_row_kernel<SRC, STRIDED, 2>, a.rows, dim3(32 * ((spans + 1) / 2)), 0, s, a);
+    }
+    const int each = a.each = (spans + a.warps - 1) / a.warps;
+    if (each <= 1) return tall_launch<SRC, OUT, STRIDED, 1>(a, s);
+    if (each <= 2) return tall_launch<SRC, OUT, STRIDED, 2>(a, s);
+    if (each <= 4) return tall_launch<SRC, OUT, STRIDED, 4>(a, s);
+    if (each <= 8) return tall_launch<SRC, OUT, STRIDED, 8>(a, s);
+    if constexpr (TWO) return tall_launch<SRC, OUT, STRIDED, 16>(a, s);
+    return LRBI_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+lrbi_status launch_layer_norm(const NormArgs &n, cudaStream_t s)
+{
+    const NormForward a = {{n.x, n.x_stride}, make_params(n), {n.y, n.y_stride, n.y_dtype},
+                           {n.q_out, n.scale_out, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)}, n.mean_out, n.rstd_out, n.eps, n.rows, n.cols, 1, 1, {{16, 0xFFFF0000u}, {16, 0xFFFF0000u}, {16, 0xFFFF0000u}}};
+    const bool strided = n.cols % CHUNK != 0 || !rows16(n.x, n.x_stride, n.x_dtype) || !rows16(n.y, n.y_stride, n.y_dtype);
+    if (n.x_dtype == LRBI_Y_BF16) {
+        if (n.y_dtype == LRBI_Y_BF16) return strided ? forward_launch<SRC_BF16, LRBI_Y_BF16, true>(a, s) : forward_launch<SRC_BF16, LRBI_Y_BF16, false>(a, s);
+        return strided ? forward_launch<SRC_BF16, LRBI_Y_F32, true>(a, s) : forward_launch<SRC_BF16, LRBI_Y_F32, false>(a, s);
+    }
+    if (n.y_dtype == LRBI_Y_BF16) return strided ? forward_launch<SRC_F32, LRBI_Y_BF16, true>(a, s) : forward_launch<SRC_F32, LRBI_Y_BF16, false>(a, s);
+    return strided ? forward_launch<SRC_F32, LRBI_Y_F32, true>(a, s) : forward_launch<SRC_F32, LRBI_Y_F32, false>(a, s);
+}
+
+}  // namespace lrbi

@@ -1,13 +1,16 @@
-// Row-wise building blocks of the layer norm, the 8-bit copies and the activations: how a warp takes columns of a
-// row, loads and stores them in 16 or 32 bits, and keeps a group of them in 8 bits.
+// Row-wise building blocks of the layer norm, the 8-bit copies and the activations: how lanes take columns of a row,
+// load and store them in 16 or 32 bits, and keep them in 8 bits.
 //
-// A warp takes columns in chunks, in one of two ways:
-//   vector   a lane has 8 neighbouring columns (a chunk is 256 columns).  Needs rows that start on 16-byte boundaries
-//            and a multiple of 8 columns.
-//   strided  a lane has columns lane, lane + 32, lane + 64, lane + 96 (a chunk is 128 columns).  Any alignment; every
-//            access of the warp is still one run of memory.
-// Either way a group of 128 columns (what shares a scale in 8 bits) lies in one warp: 16 neighbouring lanes, or all.
+// A warp takes 256 columns at a time (a span), 8 a lane (a chunk), in one of two ways:
+//   vector    a lane has 8 neighbouring columns: one 16-byte access in bf16, two in fp32.  For rows that start on 16-byte
+//             boundaries and hold a multiple of 8 columns.
+//   strided   a lane has columns lane, lane + 32, ..: any alignment and any width; an access of the warp is 64 or 128
+//             neighbouring bytes.  (Aligned vectors moved into place by shuffles and funnel shifts were built too: 35
+//             instructions a value in the layer norm against 9.)
+// Either way a group of 128 columns (what shares a scale in 8 bits) lies within a span.
 #pragma once
+#include <type_traits>
+
 #include "lrbi_common.cuh"
 
 namespace lrbi {
@@ -17,6 +20,11 @@ constexpr int KEEP_GROUP = LRBI_CHECKPOINT_GROUP;
 constexpr float KEEP_TINY = 0x1p-118f;
 
 enum { SRC_BF16 = LRBI_Y_BF16, SRC_F32 = LRBI_Y_F32, SRC_KEPT = 2 };
+constexpr int CHUNK = 8, SPAN = 32 * CHUNK;   // columns of a lane, of a warp
+
+// First column of a lane in the span that starts at c0, and column e of a chunk that starts at c.
+template <bool STRIDED> __device__ __forceinline__ int lane_column(int c0, int lane) { return STRIDED ? c0 + lane : c0 + lane * CHUNK; }
+template <bool STRIDED> __device__ __forceinline__ constexpr int chunk_column(int c, int e) { return STRIDED ? c + 32 * e : c + e; }
 
 // Rows of a matrix in device memory: element (r, c) is at data[r * stride + c].
 struct RowsIn { const void *data; long long stride; };
@@ -44,154 +52,250 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)   // round to 
     return r;
 }
 
-// How a lane's chunk maps to columns.
-template <bool VEC>
-struct Chunk {
-    static constexpr int E = VEC ? 8 : 4;            // columns of a lane
-    static constexpr int SPAN = VEC ? 256 : 128;     // columns of a warp
-    // first column of this lane in the chunk that starts at column c0
-    static __device__ __forceinline__ int first(int c0, int lane) { return VEC ? c0 + lane * 8 : c0 + lane; }
-    static __device__ __forceinline__ int column(int first, int e) { return VEC ? first + e : first + 32 * e; }
-};
-
-// Raw contents of a lane's chunk, as loaded; unpacked when they are used, so that several loads can be under way.
-template <int SRC, bool VEC>
-struct Raw;
-
-template <bool VEC>
-struct Raw<SRC_BF16, VEC> {
-    uint32_t w[4];
-    __device__ __forceinline__ void load(const RowsIn &x, const KeptIn &, long long row, int c, int cols)
-    {
-        const uint16_t *p = static_cast<const uint16_t *>(x.data) + row * x.stride;
-        if (VEC) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (c < cols) v = ld_once16(p + c);
-            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = c + 32 * e < cols ? (uint32_t)__ldg(p + c + 32 * e) << 16 : 0u;
-        }
-    }
-    __device__ __forceinline__ void get(float (&v)[Chunk<VEC>::E]) const
-    {
-        if constexpr (VEC) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(w[i]); v[2 * i + 1] = bf16_hi(w[i]); }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
-        }
-    }
-};
-
-template <bool VEC>
-struct Raw<SRC_F32, VEC> {
-    float w[Chunk<VEC>::E];
-    __device__ __forceinline__ void load(const RowsIn &x, const KeptIn &, long long row, int c, int cols)
-    {
-        const float *p = static_cast<const float *>(x.data) + row * x.stride;
-        if constexpr (VEC) {
-            uint4 a = make_uint4(0, 0, 0, 0), b = a;
-            if (c < cols) { a = ld_once16(p + c); b = ld_once16(p + c + 4); }
-            w[0] = __uint_as_float(a.x); w[1] = __uint_as_float(a.y); w[2] = __uint_as_float(a.z); w[3] = __uint_as_float(a.w);
-            w[4] = __uint_as_float(b.x); w[5] = __uint_as_float(b.y); w[6] = __uint_as_float(b.z); w[7] = __uint_as_float(b.w);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = c + 32 * e < cols ? __ldg(p + c + 32 * e) : 0.f;
-        }
-    }
-    __device__ __forceinline__ void get(float (&v)[Chunk<VEC>::E]) const
-    {
-#pragma unroll
-        for (int e = 0; e < Chunk<VEC>::E; ++e) v[e] = w[e];
-    }
-};
-
-// The 8-bit copy stands for q * scale; rows of q start on 16-byte boundaries and end in zeros.
-template <bool VEC>
-struct Raw<SRC_KEPT, VEC> {
-    uint32_t w[VEC ? 2 : 1];
-    float scale;
-    __device__ __forceinline__ void load(const RowsIn &, const KeptIn &k, long long row, int c, int cols)
-    {
-        const int8_t *p = k.q + row * k.pitch;
-        w[0] = 0; scale = 0.f;
-        if constexpr (VEC) {
-            w[1] = 0;
-            if (c < cols) { const uint2 v = ld_once8(p + c); w[0] = v.x; w[1] = v.y; }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) if (c + 32 * e < cols) w[0] |= (uint32_t)(uint8_t)__ldg(p + c + 32 * e) << (8 * e);
-        }
-        if (c / KEEP_GROUP < k.groups) scale = __ldg(k.scale + row * k.groups + c / KEEP_GROUP);
-    }
-    __device__ __forceinline__ void get(float (&v)[Chunk<VEC>::E]) const
-    {
-#pragma unroll
-        for (int e = 0; e < Chunk<VEC>::E; ++e) v[e] = (float)(int8_t)(w[VEC ? e / 4 : 0] >> (8 * (e & 3))) * scale;
-    }
-};
-
-// Stores a lane's chunk, rounding once (to nearest even) to the output's type.
-template <bool VEC>
-__device__ __forceinline__ void store_chunk(const RowsOut &y, long long row, int c, int cols, const float (&v)[Chunk<VEC>::E])
+// Two fp32 values that go through the pipeline together: each operation is the IEEE one on both halves, at half the issue
+// slots.  The kernels here stream at rates where arithmetic and memory take about the same time.
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float a, float b)
 {
-    if (y.dtype == LRBI_Y_BF16) {
-        uint16_t *p = static_cast<uint16_t *>(y.data) + row * y.stride;
-        if constexpr (VEC) {
-            if (c < cols)
-                *reinterpret_cast<uint4 *>(p + c) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        } else {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ void split(F2 p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ F2 operator+(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b)
+{
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float sum2(F2 p)
+{
+    float a, b;
+    split(p, a, b);
+    return a + b;
+}
+constexpr int PAIRS = CHUNK / 2;
+
+// Contents of a lane's chunk, as loaded; unpacked when they are used, so that several loads can be under way.  Zeros where
+// there is no column.
+template <int SRC, bool STRIDED>
+struct Raw {
+    static constexpr int SIZE = SRC == SRC_F32 ? 4 : 2, WORDS = STRIDED ? CHUNK : CHUNK * SIZE / 4;
+    uint32_t w[WORDS];
+
+    __device__ __forceinline__ void load(const RowsIn &x, const KeptIn &, long long row, int c, int cols)
+    {
+        load_at(static_cast<const char *>(x.data) + (row * x.stride + c) * SIZE, cols - c);
+    }
+    // p: the place of the chunk's first column; `left` columns are there from that one on.
+    __device__ __forceinline__ void load_at(const char *p, int left)
+    {
+        if constexpr (!STRIDED) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (c + 32 * e < cols) p[c + 32 * e] = (uint16_t)pack_bf16(v[e], 0.f);
-        }
-    } else {
-        float *p = static_cast<float *>(y.data) + row * y.stride;
-        if constexpr (VEC) {
-            if (c < cols) {
-                *reinterpret_cast<float4 *>(p + c) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4 *>(p + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            for (int i = 0; i < WORDS / 4; ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (left > 0) v = ld_once16(p + 16 * i);
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) if (c + 32 * e < cols) p[c + 32 * e] = v[e];
+            for (int e = 0; e < CHUNK; ++e) {
+                w[e] = 0;
+                if (32 * e < left) {
+                    if (SIZE == 4) w[e] = __ldg(reinterpret_cast<const uint32_t *>(p) + 32 * e);
+                    else w[e] = __ldg(reinterpret_cast<const uint16_t *>(p) + 32 * e);
+                }
+            }
         }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void get(F2 (&v)[PAIRS]) const
+    {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            if constexpr (SIZE == 4) v[i] = f2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            else if constexpr (STRIDED) v[i] = f2(__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i + 1] << 16));
+            else v[i] = f2(bf16_lo(w[i]), bf16_hi(w[i]));
+        }
+    }
+    // Largest magnitude as a bit pattern of fp32 (a NaN is above infinity): of the chunk, or of each half of it (its two groups).
+    __device__ __forceinline__ void tops(uint32_t (&top)[STRIDED ? 2 : 1]) const
+    {
+        if constexpr (SIZE == 2 && !STRIDED) {   // both halves of a word at once
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+            top[0] = max(m << 16, m & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int h = 0; h < (STRIDED ? 2 : 1); ++h) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < WORDS / (STRIDED ? 2 : 1); ++i) m = max(m, w[h * WORDS / 2 + i] & (SIZE == 4 ? 0x7FFFFFFFu : 0x7FFFu));
+                top[h] = SIZE == 4 ? m : m << 16;
+            }
+        }
+    }
+};
+
+// The 8-bit copy stands for q * scale; its rows start on 16-byte boundaries, and q is 0 past the last column.
+template <bool STRIDED>
+struct Raw<SRC_KEPT, STRIDED> {
+    uint32_t w[STRIDED ? CHUNK : 2];
+    float scale[STRIDED ? 2 : 1];
+    __device__ __forceinline__ void load(const RowsIn &, const KeptIn &k, long long row, int c, int cols)
+    {
+        clear();
+        if constexpr (!STRIDED) {
+            if (c < cols) {
+                const uint2 v = ld_once8(k.q + row * k.pitch + c);
+                w[0] = v.x;
+                w[1] = v.y;
+                scale[0] = __ldg(k.scale + row * k.groups + c / KEEP_GROUP);
+            }
+        } else {
+            const int8_t *p = k.q + row * k.pitch + c;
+#pragma unroll
+            for (int e = 0; e < CHUNK; ++e) if (c + 32 * e < cols) w[e] = (uint32_t)(int)__ldg(p + 32 * e);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) if (c / KEEP_GROUP + h < k.groups) scale[h] = __ldg(k.scale + row * k.groups + c / KEEP_GROUP + h);
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < (STRIDED ? CHUNK : 2); ++i) w[i] = 0;
+#pragma unroll
+        for (int h = 0; h < (STRIDED ? 2 : 1); ++h) scale[h] = 0.f;
+    }
+    __device__ __forceinline__ void get(F2 (&v)[PAIRS]) const
+    {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            if constexpr (STRIDED) v[i] = f2((float)(int)w[2 * i], (float)(int)w[2 * i + 1]) * f2(scale[i / 2]);
+            else {
+                const uint32_t q = w[i / 2] >> (16 * (i & 1));
+                v[i] = f2((float)(int8_t)q, (float)(int8_t)(q >> 8)) * f2(scale[0]);
+            }
+        }
+    }
+};
+
+// Asynchronous copies into shared memory: later rows are under way without registers to wait for them.
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)   // bytes: 4, 8 or 16
+{
+    if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>   // all but the last LEFT groups are there
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Stores a lane's chunk at p, the place of its first column; `left` columns are there from that one on (none: 0 or less).
+template <int SIZE, bool STRIDED>
+__device__ __forceinline__ void store_at(char *p, int left, const F2 (&v)[PAIRS])
+{
+#pragma unroll
+    for (int i = 0; i < (STRIDED ? PAIRS : 0); ++i) {
+        float lo, hi;
+        split(v[i], lo, hi);
+        if (SIZE == 4) {
+            if (64 * i < left) *(reinterpret_cast<float *>(p) + 64 * i) = lo;
+            if (64 * i + 32 < left) *(reinterpret_cast<float *>(p) + 64 * i + 32) = hi;
+        } else {
+            const uint32_t w = pack_bf16(lo, hi);
+            if (64 * i < left) *(reinterpret_cast<uint16_t *>(p) + 64 * i) = (uint16_t)w;
+            if (64 * i + 32 < left) *(reinterpret_cast<uint16_t *>(p) + 64 * i + 32) = (uint16_t)(w >> 16);
+        }
+    }
+    if (!STRIDED && left > 0) {
+        float f[CHUNK];
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
+        if (SIZE == 4) {
+            *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<float4 *>(p + 16) = make_float4(f[4], f[5], f[6], f[7]);
+        } else
+            *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     }
 }
 
-// Keeps a lane's chunk in 8 bits: q = rint(v * (127 / top)), scale = top / 127, top = max |v| over the group.  The
-// quotients and the product are single IEEE operations, so the bytes are a function of the values alone.  Magnitudes are
-// compared as bit patterns, where a NaN is above infinity and cannot be lost; a group that holds either is kept with the
-// scale NaN.  Columns past the last one hold v = 0 here.  Every lane of the warp calls this.
-template <bool VEC>
-__device__ __forceinline__ void keep_chunk(const KeptOut &k, long long row, int c, const float (&v)[Chunk<VEC>::E])
+// Stores a lane's chunk, rounding once (to nearest even) to the output's type.
+template <bool STRIDED>
+__device__ __forceinline__ void store_chunk(const RowsOut &y, long long row, int c, int cols, const F2 (&v)[PAIRS])
 {
-    constexpr int E = Chunk<VEC>::E;
-    uint32_t top = 0;
+    if (y.dtype == LRBI_Y_BF16) store_at<2, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 2, cols - c, v);
+    else store_at<4, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 4, cols - c, v);
+}
+
+// Keeps a lane's chunk in 8 bits: q = rint(v * (127 / top)), scale = top / 127, top = max |v| over the group.  A half warp
+// has the maximum of a group in the end: vector, its own 16 lanes' group; strided, the first or the second group of the
+// span.  The quotients and the product are single IEEE operations, so the bytes are a function of the values alone.
+// Magnitudes are compared as bit patterns, where a NaN is above infinity and cannot be lost; a group that holds either is
+// kept with the scale NaN.  Columns past the last one hold v = 0 here.  A half warp's first lane divides 127 by top, its
+// second top by 127, at the same time.  Every lane of the warp calls this.
+// to: where the byte of the chunk's first column goes, `left` bytes from there on; scale: the place of the span's first
+// group, `groups` of them from there on.
+template <bool STRIDED>
+__device__ __forceinline__ void keep_chunk(int8_t *to, int left, float *scale, int groups, const F2 (&v)[PAIRS], const uint32_t (&tops)[STRIDED ? 2 : 1])
+{
+    const bool upper = threadIdx.x & 16;
+    uint32_t top = tops[0];
+    if constexpr (STRIDED) top = max(upper ? tops[1] : tops[0], __shfl_xor_sync(0xFFFFFFFFu, upper ? tops[0] : tops[1], 16));
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int j = VEC ? 8 : 16; j; j >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, j));
+    for (int j = 8; j; j >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, j));
     const float t = __uint_as_float(top);
-    const bool fine = top < 0x7F800000u, low = t < KEEP_TINY;
-    const float factor = fine && !low ? __fdiv_rn(127.f, t) : 0.f;
-    const float scale = fine ? (low ? 0.f : __fdiv_rn(t, 127.f)) : __uint_as_float(0x7FC00000u);
-    uint32_t b[E];
-    // adding 1.5 * 2^23 leaves the integer nearest to the product (ties to even) in the low bits
+    const bool fine = top < 0x7F800000u && t >= KEEP_TINY, second = (threadIdx.x & 15) == 1;
+    const float quotient = fine ? __fdiv_rn(second ? t : 127.f, second ? 127.f : t) : top < 0x7F800000u ? 0.f : __uint_as_float(0x7FC00000u);
+    const float own = __shfl_sync(0xFFFFFFFFu, quotient, 0, 16), other = STRIDED ? __shfl_xor_sync(0xFFFFFFFFu, own, 16) : own;
+    const float factors[2] = {STRIDED && upper ? other : own, STRIDED && !upper ? other : own};
+    uint32_t b[CHUNK];
+    // Adding 1.5 * 2^23 leaves the integer nearest to the product (ties to even) in the low bits.  The product is rounded
+    // first: the two operations stay apart as scalar ones (a packed product and a packed sum came out as one fused step).
 #pragma unroll
-    for (int e = 0; e < E; ++e) b[e] = fine ? __float_as_uint(__fadd_rn(__fmul_rn(v[e], factor), 12582912.f)) : 0u;
-    int8_t *p = k.q + row * k.pitch;
-    if constexpr (VEC) {
+    for (int i = 0; i < PAIRS; ++i) {
+        float lo, hi;
+        split(v[i], lo, hi);
+        const float factor = factors[STRIDED ? i / 2 : 0];
+        b[2 * i] = __float_as_uint(__fadd_rn(__fmul_rn(lo, factor), 12582912.f));
+        b[2 * i + 1] = __float_as_uint(__fadd_rn(__fmul_rn(hi, factor), 12582912.f));
+    }
+    if constexpr (STRIDED) {
+#pragma unroll
+        for (int e = 0; e < CHUNK; ++e)
+            if (32 * e < left) to[32 * e] = factors[e / 4] == factors[e / 4] ? (int8_t)b[e] : (int8_t)0;
+    } else {
         uint2 w;
         w.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
         w.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-        if (c < k.pitch) *reinterpret_cast<uint2 *>(p + c) = w;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) if (c + 32 * e < k.pitch) p[c + 32 * e] = (int8_t)b[e];
+        if (!(own == own)) w = make_uint2(0, 0);
+        if (left > 0) *reinterpret_cast<uint2 *>(to) = w;
     }
-    if ((c & (KEEP_GROUP - 1)) == 0 && c / KEEP_GROUP < k.groups) k.scale[row * k.groups + c / KEEP_GROUP] = scale;
+    if (second && (int)upper < groups) scale[upper] = quotient;
+}
+template <bool STRIDED>
+__device__ __forceinline__ void keep_chunk(const KeptOut &k, long long row, int c0, int lane, const F2 (&v)[PAIRS], const uint32_t (&tops)[STRIDED ? 2 : 1], bool on = true)
+{
+    const int c = lane_column<STRIDED>(c0, lane), group = c0 / KEEP_GROUP;
+    keep_chunk<STRIDED>(k.q + row * k.pitch + c, on ? k.pitch - c : 0, k.scale + row * k.groups + group, on ? k.groups - group : 0, v, tops);
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -201,7 +305,7 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// Host side: whether rows can be taken in vectors of 8 columns.
+// Host side: whether rows are whole vectors.
 inline bool rows16(const void *p, long long stride, int dtype)
 {
     const long long bytes = dtype == LRBI_Y_F32 ? 4 : 2;
