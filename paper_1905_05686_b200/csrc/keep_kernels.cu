@@ -75,6 +75,7 @@ constexpr int KEEP_THREADS = 256, KEEP_ROWS = 2;
 template <int SRC, int ACT, bool BACK, int DA, bool STRIDED>
 __global__ void __launch_bounds__(KEEP_THREADS) keep_kernel(KeepArgs k)
 {
+    begin();
     constexpr int WARPS = KEEP_THREADS / 32, U = KEEP_ROWS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int c0 = ((blockIdx.y << k.shift) + (warp & ((1 << k.shift) - 1))) * SPAN, c = lane_column<STRIDED>(c0, lane);
@@ -91,6 +92,7 @@ __global__ void __launch_bounds__(KEEP_THREADS) keep_kernel(KeepArgs k)
             if constexpr (BACK) raw_da[i].load(k.da, k.from, row, c, k.cols);
         }
     }
+    let_next();
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const long long row = row0 + i * down;
@@ -133,12 +135,8 @@ lrbi_status keep_launch(KeepArgs k, bool strided, cudaStream_t s)
     const long long down = (long long)(warps >> k.shift) * KEEP_ROWS;
     const dim3 grid((unsigned)((k.rows + down - 1) / down), (unsigned)((spans + wide - 1) / wide));
     if (grid.y > 65535) return LRBI_ERR_UNSUPPORTED;
-    if (strided) keep_kernel<SRC, ACT, BACK, DA, true><<<grid, KEEP_THREADS, 0, s>>>(k);
-    else keep_kernel<SRC, ACT, BACK, DA, false><<<grid, KEEP_THREADS, 0, s>>>(k);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
-    count_launch(1);
-    return LRBI_OK;
+    if (strided) return launch_kernel(keep_kernel<SRC, ACT, BACK, DA, true>, grid, dim3(KEEP_THREADS), 0, s, 1, k);
+    return launch_kernel(keep_kernel<SRC, ACT, BACK, DA, false>, grid, dim3(KEEP_THREADS), 0, s, 1, k);
 }
 
 template <int SRC, bool BACK, int DA>

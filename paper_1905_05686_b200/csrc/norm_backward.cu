@@ -44,6 +44,7 @@ constexpr int BACK_THREADS = 512;
 template <int DY, int SRC, int OUT, bool STRIDED, bool EXTRA, int NV, int R>
 __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBackward a)
 {
+    begin();
     constexpr int STAGES = 3, WARPS = BACK_THREADS / 32;
     constexpr int DSIZE = DY == SRC_F32 ? 4 : 2, XSIZE = SRC == SRC_F32 ? 4 : SRC == SRC_BF16 ? 2 : 1, OSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
     constexpr int DBYTES = CHUNK * DSIZE, XBYTES = SRC == SRC_KEPT ? 16 : CHUNK * XSIZE;     // of a chunk in the ring
@@ -237,6 +238,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
     }
     statistics(row);
     for (; row + R <= rows; row += step) round(std::true_type());
+    let_next();
     if (R > 1 && row < rows) round(std::false_type());
     if constexpr (!STRIDED) copies_wait<0>();
 
@@ -280,6 +282,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
 template <int DY, int SRC, bool STRIDED, int NV>
 __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_again_kernel(NormBackward a)
 {
+    begin();
     __shared__ float part[2][2 * (BACK_THREADS / 32)];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, apart = warps * SPAN;
     const float over = 1.f / (float)a.cols;
@@ -356,6 +359,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_again_kernel(No
 template <int DY, int SRC, bool STRIDED>
 __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(NormBackward a)
 {
+    begin();
     __shared__ float part[2][2 * 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int span = warps * SPAN;
@@ -424,6 +428,8 @@ __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(NormBackward a
 // Sums the blocks' parts in order: 32 columns a block, 32 threads along the parts of each.
 __global__ void __launch_bounds__(1024) norm_param_sum_kernel(const float *__restrict__ part, int parts, int pitch, int cols, float *dgamma, float *dbeta)
 {
+    begin();
+    let_next();
     __shared__ float s[32][33];
     const int k = blockIdx.x * 32 + threadIdx.x;
     float v = 0.f;
@@ -510,11 +516,7 @@ lrbi_status launch_layer_norm_backward(const NormArgs &n, float *workspace, cuda
     }
 #undef BACKWARD
     if (st != LRBI_OK || (!n.dgamma && !n.dbeta)) return st;
-    norm_param_sum_kernel<<<(2 * pitch + 31) / 32, dim3(32, 32), 0, s>>>(workspace, grid, pitch, n.cols, n.dgamma, n.dbeta);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
-    count_launch();
-    return LRBI_OK;
+    return launch_kernel(norm_param_sum_kernel, dim3((2 * pitch + 31) / 32), dim3(32, 32), 0, s, 1, (const float *)workspace, grid, pitch, n.cols, n.dgamma, n.dbeta);
 }
 
 }  // namespace lrbi

@@ -112,15 +112,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *part, int lane, i
 template <class K, class A>
 lrbi_status norm_launch(K kernel, int grid, dim3 block, size_t smem, cudaStream_t s, const A &a)
 {
-    if (smem > 40 * 1024) {   // what every kernel may have is 48 KB with its static arrays
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
-    }
-    kernel<<<grid, block, smem, s>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
-    count_launch();
-    return LRBI_OK;
+    return launch_kernel(kernel, dim3(grid), block, smem, s, 1, a);
 }
 
 }  // namespace lrbi

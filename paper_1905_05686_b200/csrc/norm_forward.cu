@@ -80,6 +80,7 @@ struct Tall {
 template <int SRC, int OUT, bool STRIDED, int K>
 __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, STRIDED, K>::BLOCKS) norm_forward_tall_kernel(NormForward a)
 {
+    begin();
     constexpr int WARPS = Tall<SRC, STRIDED, K>::WARPS, SIZE = SRC == SRC_F32 ? 4 : 2, VECTORS = CHUNK * SIZE / 16;
     extern __shared__ float4 params[];   // [chunks of a row][gamma, gamma, beta, beta][32]: a lane's 8 columns as 4 vectors
     __shared__ float part[WARPS][2][WARPS];
@@ -124,6 +125,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
     const float over = 1.f / (float)a.cols;
     const float4 *own = params + warp * a.each * 4 * 32;
     for (; row < a.rows; row += step) {
+        if (row + step >= a.rows) let_next();
         Part<SRC, STRIDED, K> x;
         if constexpr (STRIDED) x.load(static_cast<const char *>(a.x.data) + (row * a.x.stride + c) * SIZE, c, first, end);
         else {
@@ -198,6 +200,8 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
 template <int SRC, bool STRIDED, int NV>
 __global__ void __launch_bounds__(1024) norm_forward_row_kernel(NormForward a)
 {
+    begin();
+    let_next();
     __shared__ float part[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const long long row = blockIdx.x;
@@ -254,6 +258,7 @@ __global__ void __launch_bounds__(1024) norm_forward_row_kernel(NormForward a)
 template <int SRC, bool STRIDED>
 __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(NormForward a)
 {
+    begin();
     __shared__ float part[2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int span = warps * SPAN;

@@ -198,6 +198,13 @@ struct Raw<SRC_KEPT, STRIDED> {
     }
 };
 
+// Kernels here are launched so that their blocks may be set up while the kernel before them in the stream drains: every
+// thread calls begin() first, which waits until that kernel is through with memory, and let_next() where the next kernel's
+// blocks may come (early in short kernels, towards the end of long ones: blocks that come while others still run fill the
+// SMs unevenly).  On calls of a few microseconds the gap between two kernels is a good part of the time.
+__device__ __forceinline__ void begin() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Asynchronous copies into shared memory: later rows are under way without registers to wait for them.
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)   // bytes: 4, 8 or 16
 {
@@ -303,6 +310,31 @@ __device__ __forceinline__ float warp_sum(float v)
 #pragma unroll
     for (int j = 16; j; j >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, j);
     return v;
+}
+
+// Host side: launches a kernel that calls begin(), with `smem` bytes of dynamic shared memory and clusters of `cluster` blocks.
+template <class K, class... A>
+lrbi_status launch_kernel(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t s, unsigned cluster, const A &...a)
+{
+    cudaError_t e = cudaSuccess;
+    if (smem > 32 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);   // 48 KB are free, with static arrays
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = block;
+    c.dynamicSmemBytes = smem;
+    c.stream = s;
+    cudaLaunchAttribute attribute[2] = {};
+    attribute[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute[0].val.programmaticStreamSerializationAllowed = 1;
+    attribute[1].id = cudaLaunchAttributeClusterDimension;
+    attribute[1].val.clusterDim.x = cluster;
+    attribute[1].val.clusterDim.y = attribute[1].val.clusterDim.z = 1;
+    c.attrs = attribute;
+    c.numAttrs = cluster > 1 ? 2 : 1;
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&c, kernel, a...);
+    if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
+    count_launch();
+    return LRBI_OK;
 }
 
 // Host side: whether rows are whole vectors.

@@ -7,6 +7,8 @@
 // (w >> 4j) & 0x000F000F with the exponent of 128 set gives the pair (128 + q, 128 + q') in bf16 with a shift and one
 // logic operation, and subtracting (128 + z) gives q - z exactly: weights and activations enter the product unrounded,
 // sums and scales are fp32.
+#include <type_traits>
+
 #include "row_ops.cuh"
 
 namespace lrbi {
@@ -17,17 +19,39 @@ struct W4 {
     int units, groups;     // units of 64 columns, groups of columns, per row
 };
 
-__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b)
+// (128 + nibble j, 128 + nibble j + 4) in bf16, less (z, z): z holds 128 + zero point twice.
+__device__ __forceinline__ uint32_t nibbles(uint32_t word, int j, uint32_t z)
 {
     uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    asm("{\n\t.reg .b32 s, t;\n\tshr.b32 s, %1, %2;\n\tlop3.b32 t, s, %3, %4, 0xEA;\n\tsub.rn.bf16x2 %0, t, %5;\n\t}"     // 0xEA: (a & b) | c
+        : "=r"(r) : "r"(word), "r"(4 * j), "r"(0x000F000Fu), "r"(0x43004300u), "r"(z));
     return r;
 }
 
-__device__ __forceinline__ void mma_m16n8k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_m16n8k16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool first)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if (first)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Two 16-byte loads, 64 bytes apart, where `on`; the registers stay as they are elsewhere.  (As one predicate, not a branch.)
+__device__ __forceinline__ void load_pair(const uint16_t *p, bool on, uint32_t (&x)[8])
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %9, 0;\n\t@q ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%8];\n\t@q ld.global.nc.v4.u32 {%4, %5, %6, %7}, [%8+64];\n\t}"
+                 : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]), "+r"(x[4]), "+r"(x[5]), "+r"(x[6]), "+r"(x[7]) : "l"(p), "r"((uint32_t)on));
+}
+__device__ __forceinline__ void copy_async16(uint32_t to, const void *from, bool on)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(to), "l"(from), "r"((uint32_t)on) : "memory");
+}
+__device__ __forceinline__ void copy_async32(uint32_t to, const void *from, bool on)     // and 512 bytes on
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q cp.async.cg.shared.global [%0], [%1], 16;\n\t@q cp.async.cg.shared.global [%0+512], [%1+512], 16;\n\t}"
+                 ::"r"(to), "l"(from), "r"((uint32_t)on) : "memory");
 }
 
 // Activations of a batch row that a lane needs for a unit: columns c .. c + 7 and c + 32 .. c + 39 (zeros past the last
@@ -53,91 +77,214 @@ __device__ __forceinline__ void load_x16(const uint16_t *X, int batch, int cols,
     }
 }
 
-constexpr int W4_WARPS = 8;
+constexpr int W4_WARPS = 8, W4_STEP = 128;                       // warps of a block; columns that a warp takes at a time
 
-// A block takes 16 rows; its warps split the columns in steps of 128 and add up in shared memory.  NT: tiles of 8 batch rows.
-template <int GROUP, int NT, bool VEC>
-__global__ void __launch_bounds__(32 * W4_WARPS) w4_gemv_kernel(W4 w, const uint16_t *__restrict__ X, int batch, void *__restrict__ Y, int y_dtype)
+__device__ __forceinline__ uint32_t cluster_rank()
 {
-    __shared__ float4 part[W4_WARPS][NT][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g = lane >> 2, t = lane & 3;
-    const int tile = blockIdx.x, batch0 = blockIdx.y * 8 * NT;
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float cluster_load(const float *mine, uint32_t rank)   // the same place in another block of the cluster
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(mine), there;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void store(const W4 &w, void *Y, int y_dtype, int o, int b, int batch, float v)
+{
+    if (o >= w.rows || b >= batch) return;
+    const long long to = (long long)b * w.rows + o;
+    if (y_dtype == LRBI_Y_F32) static_cast<float *>(Y)[to] = v;
+    else static_cast<uint16_t *>(Y)[to] = (uint16_t)pack_bf16(v, 0.f);
+}
+
+// `sharing` warps of a block (and of each block of a cluster) take TILES * 16 rows: the columns in turn, in steps of 128, and
+// add up in shared memory, block by block and then over the cluster, in a fixed order that depends on the layer alone.  A step's weights come through a ring
+// of asynchronous copies, the activations a step ahead in registers.  NT: tiles of 8 batch rows.
+template <int GROUP, int NT, int TILES, bool VEC>
+__global__ void __launch_bounds__(32 * W4_WARPS, NT == 1 && TILES == 1 ? 4 : 2) w4_gemv_kernel(W4 w, const uint16_t *__restrict__ X, int batch, void *__restrict__ Y, int y_dtype, int sharing)
+{
+    begin();
+    constexpr int PER = W4_STEP / GROUP, IN_UNIT = GROUP >= 64 ? 1 : 64 / GROUP, MMAS = 4 / IN_UNIT;   // groups of a step, of a unit; products of a group in a unit
+    constexpr int DEPTH = TILES == 1 ? 4 : 3;                         // steps under way, with the one that is worked on
+    constexpr int TILE = 1024 + PER * 64, SLOT = TILES * TILE;        // bytes of a step: weights, then scales and zero points, of each tile
+    extern __shared__ __align__(16) char ring[];                      // [W4_WARPS][DEPTH][SLOT]
+    __shared__ float4 part[W4_WARPS][TILES][NT][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int ranks = cluster_size(), rank = cluster_rank(), side = W4_WARPS / sharing;
+    const int all_tiles = (w.rows + 15) / 16, tile0 = blockIdx.x / ranks * side * TILES, tile = tile0 + warp / sharing * TILES;   // of the block, of this warp
+    const bool two = TILES == 1 || tile + 1 < all_tiles;      // the second tile is there
+    const int batch0 = blockIdx.y * 8 * NT, left = batch - batch0;
+    const int steps = tile < all_tiles ? (w.units + 1) / 2 : 0, stride = sharing * ranks, whole = min(steps, w.cols / W4_STEP);      // steps of 128 columns that are all there
     X += (long long)batch0 * w.cols;
-    const int left = batch - batch0;
-    const uint4 *packed = reinterpret_cast<const uint4 *>(w.packed) + (long long)tile * w.units * 32 + lane;
-    const uint32_t *meta = w.meta + (long long)tile * w.groups * 16 + g;
-    float acc[NT][4];
+    int step = rank * sharing + warp % sharing;
+    const char *packed = reinterpret_cast<const char *>(w.packed) + ((long long)tile * w.units * 512 + (long long)step * 1024 + lane * 16);
+    const char *meta = reinterpret_cast<const char *>(w.meta) + ((long long)tile * w.groups * 64 + (long long)step * PER * 64 + lane * 16);
+    const uint16_t *from = X + (long long)g * w.cols + step * W4_STEP + t * 8;
+    char *slots = ring + warp * DEPTH * SLOT;
+    const uint32_t slots_lane = (uint32_t)__cvta_generic_to_shared(slots) + lane * 16;
+    const long long packed_tile = (long long)w.units * 512, meta_tile = (long long)w.groups * 64;
+    int asked = step;
+    // Whole steps go through the ring.
+    auto ask = [&](int at) {
+        const bool on = asked < whole;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+        for (int r = 0; r < TILES; ++r) {
+            const uint32_t to = slots_lane + at * SLOT + r * TILE;
+            copy_async32(to, packed + r * packed_tile, on && (r == 0 || two));
+            copy_async16(to + 1024, meta + r * meta_tile, on && (r == 0 || two) && lane < PER * 4);
+        }
+        copies_asked();
+        asked += stride;
+        packed += stride * 1024;
+        meta += stride * PER * 64;
+    };
+    float acc[TILES][NT][4];
+    uint32_t x[2][NT][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
-    constexpr int PER = GROUP >= 64 ? 1 : 64 / GROUP;     // groups in a unit
-    constexpr int STEPS = 4 / PER;                         // tensor-core steps of a group within a unit
-    for (int u0 = warp * 2; u0 < w.units; u0 += W4_WARPS * 2) {
-        uint4 q[2];
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) q[h] = u0 + h < w.units ? ld_once16(packed + (long long)(u0 + h) * 32) : make_uint4(0, 0, 0, 0);
-        float part_acc[NT][4];
+        for (int i = 0; i < 4 * TILES; ++i) acc[i / 4][n][i & 3] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[0][n][i] = x[1][n][i] = 0;      // rows past the batch stay zero
+    }
+    // Activations of a step: for each half of 64 columns the lane's 8 columns of either 32.
+    auto activations = [&](int s) {
+        if (VEC) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) load_pair(from + (long long)n * 8 * w.cols + h * 64, s < whole && n * 8 + g < left, x[h][n]);
+        } else if (s < whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) load_x16<VEC>(X, left, w.cols, n * 8 + g, s * W4_STEP + h * 64 + t * 8, x[h][n]);
+        }
+        from += stride * W4_STEP;
+    };
+    // The products of a step; all: both of its units and all of its groups are there.
+    auto products = [&](const char *places, auto all) {
+        constexpr bool ALL = decltype(all)::value;
+#pragma unroll
+        for (int r = 0; r < TILES; ++r) {
+        const char *slot = places + r * TILE;
+        const uint32_t *own = reinterpret_cast<const uint32_t *>(slot + 1024) + g;
+        float sum[NT][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int u = u0 + h;
-            if (u >= w.units) break;
-            uint32_t x[NT][8];
+            if (!ALL && step * 2 + h >= w.units) break;
+            const uint4 q = *reinterpret_cast<const uint4 *>(slot + h * 512 + lane * 16);
+            const uint32_t word[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int n = 0; n < NT; ++n) load_x16<VEC>(X, left, w.cols, n * 8 + g, u * 64 + t * 8, x[n]);
-            const uint32_t word[4] = {q[h].x, q[h].y, q[h].z, q[h].w};
-#pragma unroll
-            for (int p = 0; p < PER; ++p) {
-                const int group = min(GROUP == 128 ? u >> 1 : u * PER + p, w.groups - 1);
-                const uint32_t lo = __ldg(meta + group * 16), hi = __ldg(meta + group * 16 + 8);
+            for (int p = 0; p < IN_UNIT; ++p) {
+                const int group = GROUP == 128 ? 0 : h * IN_UNIT + p;
+                const bool there = ALL || step * PER + group < w.groups;
+                const uint32_t lo = there ? own[group * 16] : 0u, hi = there ? own[group * 16 + 8] : 0u;
                 const uint32_t z_lo = ((lo & 15u) | 0x4300u) * 0x10001u, z_hi = ((hi & 15u) | 0x4300u) * 0x10001u;
-                if (GROUP != 128 || h == 0) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) part_acc[n][i] = 0.f;
-                }
-#pragma unroll
-                for (int s = p * STEPS; s < (p + 1) * STEPS; ++s) {
+                for (int m = p * MMAS; m < (p + 1) * MMAS; ++m) {
                     uint32_t a[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) a[j] = sub_bf16x2(((word[s] >> (4 * j)) & 0x000F000Fu) | 0x43004300u, j & 1 ? z_hi : z_lo);
+                    for (int j = 0; j < 4; ++j) a[j] = nibbles(word[m], j, j & 1 ? z_hi : z_lo);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_m16n8k16(part_acc[n], a[0], a[1], a[2], a[3], x[n][2 * s], x[n][2 * s + 1]);
+                    for (int n = 0; n < NT; ++n) mma_m16n8k16(sum[n], a, x[h][n][2 * m], x[h][n][2 * m + 1], m == p * MMAS && (GROUP != 128 || h == 0));
                 }
-                if (GROUP != 128 || h == 1 || u + 1 == w.units) {
+                if (GROUP != 128 || h == 1 || (!ALL && step * 2 + 1 == w.units)) {
                     const float s_lo = bf16_hi(lo), s_hi = bf16_hi(hi);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        acc[n][0] = fmaf(s_lo, part_acc[n][0], acc[n][0]);
-                        acc[n][1] = fmaf(s_lo, part_acc[n][1], acc[n][1]);
-                        acc[n][2] = fmaf(s_hi, part_acc[n][2], acc[n][2]);
-                        acc[n][3] = fmaf(s_hi, part_acc[n][3], acc[n][3]);
+                        acc[r][n][0] = fmaf(s_lo, sum[n][0], acc[r][n][0]);
+                        acc[r][n][1] = fmaf(s_lo, sum[n][1], acc[r][n][1]);
+                        acc[r][n][2] = fmaf(s_hi, sum[n][2], acc[r][n][2]);
+                        acc[r][n][3] = fmaf(s_hi, sum[n][3], acc[r][n][3]);
                     }
                 }
             }
         }
-    }
+        }
+    };
 #pragma unroll
-    for (int n = 0; n < NT; ++n) part[warp][n][lane] = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+    for (int i = 0; i < DEPTH - 1; ++i) ask(i);
+    activations(step);
+    while (step < whole) {
+#pragma unroll
+        for (int at = 0; at < DEPTH; ++at) {
+            if (step >= whole) break;
+            ask((at + DEPTH - 1) % DEPTH);
+            copies_wait<DEPTH - 1>();
+            __syncwarp();                   // scales and zero points were copied by other lanes
+            products(slots + at * SLOT, std::true_type());
+            step += stride;
+            activations(step);
+            __syncwarp();                   // before the place is asked for again
+        }
+    }
+    let_next();
+    copies_wait<0>();
+    if (step < steps) {                     // the last step, where it is not whole: units and groups that are there
+        __syncwarp();
+        const char *p = reinterpret_cast<const char *>(w.packed) + (long long)tile * packed_tile + (long long)step * 1024 + lane * 16;
+        const char *m = reinterpret_cast<const char *>(w.meta) + (long long)tile * meta_tile + (long long)step * PER * 64 + lane * 16;
+#pragma unroll
+        for (int r = 0; r < TILES; ++r) {
+            const bool on = r == 0 || two;
+            copy_async16(slots_lane + r * TILE, p + r * packed_tile, on);
+            copy_async16(slots_lane + r * TILE + 512, p + r * packed_tile + 512, on && step * 2 + 1 < w.units);
+            copy_async16(slots_lane + r * TILE + 1024, m + r * meta_tile, on && lane < PER * 4 && step * PER + lane / 4 < w.groups);
+        }
+        copies_asked();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) load_x16<VEC>(X, left, w.cols, n * 8 + g, step * W4_STEP + h * 64 + t * 8, x[h][n]);
+        copies_wait<0>();
+        __syncwarp();
+        products(slots, std::false_type());
+    }
+    __syncthreads();                        // the ring may be written anew
+#pragma unroll
+    for (int r = 0; r < TILES; ++r)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) part[warp][r][n][lane] = make_float4(acc[r][n][0], acc[r][n][1], acc[r][n][2], acc[r][n][3]);
     __syncthreads();
     // thread -> (batch row, output row): neighbouring threads have neighbouring output rows
     const float *sums = reinterpret_cast<const float *>(part);
-    for (int k = threadIdx.x; k < NT * 128; k += 32 * W4_WARPS) {
-        const int row = k & 15, b = k >> 4, n = b >> 3, in = b & 7;
-        // the sum of (row, column in) is value (row >> 3) * 2 + (in & 1) of lane (row & 7) * 4 + in / 2
-        const int at = n * 128 + ((row & 7) * 4 + (in >> 1)) * 4 + (row >> 3) * 2 + (in & 1);
+    constexpr int ALL = TILES * NT * 128;
+    const int rows = side * TILES * 16, outputs = rows * NT * 8;
+    float *block = reinterpret_cast<float *>(ring);             // the ring is through
+    for (int k = threadIdx.x; k < outputs; k += 32 * W4_WARPS) {
+        // the sum of (row, batch row b) is value (row >> 3) * 2 + (b & 1) of lane (row & 7) * 4 + (b & 7) / 2 of tile b >> 3
+        const int row = k % rows, b = k / rows, in = b & 7, r = row >> 4;
+        const int value = ((r % TILES) * NT + (b >> 3)) * 128 + ((row & 7) * 4 + (in >> 1)) * 4 + (row >> 3 & 1) * 2 + (in & 1);
         float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < W4_WARPS; ++i) v += sums[i * NT * 128 + at];
-        const int o = tile * 16 + row;
-        if (o < w.rows && b < left) {
-            const long long to = (long long)(batch0 + b) * w.rows + o;
-            if (y_dtype == LRBI_Y_F32) static_cast<float *>(Y)[to] = v;
-            else static_cast<uint16_t *>(Y)[to] = (uint16_t)pack_bf16(v, 0.f);
-        }
+        for (int i = 0; i < sharing; ++i) v += sums[(r / TILES * sharing + i) * ALL + value];
+        if (ranks > 1) block[k] = v;
+        else store(w, Y, y_dtype, tile0 * 16 + row, batch0 + b, batch, v);
     }
+    if (ranks == 1) return;
+    cluster_barrier();
+    if (rank == 0)
+        for (int k = threadIdx.x; k < outputs; k += 32 * W4_WARPS) {
+            float v = block[k];
+            for (int r = 1; r < ranks; ++r) v += cluster_load(block + k, r);
+            store(w, Y, y_dtype, tile0 * 16 + k % rows, batch0 + k / rows, batch, v);
+        }
+    cluster_barrier();                      // the other blocks' sums are read before they end
 }
 
 // Quantises a block of 16 rows x 128 columns (bf16) and lays it out.  A group's range is that of its kept weights and
@@ -215,19 +362,39 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(Geo geo, const uint16_
 
 namespace {
 
-template <int GROUP, int NT>
-void gemv_launch(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, bool vec, cudaStream_t s)
+// How a layer is cut: warps of a block that share a tile, and blocks that do.
+struct Cut { int sharing, split; };
+Cut gemv_cut(const W4 &w)
 {
-    const dim3 grid((w.rows + 15) / 16, (batch + 8 * NT - 1) / (8 * NT));
-    if (vec) w4_gemv_kernel<GROUP, NT, true><<<grid, 32 * W4_WARPS, 0, s>>>(w, X, batch, Y, y_dtype);
-    else w4_gemv_kernel<GROUP, NT, false><<<grid, 32 * W4_WARPS, 0, s>>>(w, X, batch, Y, y_dtype);
+    const int tiles = (w.rows + 15) / 16, steps = (w.units + 1) / 2;
+    Cut c = {W4_WARPS, 1};
+    while (c.sharing > 1 && tiles * c.sharing > 4736) c.sharing /= 2;
+    while (c.split < 8 && tiles * c.split < 148 && steps >= 2 * c.split * W4_WARPS) c.split *= 2;
+    return c;
+}
+
+template <int GROUP, int NT, int TILES, bool VEC>
+lrbi_status gemv_launch(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, cudaStream_t s)
+{
+    const Cut cut = gemv_cut(w);
+    const int rows = 16 * TILES * (W4_WARPS / cut.sharing), split = cut.split;      // of a block
+    constexpr size_t smem = (size_t)W4_WARPS * (TILES == 1 ? 4 : 3) * TILES * (1024 + W4_STEP / GROUP * 64);
+    return launch_kernel(w4_gemv_kernel<GROUP, NT, TILES, VEC>, dim3((w.rows + rows - 1) / rows * split, (batch + 8 * NT - 1) / (8 * NT)), dim3(32 * W4_WARPS), smem, s,
+                         split, w, X, batch, Y, y_dtype, cut.sharing);
+}
+
+template <int GROUP, int NT>
+lrbi_status gemv_tiles(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, bool vec, cudaStream_t s)
+{
+    if ((w.rows + 15) / 16 >= 512)
+        return vec ? gemv_launch<GROUP, NT, 2, true>(w, X, batch, Y, y_dtype, s) : gemv_launch<GROUP, NT, 2, false>(w, X, batch, Y, y_dtype, s);
+    return vec ? gemv_launch<GROUP, NT, 1, true>(w, X, batch, Y, y_dtype, s) : gemv_launch<GROUP, NT, 1, false>(w, X, batch, Y, y_dtype, s);
 }
 
 template <int GROUP>
-void gemv_group(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, bool vec, cudaStream_t s)
+lrbi_status gemv_group(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, bool vec, cudaStream_t s)
 {
-    if (batch <= 8) gemv_launch<GROUP, 1>(w, X, batch, Y, y_dtype, vec, s);
-    else gemv_launch<GROUP, 2>(w, X, batch, Y, y_dtype, vec, s);
+    return batch <= 8 ? gemv_tiles<GROUP, 1>(w, X, batch, Y, y_dtype, vec, s) : gemv_tiles<GROUP, 2>(w, X, batch, Y, y_dtype, vec, s);
 }
 
 lrbi_status launched()
@@ -246,10 +413,9 @@ lrbi_status launch_w4_gemv(const uint32_t *packed, const uint32_t *meta, int row
     const W4 w = {packed, meta, rows, cols, (cols + 63) / 64, (cols + group - 1) / group};
     if ((batch + 15) / 16 > 65535) return LRBI_ERR_UNSUPPORTED;
     const bool vec = cols % 8 == 0 && (reinterpret_cast<uintptr_t>(X) & 15u) == 0;
-    if (group == 32) gemv_group<32>(w, X, batch, Y, y_dtype, vec, s);
-    else if (group == 64) gemv_group<64>(w, X, batch, Y, y_dtype, vec, s);
-    else gemv_group<128>(w, X, batch, Y, y_dtype, vec, s);
-    return launched();
+    if (group == 32) return gemv_group<32>(w, X, batch, Y, y_dtype, vec, s);
+    if (group == 64) return gemv_group<64>(w, X, batch, Y, y_dtype, vec, s);
+    return gemv_group<128>(w, X, batch, Y, y_dtype, vec, s);
 }
 
 lrbi_status launch_w4_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int group, uint32_t *packed, uint32_t *meta,
