@@ -332,12 +332,16 @@ lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
     const size_t ahead = STRIDED ? 0 : (size_t)a.warps * a.each * (CHUNK * (SRC == SRC_F32 ? 4 : 2) / 16) * 512;      // of a row
     int rows = T::WARPS / a.warps;
     if (!STRIDED) rows = std::min<int>(rows, (int)((MOST_SHARED - params) / ahead));
-    const dim3 block(32, a.warps, std::max(1, rows));
+    dim3 block(32, a.warps, std::max(1, rows));
     const size_t smem = params + ahead * block.z;
     auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, K>;
+    const long long most = NORM_SMS * blocks_per_sm(kernel, 32 * block.y * block.z, smem);
+    // Rows go in rounds over all blocks: the same number of rounds with the fewest rows a block, so that the last is not
+    // nearly empty (4096 x 4096: 3 rounds of 6 rows a block, the last a third full, XX us; of 5 rows, YY us).
+    const long long rounds = ((long long)a.rows + most * block.z - 1) / (most * block.z);
+    block.z = (unsigned)std::max(1LL, ((long long)a.rows + most * rounds - 1) / (most * rounds));
     const long long need = ((long long)a.rows + block.z - 1) / block.z;
-    const int most = NORM_SMS * blocks_per_sm(kernel, 32 * block.y * block.z, smem);
-    return norm_launch(kernel, (int)std::min<long long>(need, most), block, smem, s, a);
+    return norm_launch(kernel, (int)std::min(need, most), block, params + ahead * block.z, s, a);
 }
 
 template <int SRC, int OUT, bool STRIDED>
