@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(KEEP_THREADS) keep_kernel(KeepArgs k)
 {
     begin();
     constexpr int WARPS = KEEP_THREADS / 32, U = KEEP_ROWS;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = kept_lane();
     const int c0 = ((blockIdx.y << k.shift) + (warp & ((1 << k.shift) - 1))) * SPAN, c = lane_column<STRIDED>(c0, lane);
     if (c0 >= k.cols) return;
     const int down = WARPS >> k.shift;      // rows of a block at a time

@@ -35,26 +35,29 @@ __device__ __forceinline__ void add_residual(const NormBackward &a, long long ro
     for (int i = 0; i < PAIRS; ++i) v[i] = v[i] + r[i];
 }
 
-constexpr int BACK_THREADS = 512;
+// Threads of a block: vector rows 16 warps of up to 128 registers; strided rows 20 of up to 96, without a ring to hide latency.
+constexpr int BACK_THREADS = 512, BACK_THREADS_STRIDED = 640;
 
 // blockDim = (threads of a row, rows side by side).  A thread has NV chunks of R rows at a time and keeps its columns' sums
 // and their gamma in registers.  Vector rows come through a ring of STAGES rounds in shared memory, each thread copying what
 // it reads itself; strided rows are loaded into registers a round ahead.  What is left to bound it is the number of
 // instructions a value: addresses are one multiply-add each, and rounds that are whole check nothing.
 template <int DY, int SRC, int OUT, bool STRIDED, bool EXTRA, int NV, int R>
-__global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBackward a)
+__global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BACK_THREADS, 1) norm_backward_kernel(NormBackward a)
 {
     begin();
-    constexpr int STAGES = 3, WARPS = BACK_THREADS / 32;
+    constexpr bool AHEAD = STRIDED && NV == 1;      // strided rows a round ahead in registers
+    constexpr int STAGES = 3, WARPS = BACK_THREADS_STRIDED / 32;
     constexpr int DSIZE = DY == SRC_F32 ? 4 : 2, XSIZE = SRC == SRC_F32 ? 4 : SRC == SRC_BF16 ? 2 : 1, OSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
-    constexpr int DBYTES = CHUNK * DSIZE, XBYTES = SRC == SRC_KEPT ? 16 : CHUNK * XSIZE;     // of a chunk in the ring
+    constexpr int DBYTES = CHUNK * DSIZE, XBYTES = CHUNK * XSIZE;     // of a chunk in the ring
     extern __shared__ float4 shared[];          // the ring: [STAGES][R][NV][dy, x][threads]
     __shared__ float part[2][2 * R * WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + threadIdx.x, id = 1 + threadIdx.y;
+    const int lane = kept_lane(), warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), warps = blockDim.x >> 5;
+    const int threads = blockDim.x * blockDim.y, me = threadIdx.y * blockDim.x + warp * 32 + lane, id = 1 + threadIdx.y;
     const float over = 1.f / (float)a.cols;
     const int c0 = lane_column<STRIDED>(warp * SPAN, lane), apart = warps * SPAN;
     const int left = a.cols - c0;               // columns from the thread's first one on
+    const int warp_left = a.cols - warp * SPAN;  // from the warp's
     F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS], gamma[NV][PAIRS];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -84,9 +87,8 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
                     const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes, to_x = to + DBYTES * threads;
 #pragma unroll
                     for (int i = 0; i < DBYTES / 16; ++i) copy_async(to + (i * threads + me) * 16, d + 16 * i, 16);
-                    if constexpr (SRC == SRC_KEPT) {
-                        copy_async(to_x + me * 8, x, 8);
-                        copy_async(to_x + threads * 8 + me * 4, a.kept.scale + (uint64_t)(first + r) * (uint32_t)a.kept.groups + (c0 + j * apart) / KEEP_GROUP, 4);
+                    if constexpr (SRC == SRC_KEPT) {       // a vector for two threads; rows of the copy are whole vectors
+                        if ((me & 1) == 0) copy_async(to_x + me * 8, x, 16);
                     } else {
 #pragma unroll
                         for (int i = 0; i < XBYTES / 16; ++i) copy_async(to_x + (i * threads + me) * 16, x + 16 * i, 16);
@@ -94,9 +96,22 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
                 }
         copies_asked();
     };
+    float mean[R], rstd[R], scales[R][NV];      // of the round to come; a vector row's scales of its 8-bit copy
+    auto statistics = [&](uint32_t first) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = rstd[r] = 0.f;
+            if (first + r < rows) { mean[r] = __ldg(a.mean + first + r); rstd[r] = __ldg(a.rstd + first + r); }
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (SRC == SRC_KEPT && !STRIDED)
+                    scales[r][j] = first + r < rows && j * apart < left ? __ldg(a.kept.scale + (uint64_t)(first + r) * (uint32_t)a.kept.groups + (c0 + j * apart) / KEEP_GROUP) : 0.f;
+        }
+    };
     Raw<DY, STRIDED> raw_dy[R][NV];
     Raw<SRC, STRIDED> raw_x[R][NV];
     auto take = [&](int at) {
+        if (SRC == SRC_KEPT) __syncwarp();
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -115,7 +130,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
                         const uint2 v = *reinterpret_cast<const uint2 *>(from_x + me * 8);
                         raw_x[r][j].w[0] = v.x;
                         raw_x[r][j].w[1] = v.y;
-                        raw_x[r][j].scale[0] = *reinterpret_cast<const float *>(from_x + threads * 8 + me * 4);
+                        raw_x[r][j].scale[0] = scales[r][j];
                     } else {
 #pragma unroll
                         for (int i = 0; i < XBYTES / 16; ++i) {
@@ -133,18 +148,11 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int there = first + r < rows ? left - j * apart : 0;
-                raw_dy[r][j].load_at(dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, there);
+                const bool whole = first + r < rows && warp_left - j * apart >= SPAN;
+                raw_dy[r][j].load_at(dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, there, whole);
                 if constexpr (SRC == SRC_KEPT) raw_x[r][j].load(a.x, a.kept, first + r, c0 + j * apart, first + r < rows ? a.cols : 0);
-                else raw_x[r][j].load_at(x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE, there);
+                else raw_x[r][j].load_at(x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE, there, whole);
             }
-    };
-    float mean[R], rstd[R];                     // of the round to come
-    auto statistics = [&](uint32_t first) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            mean[r] = rstd[r] = 0.f;
-            if (first + r < rows) { mean[r] = __ldg(a.mean + first + r); rstd[r] = __ldg(a.rstd + first + r); }
-        }
     };
     int at = 0, turn = 0;
     // One round; `whole`: all R rows are there.
@@ -155,7 +163,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
             copies_wait<STAGES - 1>();
             take(at);
             at = at + 1 == STAGES ? 0 : at + 1;
-        }
+        } else if (!AHEAD) load(row);
         F2 g[R][NV][PAIRS], n[R][NV][PAIRS], scale[R];      // dy * gamma, and the normalised input
         float both[2 * R];
 #pragma unroll
@@ -187,9 +195,9 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
             both[2 * r] = sum2(sg);
             both[2 * r + 1] = sum2(sgn);
         }
-        if constexpr (STRIDED) load(row + step);
-        Raw<OUT, STRIDED> res[EXTRA ? R * NV : 1];          // the residual's gradient, under way during the sums
-        if constexpr (EXTRA) {
+        if constexpr (AHEAD) load(row + step);
+        Raw<OUT, STRIDED> res[EXTRA && !STRIDED ? R * NV : 1];          // the residual's gradient, under way during the sums
+        if constexpr (EXTRA && !STRIDED) {
             if (a.dres.data) {
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -198,7 +206,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
                         res[r * NV + j].load_at(res0 + (uint64_t)(row + r) * res_row + j * apart * OSIZE, WHOLE || row + r < rows ? left - j * apart : 0);
             }
         }
-        statistics(row + step);
+        statistics(row + step);                 // after a round's values are taken, within which scales are used
         row_sums<2 * R, WARPS>(both, part[turn] + threadIdx.y * warps, lane, warp, warps, id);
         turn ^= 1;
 #pragma unroll
@@ -213,26 +221,27 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_kernel(NormBack
                 if constexpr (EXTRA) {
                     if (a.dres.data) {
                         F2 w[PAIRS];
-                        res[r * NV + j].get(w);
+                        if (STRIDED) res[0].load_at(res0 + (uint64_t)(row + r) * res_row + j * apart * OSIZE, left - j * apart, warp_left - j * apart >= SPAN);
+                        res[STRIDED ? 0 : r * NV + j].get(w);
 #pragma unroll
                         for (int i = 0; i < PAIRS; ++i) d[i] = d[i] + w[i];
                     }
                 }
-                store_at<OSIZE, STRIDED>(dx0 + (uint64_t)(row + r) * dx_row + j * apart * OSIZE, left - j * apart, d);
+                store_at<OSIZE, STRIDED>(dx0 + (uint64_t)(row + r) * dx_row + j * apart * OSIZE, left - j * apart, d, warp_left - j * apart >= SPAN);
                 if constexpr (EXTRA) {
                     if (a.y.data) {
                         F2 beta[PAIRS];
                         load_param<STRIDED>(a.p.beta, a.p, c0 + j * apart, a.cols, 0.f, beta);
 #pragma unroll
                         for (int i = 0; i < PAIRS; ++i) d[i] = fma2(n[r][j][i], gamma[j][i], beta[i]);
-                        store_at<DSIZE, STRIDED>(y0 + (uint64_t)(row + r) * y_row + j * apart * DSIZE, left - j * apart, d);
+                        store_at<DSIZE, STRIDED>(y0 + (uint64_t)(row + r) * y_row + j * apart * DSIZE, left - j * apart, d, warp_left - j * apart >= SPAN);
                     }
                 }
             }
         }
     };
-    if constexpr (STRIDED) load(row);
-    else {
+    if constexpr (AHEAD) load(row);
+    if constexpr (!STRIDED) {
 #pragma unroll
         for (int i = 0; i < STAGES - 1; ++i) ask(row + i * step, i);
     }
@@ -284,7 +293,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_again_kernel(No
 {
     begin();
     __shared__ float part[2][2 * (BACK_THREADS / 32)];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, apart = warps * SPAN;
+    const int lane = kept_lane(), warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), warps = blockDim.x >> 5, apart = warps * SPAN;
     const float over = 1.f / (float)a.cols;
     const int c0 = lane_column<STRIDED>(warp * SPAN, lane);
     F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS];
@@ -451,18 +460,18 @@ namespace {
 
 struct Shape { int threads, side, chunks, at_a_time; };   // threads of a row, rows side by side, chunks of a thread (0: wide), R
 
-Shape backward_shape(int cols)
+Shape backward_shape(int cols, bool strided)
 {
-    const int spans = (cols + SPAN - 1) / SPAN, most = BACK_THREADS / 32;
+    const int spans = (cols + SPAN - 1) / SPAN, most = BACK_THREADS / 32, most_strided = BACK_THREADS_STRIDED / 32;
+    if (strided && spans <= most_strided) return {32 * spans, most_strided / spans, 1, 1};
     if (spans <= most) return {32 * spans, most / spans, 1, 2};
     if (spans <= 2 * most) return {32 * ((spans + 1) / 2), 1, 2, 1};
     if (spans <= 4 * most) return {32 * ((spans + 3) / 4), 1, 4, 1};
     return {1024, 1, 0, 1};
 }
 
-int backward_grid(int rows, int cols)
+int backward_grid(int rows, const Shape &s)
 {
-    const Shape s = backward_shape(cols);
     const long long rounds = ((long long)rows + s.at_a_time - 1) / s.at_a_time;
     return (int)std::max(1LL, std::min((long long)NORM_SMS, rounds));
 }
@@ -471,7 +480,7 @@ int backward_pitch(int cols) { return (cols + CHUNK - 1) / CHUNK * CHUNK; }
 template <int DY, int SRC, int OUT, bool STRIDED, int NV, int R>
 lrbi_status ring_launch(const NormBackward &a, const Shape &sh, int grid, cudaStream_t s)
 {
-    constexpr int bytes = CHUNK * (DY == SRC_F32 ? 4 : 2) + (SRC == SRC_KEPT ? 16 : CHUNK * (SRC == SRC_F32 ? 4 : 2));
+    constexpr int bytes = CHUNK * ((DY == SRC_F32 ? 4 : 2) + (SRC == SRC_KEPT ? 1 : SRC == SRC_F32 ? 4 : 2));
     const size_t ring = STRIDED ? 0 : (size_t)3 * R * NV * bytes * sh.threads * sh.side, sums = (size_t)(sh.side - 1) * 2 * NV * CHUNK * 4 * sh.threads;
     const dim3 block(sh.threads, sh.side);
     if (a.dres.data || a.y.data) return norm_launch(norm_backward_kernel<DY, SRC, OUT, STRIDED, true, NV, R>, grid, block, std::max(ring, sums), s, a);
@@ -479,11 +488,10 @@ lrbi_status ring_launch(const NormBackward &a, const Shape &sh, int grid, cudaSt
 }
 
 template <int DY, int SRC, bool STRIDED>
-lrbi_status backward_launch(const NormBackward &a, int grid, cudaStream_t s)
+lrbi_status backward_launch(const NormBackward &a, const Shape &sh, int grid, cudaStream_t s)
 {
-    const Shape sh = backward_shape(a.cols);
     const bool f32 = a.dx.dtype == LRBI_Y_F32;
-    if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, 2>(a, sh, grid, s);
+    if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s);
     if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
     if (sh.chunks == 4) return norm_launch(norm_backward_again_kernel<DY, SRC, STRIDED, 4>, grid, dim3(sh.threads), 0, s, a);
     return norm_launch(norm_backward_wide_kernel<DY, SRC, STRIDED>, grid, dim3(1024), 0, s, a);
@@ -491,20 +499,24 @@ lrbi_status backward_launch(const NormBackward &a, int grid, cudaStream_t s)
 
 }  // namespace
 
-size_t norm_backward_workspace(int rows, int cols) { return (size_t)backward_grid(std::max(rows, 1), cols) * 2 * backward_pitch(cols) * 4; }
+size_t norm_backward_workspace(int rows, int cols)      // for either way of taking the rows
+{
+    return (size_t)std::max(backward_grid(rows, backward_shape(cols, false)), backward_grid(rows, backward_shape(cols, true))) * 2 * backward_pitch(cols) * 4;
+}
 
 lrbi_status launch_layer_norm_backward(const NormArgs &n, float *workspace, cudaStream_t s)
 {
-    const int pitch = backward_pitch(n.cols), grid = backward_grid(std::max(n.rows, 1), n.cols);
+    const int pitch = backward_pitch(n.cols);
     const NormBackward a = {{n.dy, n.dy_stride}, {n.x, n.x_stride}, {n.dres, n.dres_stride}, {n.q, n.scale, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)},
                             make_params(n), n.mean, n.rstd, {n.dx, n.dx_stride, n.dx_dtype}, {n.y, n.y_stride, n.dy_dtype},
                             n.dx_dtype, workspace, n.rows, n.cols, pitch};
     const bool strided = n.cols % CHUNK != 0 || !rows16(n.dy, n.dy_stride, n.dy_dtype) || (!n.q && !rows16(n.x, n.x_stride, n.x_dtype)) ||
                        (n.dres && !rows16(n.dres, n.dres_stride, n.dx_dtype)) || !rows16(n.dx, n.dx_stride, n.dx_dtype) ||
                        (n.y && !rows16(n.y, n.y_stride, n.dy_dtype));
-    const int src = n.q ? SRC_KEPT : n.x_dtype;
+    const Shape sh = backward_shape(n.cols, strided);
+    const int grid = backward_grid(n.rows, sh), src = n.q ? SRC_KEPT : n.x_dtype;
     lrbi_status st;
-#define BACKWARD(DY, SRC) st = strided ? backward_launch<DY, SRC, true>(a, grid, s) : backward_launch<DY, SRC, false>(a, grid, s)
+#define BACKWARD(DY, SRC) st = strided ? backward_launch<DY, SRC, true>(a, sh, grid, s) : backward_launch<DY, SRC, false>(a, sh, grid, s)
     if (n.dy_dtype == LRBI_Y_BF16) {
         if (src == SRC_BF16) BACKWARD(SRC_BF16, SRC_BF16);
         else if (src == SRC_F32) BACKWARD(SRC_BF16, SRC_F32);

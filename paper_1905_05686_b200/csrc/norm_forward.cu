@@ -38,21 +38,26 @@ struct NormForward {
 // first + j * SPAN.
 template <int SRC, bool STRIDED, int K>
 struct Part {
-    static constexpr int SIZE = SRC == SRC_F32 ? 4 : 2, WORDS = Raw<SRC, STRIDED>::WORDS;
-    Raw<SRC, STRIDED> chunk[K];
+    static constexpr int SIZE = SRC == SRC_F32 ? 4 : 2;
+    Raw<STRIDED ? SRC_F32 : SRC, STRIDED> chunk[K];      // strided: unpacked as they come from shared memory
 
-    // Strided: element by element from memory.  at: the lane's first column; spans that are whole are not checked.
+    // Strided: element by element from shared memory, at: the lane's first column.  Spans that are whole are not checked.
     __device__ __forceinline__ void load(const char *at, int c, int first, int end)
     {
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            const bool whole = first + (j + 1) * SPAN <= end;
+            const char *p = at + j * SPAN * SIZE;
+            if (first + (j + 1) * SPAN <= end) {         // the whole warp
 #pragma unroll
-            for (int e = 0; e < CHUNK; ++e) {
-                const char *p = at + (j * SPAN + 32 * e) * SIZE;
-                uint32_t v = 0;
-                if (whole || c + j * SPAN + 32 * e < end) v = SIZE == 4 ? __ldg(reinterpret_cast<const uint32_t *>(p)) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p));
-                chunk[j].w[e] = v;
+                for (int e = 0; e < CHUNK; ++e) chunk[j].w[e] = SIZE == 4 ? reinterpret_cast<const uint32_t *>(p)[32 * e] : (uint32_t)reinterpret_cast<const uint16_t *>(p)[32 * e] << 16;
+            } else {
+                const int left = end - c - j * SPAN;
+#pragma unroll
+                for (int e = 0; e < CHUNK; ++e) {
+                    uint32_t v = 0;
+                    if (32 * e < left) v = SIZE == 4 ? reinterpret_cast<const uint32_t *>(p)[32 * e] : (uint32_t)reinterpret_cast<const uint16_t *>(p)[32 * e] << 16;
+                    chunk[j].w[e] = v;
+                }
             }
         }
     }
@@ -62,8 +67,7 @@ struct Part {
         const uint32_t *w = chunk[j].w;
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
-            if constexpr (SIZE == 4) v[i] = f2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-            else if constexpr (STRIDED) v[i] = f2(__uint_as_float(w[2 * i] << u.shift), __uint_as_float(w[2 * i + 1] << u.shift));
+            if constexpr (SIZE == 4 || STRIDED) v[i] = f2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
             else v[i] = f2(__uint_as_float(w[i] << u.shift), __uint_as_float(w[i] & u.mask));
         }
     }
@@ -81,29 +85,45 @@ template <int SRC, int OUT, bool STRIDED, int K>
 __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, STRIDED, K>::BLOCKS) norm_forward_tall_kernel(NormForward a)
 {
     begin();
-    constexpr int WARPS = Tall<SRC, STRIDED, K>::WARPS, SIZE = SRC == SRC_F32 ? 4 : 2, VECTORS = CHUNK * SIZE / 16;
+    constexpr int WARPS = Tall<SRC, STRIDED, K>::WARPS, SIZE = SRC == SRC_F32 ? 4 : 2, VECTORS = CHUNK * SIZE / 16;   // of a chunk
     extern __shared__ float4 params[];   // [chunks of a row][gamma, gamma, beta, beta][32]: a lane's 8 columns as 4 vectors
     __shared__ float part[WARPS][2][WARPS];
-    const int lane = threadIdx.x, warp = threadIdx.y, warps = blockDim.y;
+    const int lane = kept_lane(), warp = threadIdx.y, warps = blockDim.y;
     const int first = warp * a.each * SPAN, end = min(first + a.each * SPAN, a.cols), c = lane_column<STRIDED>(first, lane);
     long long row = (long long)blockIdx.x * blockDim.z + threadIdx.z;
     const long long step = (long long)gridDim.x * blockDim.z;
-    // then [warps of the block][chunks of a warp][VECTORS][32]: the rows to come
-    uint4 *ahead = reinterpret_cast<uint4 *>(params) + ((a.cols + SPAN - 1) / SPAN * 4 + (threadIdx.z * warps + warp) * a.each * VECTORS) * 32 + lane;
+    // then a place for each warp's part of the row to come.  Vector: [chunks][VECTORS][32].  Strided: the 16-byte vectors of
+    // memory that lie in the part, at the same distance from a boundary; lanes hold the values before and after them until
+    // the row's turn.
+    const int place = a.each * VECTORS * 512 + (STRIDED ? 16 : 0);
+    char *ahead = reinterpret_cast<char *>(params + (a.cols + SPAN - 1) / SPAN * 4 * 32) + (threadIdx.z * warps + warp) * place;
+    const uint32_t ahead_at = (uint32_t)__cvta_generic_to_shared(ahead);
+    uint32_t edge = 0;
+    int edge_at = -1, move = 0;
     auto ask = [&](long long r) {
-        if (r < a.rows) {
-            const char *from = static_cast<const char *>(a.x.data) + (r * a.x.stride + c) * SIZE;
-            const uint32_t to = (uint32_t)__cvta_generic_to_shared(ahead);
+        if (r < a.rows && first < end) {
+            if constexpr (!STRIDED) {
+                const char *from = static_cast<const char *>(a.x.data) + (r * a.x.stride + c) * SIZE;
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (c + j * SPAN < end) {
+                for (int j = 0; j < K; ++j)
+                    if (c + j * SPAN < end) {
 #pragma unroll
-                    for (int i = 0; i < VECTORS; ++i) copy_async(to + (j * VECTORS + i) * 512, from + j * SPAN * SIZE + 16 * i, 16);
-                }
+                        for (int i = 0; i < VECTORS; ++i) copy_async(ahead_at + ((j * VECTORS + i) * 32 + lane) * 16, from + j * SPAN * SIZE + 16 * i, 16);
+                    }
+            } else {
+                const char *p = static_cast<const char *>(a.x.data) + (r * a.x.stride + first) * SIZE;
+                const int bytes = (end - first) * SIZE, skip = (int)(-reinterpret_cast<intptr_t>(p) & 15), rest = skip + ((bytes - skip) & ~15);
+                move = 16 - skip & 15;
+                for (int i = skip + lane * 16; i + 16 <= bytes; i += 512) copy_async(ahead_at + move + i, p + i, 16);
+                // lanes 0 .. 7: before the first vector; 16 .. 23: after the last (a part without one has only the former)
+                const int e = lane < 16 ? lane * SIZE : (bytes > skip ? rest : skip) + (lane - 16) * SIZE;
+                edge_at = lane < 16 ? (e < skip && e < bytes ? e : -1) : (e < bytes && bytes > skip ? e : -1);
+                if (edge_at >= 0) edge = SIZE == 4 ? __ldg(reinterpret_cast<const uint32_t *>(p + edge_at)) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p + edge_at));
+            }
         }
         copies_asked();
     };
-    if (!STRIDED) ask(row);
+    ask(row);
     for (int q = threadIdx.z * warps + warp; q * SPAN < a.cols; q += warps * blockDim.z) {
         F2 v[PAIRS];
         float f[CHUNK];
@@ -127,13 +147,20 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
     for (; row < a.rows; row += step) {
         if (row + step >= a.rows) let_next();
         Part<SRC, STRIDED, K> x;
-        if constexpr (STRIDED) x.load(static_cast<const char *>(a.x.data) + (row * a.x.stride + c) * SIZE, c, first, end);
-        else {
-            copies_wait<0>();
+        copies_wait<0>();
+        if constexpr (STRIDED) {
+            if (edge_at >= 0) {
+                if (SIZE == 4) *reinterpret_cast<uint32_t *>(ahead + move + edge_at) = edge;
+                else *reinterpret_cast<uint16_t *>(ahead + move + edge_at) = (uint16_t)edge;
+            }
+            __syncwarp();
+            x.load(ahead + move + lane * SIZE, c, first, end);
+        } else {
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
-                for (int i = 0; i < VECTORS; ++i) x.put(j, i, c + j * SPAN < end ? ahead[(j * VECTORS + i) * 32] : make_uint4(0, 0, 0, 0));
+                for (int i = 0; i < VECTORS; ++i)
+                    x.put(j, i, c + j * SPAN < end ? *reinterpret_cast<const uint4 *>(ahead + ((j * VECTORS + i) * 32 + lane) * 16) : make_uint4(0, 0, 0, 0));
         }
         F2 v[PAIRS], t = f2(0.f);
 #pragma unroll
@@ -144,7 +171,8 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             for (int i = 0; i < PAIRS; ++i) t = t + v[i];
         }
         float s[1] = {sum2(t)};       // all of the row is in registers
-        if (!STRIDED) ask(row + step);
+        if (STRIDED) __syncwarp();
+        ask(row + step);
         row_sums<1, WARPS>(s, part[threadIdx.z][0], lane, warp, warps, 1 + threadIdx.z);
         const float mean = s[0] * over;
         t = f2(0.f);
@@ -189,7 +217,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
                 }
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[i] = fma2((v[i] + f2(-mean)) * f2(rstd), gamma[i], beta[i]);
-                store_at<YSIZE, STRIDED>(y + j * SPAN * YSIZE, STRIDED && first + (j + 1) * SPAN <= end ? SPAN : end - c - j * SPAN, v);
+                store_at<YSIZE, STRIDED>(y + j * SPAN * YSIZE, end - c - j * SPAN, v, first + (j + 1) * SPAN <= end);
             }
         }
     }
@@ -329,9 +357,9 @@ lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
 {
     using T = Tall<SRC, STRIDED, K>;
     const size_t params = (size_t)((a.cols + SPAN - 1) / SPAN) * 4 * 512;
-    const size_t ahead = STRIDED ? 0 : (size_t)a.warps * a.each * (CHUNK * (SRC == SRC_F32 ? 4 : 2) / 16) * 512;      // of a row
+    const size_t ahead = (size_t)a.warps * (a.each * (CHUNK * (SRC == SRC_F32 ? 4 : 2) / 16) * 512 + (STRIDED ? 16 : 0));      // of a row
     int rows = T::WARPS / a.warps;
-    if (!STRIDED) rows = std::min<int>(rows, (int)((MOST_SHARED - params) / ahead));
+    rows = std::min<int>(rows, (int)((MOST_SHARED - params) / ahead));
     dim3 block(32, a.warps, std::max(1, rows));
     const size_t smem = params + ahead * block.z;
     auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, K>;

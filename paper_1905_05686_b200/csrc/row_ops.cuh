@@ -96,12 +96,18 @@ struct Raw {
     static constexpr int SIZE = SRC == SRC_F32 ? 4 : 2, WORDS = STRIDED ? CHUNK : CHUNK * SIZE / 4;
     uint32_t w[WORDS];
 
+    static __device__ __forceinline__ uint32_t one(const char *p)     // strided: the value at p
+    {
+        return SIZE == 4 ? __ldg(reinterpret_cast<const uint32_t *>(p)) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p));
+    }
+
     __device__ __forceinline__ void load(const RowsIn &x, const KeptIn &, long long row, int c, int cols)
     {
-        load_at(static_cast<const char *>(x.data) + (row * x.stride + c) * SIZE, cols - c);
+        load_at(static_cast<const char *>(x.data) + (row * x.stride + c) * SIZE, cols - c, STRIDED && (c | 31) + 7 * 32 < cols);
     }
-    // p: the place of the chunk's first column; `left` columns are there from that one on.
-    __device__ __forceinline__ void load_at(const char *p, int left)
+    // p: the place of the chunk's first column; `left` columns are there from that one on.  whole: strided, the warp's whole
+    // span is there (nothing is checked).
+    __device__ __forceinline__ void load_at(const char *p, int left, bool whole = false)
     {
         if constexpr (!STRIDED) {
 #pragma unroll
@@ -111,12 +117,14 @@ struct Raw {
                 w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
             }
         } else {
+            if (whole) {
 #pragma unroll
-            for (int e = 0; e < CHUNK; ++e) {
-                w[e] = 0;
-                if (32 * e < left) {
-                    if (SIZE == 4) w[e] = __ldg(reinterpret_cast<const uint32_t *>(p) + 32 * e);
-                    else w[e] = __ldg(reinterpret_cast<const uint16_t *>(p) + 32 * e);
+                for (int e = 0; e < CHUNK; ++e) w[e] = one(p + 32 * e * SIZE);
+            } else {
+#pragma unroll
+                for (int e = 0; e < CHUNK; ++e) {
+                    w[e] = 0;
+                    if (32 * e < left) w[e] = one(p + 32 * e * SIZE);
                 }
             }
         }
@@ -172,10 +180,18 @@ struct Raw<SRC_KEPT, STRIDED> {
             }
         } else {
             const int8_t *p = k.q + row * k.pitch + c;
+            const float *s = k.scale + row * k.groups + c / KEEP_GROUP;
+            if ((c | 31) + 7 * 32 < cols) {
 #pragma unroll
-            for (int e = 0; e < CHUNK; ++e) if (c + 32 * e < cols) w[e] = (uint32_t)(int)__ldg(p + 32 * e);
+                for (int e = 0; e < CHUNK; ++e) w[e] = (uint32_t)(int)__ldg(p + 32 * e);
+                scale[0] = __ldg(s);
+                scale[1] = __ldg(s + 1);
+            } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) if (c / KEEP_GROUP + h < k.groups) scale[h] = __ldg(k.scale + row * k.groups + c / KEEP_GROUP + h);
+                for (int e = 0; e < CHUNK; ++e) if (c + 32 * e < cols) w[e] = (uint32_t)(int)__ldg(p + 32 * e);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) if ((c | 31) - 31 + h * KEEP_GROUP < cols) scale[h] = __ldg(s + h);
+            }
         }
     }
     __device__ __forceinline__ void clear()
@@ -205,6 +221,10 @@ struct Raw<SRC_KEPT, STRIDED> {
 __device__ __forceinline__ void begin() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// The lane, as a value that stays in a register: out of threadIdx.x the compiler reads it from its special register again and
+// again where registers are short (60 times a row in the layer norm), and spills more for it.
+__device__ __forceinline__ int kept_lane() { return __shfl_sync(0xFFFFFFFFu, threadIdx.x & 31, threadIdx.x & 31); }
+
 // Asynchronous copies into shared memory: later rows are under way without registers to wait for them.
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)   // bytes: 4, 8 or 16
 {
@@ -218,22 +238,28 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 
 // Stores a lane's chunk at p, the place of its first column; `left` columns are there from that one on (none: 0 or less).
 template <int SIZE, bool STRIDED>
-__device__ __forceinline__ void store_at(char *p, int left, const F2 (&v)[PAIRS])
+__device__ __forceinline__ void store_at(char *p, int left, const F2 (&v)[PAIRS], bool whole = false)
 {
+    if constexpr (STRIDED) {
+        auto put = [&](auto all) {
+            constexpr bool ALL = decltype(all)::value;
 #pragma unroll
-    for (int i = 0; i < (STRIDED ? PAIRS : 0); ++i) {
-        float lo, hi;
-        split(v[i], lo, hi);
-        if (SIZE == 4) {
-            if (64 * i < left) *(reinterpret_cast<float *>(p) + 64 * i) = lo;
-            if (64 * i + 32 < left) *(reinterpret_cast<float *>(p) + 64 * i + 32) = hi;
-        } else {
-            const uint32_t w = pack_bf16(lo, hi);
-            if (64 * i < left) *(reinterpret_cast<uint16_t *>(p) + 64 * i) = (uint16_t)w;
-            if (64 * i + 32 < left) *(reinterpret_cast<uint16_t *>(p) + 64 * i + 32) = (uint16_t)(w >> 16);
-        }
-    }
-    if (!STRIDED && left > 0) {
+            for (int i = 0; i < PAIRS; ++i) {
+                float lo, hi;
+                split(v[i], lo, hi);
+                if (SIZE == 4) {
+                    if (ALL || 64 * i < left) *(reinterpret_cast<float *>(p) + 64 * i) = lo;
+                    if (ALL || 64 * i + 32 < left) *(reinterpret_cast<float *>(p) + 64 * i + 32) = hi;
+                } else {
+                    const uint32_t w = pack_bf16(lo, hi);
+                    if (ALL || 64 * i < left) *(reinterpret_cast<uint16_t *>(p) + 64 * i) = (uint16_t)w;
+                    if (ALL || 64 * i + 32 < left) *(reinterpret_cast<uint16_t *>(p) + 64 * i + 32) = (uint16_t)(w >> 16);
+                }
+            }
+        };
+        if (whole) put(std::true_type());
+        else put(std::false_type());
+    } else if (left > 0) {
         float f[CHUNK];
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
@@ -249,8 +275,9 @@ __device__ __forceinline__ void store_at(char *p, int left, const F2 (&v)[PAIRS]
 template <bool STRIDED>
 __device__ __forceinline__ void store_chunk(const RowsOut &y, long long row, int c, int cols, const F2 (&v)[PAIRS])
 {
-    if (y.dtype == LRBI_Y_BF16) store_at<2, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 2, cols - c, v);
-    else store_at<4, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 4, cols - c, v);
+    const bool whole = STRIDED && (c | 31) + 7 * 32 < cols;
+    if (y.dtype == LRBI_Y_BF16) store_at<2, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 2, cols - c, v, whole);
+    else store_at<4, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 4, cols - c, v, whole);
 }
 
 // Keeps a lane's chunk in 8 bits: q = rint(v * (127 / top)), scale = top / 127, top = max |v| over the group.  A half warp
@@ -276,14 +303,13 @@ __device__ __forceinline__ void keep_chunk(int8_t *to, int left, float *scale, i
     const float factors[2] = {STRIDED && upper ? other : own, STRIDED && !upper ? other : own};
     uint32_t b[CHUNK];
     // Adding 1.5 * 2^23 leaves the integer nearest to the product (ties to even) in the low bits.  The product is rounded
-    // first: the two operations stay apart as scalar ones (a packed product and a packed sum came out as one fused step).
+    // first: the sum is a scalar one, since a packed product and a packed sum came out as one fused step.
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) {
         float lo, hi;
-        split(v[i], lo, hi);
-        const float factor = factors[STRIDED ? i / 2 : 0];
-        b[2 * i] = __float_as_uint(__fadd_rn(__fmul_rn(lo, factor), 12582912.f));
-        b[2 * i + 1] = __float_as_uint(__fadd_rn(__fmul_rn(hi, factor), 12582912.f));
+        split(v[i] * f2(factors[STRIDED ? i / 2 : 0]), lo, hi);
+        b[2 * i] = __float_as_uint(__fadd_rn(lo, 12582912.f));
+        b[2 * i + 1] = __float_as_uint(__fadd_rn(hi, 12582912.f));
     }
     if constexpr (STRIDED) {
 #pragma unroll
