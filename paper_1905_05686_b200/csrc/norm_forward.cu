@@ -31,7 +31,7 @@ struct NormForward {
     float eps;
     int rows, cols;
     int warps, each;       // tall: warps that share a row, chunks of each
-    Unpack use[3];
+    Unpack use[4];
 };
 
 // The chunks of a lane of one row (or of the part of a row that a warp has: columns first .. end), chunk j in the span at
@@ -193,17 +193,37 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
         if (a.mean && lane == 0 && warp == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
         constexpr int YSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
         char *y = static_cast<char *>(a.y.data) + (row * a.y.stride + c) * YSIZE;
-        int8_t *q = a.kept.q + row * a.kept.pitch + c;
-        float *scale = a.kept.scale + row * a.kept.groups + first / KEEP_GROUP;
+        if (a.kept.q) {
+            int8_t *q = a.kept.q + row * a.kept.pitch + c;
+            float *scale = a.kept.scale + row * a.kept.groups + first / KEEP_GROUP;
+            using Keeper = Keep<STRIDED>;
+            constexpr int TOGETHER = Keeper::CHUNKS;
+#pragma unroll
+            for (int j0 = 0; j0 < K; j0 += TOGETHER) {
+                if (first + j0 * SPAN >= end) break;
+                uint32_t tops[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < TOGETHER; ++i) {
+                    uint32_t t[STRIDED ? 2 : 1] = {};
+                    if (j0 + i < K) x.chunk[j0 + i < K ? j0 + i : 0].tops(t);
+                    tops[STRIDED ? 2 * i : i] = t[0];
+                    if (STRIDED) tops[STRIDED ? 2 * i + 1 : 0] = t[STRIDED ? 1 : 0];
+                }
+                const Keeper keep(tops, lane);
+#pragma unroll
+                for (int i = 0; i < TOGETHER; ++i)
+                    if (j0 + i < K) {
+                        x.get(j0 + i, a.use[3], v);
+                        keep.bytes(i, q + (j0 + i) * SPAN, (first + (j0 + i) * SPAN < end ? a.kept.pitch : 0) - c - (j0 + i) * SPAN, v);
+                    }
+                const int group = (j0 + Keeper::chunk(lane)) * (SPAN / KEEP_GROUP) + Keeper::group(lane);
+                if (Keeper::stores(lane) && first + group * KEEP_GROUP < end) scale[group] = keep.quotient;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             if (first + j * SPAN < end) {
                 x.get(j, a.use[2], v);
-                if (a.kept.q) {
-                    uint32_t tops[STRIDED ? 2 : 1];
-                    x.chunk[j].tops(tops);
-                    keep_chunk<STRIDED>(q + j * SPAN, a.kept.pitch - c - j * SPAN, scale + j * (SPAN / KEEP_GROUP), a.kept.groups - first / KEEP_GROUP - j * (SPAN / KEEP_GROUP), v, tops);
-                }
                 F2 gamma[PAIRS], beta[PAIRS];
                 if constexpr (STRIDED) {
                     const float *g = reinterpret_cast<const float *>(own + j * 4 * 32) + lane;
@@ -247,11 +267,7 @@ __global__ void __launch_bounds__(1024) norm_forward_row_kernel(NormForward a)
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         raw[j].get(v[j]);
-        if (a.kept.q) {
-            uint32_t tops[STRIDED ? 2 : 1];
-            raw[j].tops(tops);
-            keep_chunk<STRIDED>(a.kept, row, (j * warps + warp) * SPAN, lane, v[j], tops);
-        }
+        if (a.kept.q) keep_chunk(a.kept, row, (j * warps + warp) * SPAN, lane, v[j], raw[j]);
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) t = t + v[j][i];
     }
@@ -308,11 +324,7 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(NormForward a)
         const int c = lane_column<STRIDED>(c0, lane);
         raw.load(a.x, KeptIn{}, row, c, a.cols);
         raw.get(v);
-        if (a.kept.q) {
-            uint32_t tops[STRIDED ? 2 : 1];
-            raw.tops(tops);
-            keep_chunk<STRIDED>(a.kept, row, c0, lane, v, tops);
-        }
+        if (a.kept.q) keep_chunk(a.kept, row, c0, lane, v, raw);
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) v[i] = v[i] + f2(-mean);
         cut<STRIDED>(v, c, a.cols);
@@ -402,7 +414,7 @@ lrbi_status forward_launch(NormForward a, cudaStream_t s)
 lrbi_status launch_layer_norm(const NormArgs &n, cudaStream_t s)
 {
     const NormForward a = {{n.x, n.x_stride}, make_params(n), {n.y, n.y_stride, n.y_dtype},
-                           {n.q_out, n.scale_out, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)}, n.mean_out, n.rstd_out, n.eps, n.rows, n.cols, 1, 1, {{16, 0xFFFF0000u}, {16, 0xFFFF0000u}, {16, 0xFFFF0000u}}};
+                           {n.q_out, n.scale_out, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)}, n.mean_out, n.rstd_out, n.eps, n.rows, n.cols, 1, 1, {{16, 0xFFFF0000u}, {16, 0xFFFF0000u}, {16, 0xFFFF0000u}, {16, 0xFFFF0000u}}};
     const bool strided = n.cols % CHUNK != 0 || !rows16(n.x, n.x_stride, n.x_dtype) || !rows16(n.y, n.y_stride, n.y_dtype);
     if (n.x_dtype == LRBI_Y_BF16) {
         if (n.y_dtype == LRBI_Y_BF16) return strided ? forward_launch<SRC_BF16, LRBI_Y_BF16, true>(a, s) : forward_launch<SRC_BF16, LRBI_Y_BF16, false>(a, s);

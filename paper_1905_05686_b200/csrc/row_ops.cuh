@@ -280,55 +280,76 @@ __device__ __forceinline__ void store_chunk(const RowsOut &y, long long row, int
     else store_at<4, STRIDED>(static_cast<char *>(y.data) + (row * y.stride + c) * 4, cols - c, v, whole);
 }
 
-// Keeps a lane's chunk in 8 bits: q = rint(v * (127 / top)), scale = top / 127, top = max |v| over the group.  A half warp
-// has the maximum of a group in the end: vector, its own 16 lanes' group; strided, the first or the second group of the
-// span.  The quotients and the product are single IEEE operations, so the bytes are a function of the values alone.
-// Magnitudes are compared as bit patterns, where a NaN is above infinity and cannot be lost; a group that holds either is
-// kept with the scale NaN.  Columns past the last one hold v = 0 here.  A half warp's first lane divides 127 by top, its
-// second top by 127, at the same time.  Every lane of the warp calls this.
-// to: where the byte of the chunk's first column goes, `left` bytes from there on; scale: the place of the span's first
-// group, `groups` of them from there on.
+// Keeping chunks in 8 bits: q = rint(v * (127 / top)), scale = top / 127, top = max |v| over the group.  Four groups go
+// together, so that their maxima share shuffles and all their divisions are one: vector, the groups of four chunks in either
+// half warp; strided, the two groups of two chunks over the warp.  The quotients and the product are single IEEE operations,
+// so the bytes are a function of the values alone.  Magnitudes are compared as bit patterns, where a NaN is above infinity
+// and cannot be lost; a group that holds either is kept with the scale NaN.  Columns past the last one hold 0.
 template <bool STRIDED>
-__device__ __forceinline__ void keep_chunk(int8_t *to, int left, float *scale, int groups, const F2 (&v)[PAIRS], const uint32_t (&tops)[STRIDED ? 2 : 1])
-{
-    const bool upper = threadIdx.x & 16;
-    uint32_t top = tops[0];
-    if constexpr (STRIDED) top = max(upper ? tops[1] : tops[0], __shfl_xor_sync(0xFFFFFFFFu, upper ? tops[0] : tops[1], 16));
+struct Keep {
+    static constexpr int L = STRIDED ? 32 : 16, EACH = L / 4, CHUNKS = STRIDED ? 2 : 4;   // lanes of four groups, of one in the end; chunks at a time
+    float quotient;      // even lanes of a group 127 / top, odd ones the scale
+
+    // tops: of the chunks in turn (strided: of each chunk's two groups); by every lane of the warp
+    __device__ __forceinline__ Keep(const uint32_t (&tops)[4], int lane)
+    {
+        const bool up = lane & (L / 2), up2 = lane & (L / 4);
+        const uint32_t a = max(up ? tops[2] : tops[0], __shfl_xor_sync(0xFFFFFFFFu, up ? tops[0] : tops[2], L / 2));
+        const uint32_t b = max(up ? tops[3] : tops[1], __shfl_xor_sync(0xFFFFFFFFu, up ? tops[1] : tops[3], L / 2));
+        uint32_t top = max(up2 ? b : a, __shfl_xor_sync(0xFFFFFFFFu, up2 ? a : b, L / 4));
 #pragma unroll
-    for (int j = 8; j; j >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, j));
-    const float t = __uint_as_float(top);
-    const bool fine = top < 0x7F800000u && t >= KEEP_TINY, second = (threadIdx.x & 15) == 1;
-    const float quotient = fine ? __fdiv_rn(second ? t : 127.f, second ? 127.f : t) : top < 0x7F800000u ? 0.f : __uint_as_float(0x7FC00000u);
-    const float own = __shfl_sync(0xFFFFFFFFu, quotient, 0, 16), other = STRIDED ? __shfl_xor_sync(0xFFFFFFFFu, own, 16) : own;
-    const float factors[2] = {STRIDED && upper ? other : own, STRIDED && !upper ? other : own};
-    uint32_t b[CHUNK];
-    // Adding 1.5 * 2^23 leaves the integer nearest to the product (ties to even) in the low bits.  The product is rounded
-    // first: the sum is a scalar one, since a packed product and a packed sum came out as one fused step.
-#pragma unroll
-    for (int i = 0; i < PAIRS; ++i) {
-        float lo, hi;
-        split(v[i] * f2(factors[STRIDED ? i / 2 : 0]), lo, hi);
-        b[2 * i] = __float_as_uint(__fadd_rn(lo, 12582912.f));
-        b[2 * i + 1] = __float_as_uint(__fadd_rn(hi, 12582912.f));
+        for (int j = EACH / 2; j; j >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, j));
+        const float t = __uint_as_float(top);
+        const bool fine = top < 0x7F800000u && t >= KEEP_TINY, odd = lane & 1;
+        quotient = fine ? __fdiv_rn(odd ? t : 127.f, odd ? 127.f : t) : top < 0x7F800000u ? 0.f : __uint_as_float(0x7FC00000u);
     }
-    if constexpr (STRIDED) {
+    // The scale that this lane stores, if any: of chunk `chunk`, group `group` of the chunk's span.
+    static __device__ __forceinline__ bool stores(int lane) { return lane % EACH == 1; }
+    static __device__ __forceinline__ int chunk(int lane) { return STRIDED ? lane / EACH / 2 : lane % L / EACH; }
+    static __device__ __forceinline__ int group(int lane) { return STRIDED ? lane / EACH & 1 : lane / L; }
+
+    // The bytes of chunk `i`: at `to`, the place of its first column, `left` bytes from there on.
+    __device__ __forceinline__ void bytes(int i, int8_t *to, int left, const F2 (&v)[PAIRS]) const
+    {
+        float factors[2];
+        factors[0] = __shfl_sync(0xFFFFFFFFu, quotient, (STRIDED ? 2 * i : i) * EACH, L);
+        factors[1] = STRIDED ? __shfl_sync(0xFFFFFFFFu, quotient, (2 * i + 1) * EACH, L) : factors[0];
+        uint32_t b[CHUNK];
+        // Adding 1.5 * 2^23 leaves the integer nearest to the product (ties to even) in the low bits.  The product is rounded
+        // first: the sum is a scalar one, since a packed product and a packed sum came out as one fused step.
 #pragma unroll
-        for (int e = 0; e < CHUNK; ++e)
-            if (32 * e < left) to[32 * e] = factors[e / 4] == factors[e / 4] ? (int8_t)b[e] : (int8_t)0;
-    } else {
-        uint2 w;
-        w.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-        w.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-        if (!(own == own)) w = make_uint2(0, 0);
-        if (left > 0) *reinterpret_cast<uint2 *>(to) = w;
+        for (int j = 0; j < PAIRS; ++j) {
+            float lo, hi;
+            split(v[j] * f2(factors[STRIDED ? j / 2 : 0]), lo, hi);
+            b[2 * j] = __float_as_uint(__fadd_rn(lo, 12582912.f));
+            b[2 * j + 1] = __float_as_uint(__fadd_rn(hi, 12582912.f));
+        }
+        if constexpr (STRIDED) {
+#pragma unroll
+            for (int e = 0; e < CHUNK; ++e)
+                if (32 * e < left) to[32 * e] = factors[e / 4] == factors[e / 4] ? (int8_t)b[e] : (int8_t)0;
+        } else {
+            uint2 w;
+            w.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            w.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+            if (!(factors[0] == factors[0])) w = make_uint2(0, 0);
+            if (left > 0) *reinterpret_cast<uint2 *>(to) = w;
+        }
     }
-    if (second && (int)upper < groups) scale[upper] = quotient;
-}
-template <bool STRIDED>
-__device__ __forceinline__ void keep_chunk(const KeptOut &k, long long row, int c0, int lane, const F2 (&v)[PAIRS], const uint32_t (&tops)[STRIDED ? 2 : 1], bool on = true)
+};
+
+// One chunk by itself, in the span at c0.
+template <int SRC, bool STRIDED>
+__device__ __forceinline__ void keep_chunk(const KeptOut &k, long long row, int c0, int lane, const F2 (&v)[PAIRS], const Raw<SRC, STRIDED> &raw)
 {
-    const int c = lane_column<STRIDED>(c0, lane), group = c0 / KEEP_GROUP;
-    keep_chunk<STRIDED>(k.q + row * k.pitch + c, on ? k.pitch - c : 0, k.scale + row * k.groups + group, on ? k.groups - group : 0, v, tops);
+    uint32_t own[STRIDED ? 2 : 1], tops[4] = {0, 0, 0, 0};
+    raw.tops(own);
+    tops[0] = own[0];
+    if (STRIDED) tops[1] = own[STRIDED ? 1 : 0];
+    const Keep<STRIDED> keep(tops, lane);
+    const int c = lane_column<STRIDED>(c0, lane), group = c0 / KEEP_GROUP + Keep<STRIDED>::group(lane);
+    keep.bytes(0, k.q + row * k.pitch + c, k.pitch - c, v);
+    if (Keep<STRIDED>::stores(lane) && Keep<STRIDED>::chunk(lane) == 0 && group < k.groups) k.scale[row * k.groups + group] = keep.quotient;
 }
 
 __device__ __forceinline__ float warp_sum(float v)
