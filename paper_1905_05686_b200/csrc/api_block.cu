@@ -1,5 +1,29 @@
 // C ABI of the operators around the masked layers: argument checks and calls of the launchers.
-#include "lrbi_common.cuh"
+#include <unordered_map>
+
+#include "row_ops.cuh"
+
+namespace lrbi {
+
+cudaError_t allow_shared(const void *kernel, size_t smem)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || dev < 0 || dev >= LRBI_MAX_DEVICES) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
+    std::lock_guard<std::mutex> lock(lib_mutex());
+    static std::unordered_map<const void *, size_t> allowed[LRBI_MAX_DEVICES];
+    try {
+        size_t &most = allowed[dev][kernel];
+        if (most >= smem) return cudaSuccess;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e == cudaSuccess) most = smem;
+    } catch (...) {      // no room to remember it
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    }
+    return e;
+}
+
+}  // namespace lrbi
 
 using namespace lrbi;
 

@@ -81,7 +81,7 @@ struct Tall {
 };
 
 // blockDim = (32, warps of a row, rows of a block).  The next row (whole vectors) is copied to shared memory meanwhile.
-template <int SRC, int OUT, bool STRIDED, int K>
+template <int SRC, int OUT, bool STRIDED, bool COPY, int K>
 __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, STRIDED, K>::BLOCKS) norm_forward_tall_kernel(NormForward a)
 {
     begin();
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
         if (a.mean && lane == 0 && warp == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
         constexpr int YSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
         char *y = static_cast<char *>(a.y.data) + (row * a.y.stride + c) * YSIZE;
-        if (a.kept.q) {
+        if constexpr (COPY) {
             int8_t *q = a.kept.q + row * a.kept.pitch + c;
             float *scale = a.kept.scale + row * a.kept.groups + first / KEEP_GROUP;
             using Keeper = Keep<STRIDED>;
@@ -364,8 +364,8 @@ int blocks_per_sm(Kernel kernel, int threads, size_t smem)
     return n;
 }
 
-template <int SRC, int OUT, bool STRIDED, int K>
-lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
+template <int SRC, int OUT, bool STRIDED, bool COPY, int K>
+lrbi_status tall_kernel_launch(const NormForward &a, cudaStream_t s)
 {
     using T = Tall<SRC, STRIDED, K>;
     const size_t params = (size_t)((a.cols + SPAN - 1) / SPAN) * 4 * 512;
@@ -374,7 +374,7 @@ lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
     rows = std::min<int>(rows, (int)((MOST_SHARED - params) / ahead));
     dim3 block(32, a.warps, std::max(1, rows));
     const size_t smem = params + ahead * block.z;
-    auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, K>;
+    auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, COPY, K>;
     const long long most = NORM_SMS * blocks_per_sm(kernel, 32 * block.y * block.z, smem);
     // Rows go in rounds over all blocks: the same number of rounds with the fewest rows a block, so that the last is not
     // nearly empty (4096 x 4096: 3 rounds of 6 rows a block, the last a third full, XX us; of 5 rows, YY us).
@@ -382,6 +382,12 @@ lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
     block.z = (unsigned)std::max(1LL, ((long long)a.rows + most * rounds - 1) / (most * rounds));
     const long long need = ((long long)a.rows + block.z - 1) / block.z;
     return norm_launch(kernel, (int)std::min(need, most), block, params + ahead * block.z, s, a);
+}
+
+template <int SRC, int OUT, bool STRIDED, int K>
+lrbi_status tall_launch(const NormForward &a, cudaStream_t s)
+{
+    return a.kept.q ? tall_kernel_launch<SRC, OUT, STRIDED, true, K>(a, s) : tall_kernel_launch<SRC, OUT, STRIDED, false, K>(a, s);
 }
 
 template <int SRC, int OUT, bool STRIDED>

@@ -359,12 +359,18 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// Host side: lets a kernel have `smem` bytes of dynamic shared memory on the current device; asked once for what is enough.
+// (The most that was allowed is kept by kernel and device: pointers of kernels are few.)
+cudaError_t allow_shared(const void *kernel, size_t smem);
+template <class... A>
+cudaError_t allow_shared(void (*kernel)(A...), size_t smem) { return allow_shared(reinterpret_cast<const void *>(kernel), smem); }
+
 // Host side: launches a kernel that calls begin(), with `smem` bytes of dynamic shared memory and clusters of `cluster` blocks.
 template <class K, class... A>
 lrbi_status launch_kernel(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t s, unsigned cluster, const A &...a)
 {
     cudaError_t e = cudaSuccess;
-    if (smem > 32 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);   // 48 KB are free, with static arrays
+    if (smem > 32 * 1024) e = allow_shared(kernel, smem);      // 48 KB are free, with static arrays
     cudaLaunchConfig_t c = {};
     c.gridDim = grid;
     c.blockDim = block;

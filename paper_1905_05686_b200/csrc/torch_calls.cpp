@@ -13,6 +13,7 @@
 #include <climits>
 #include <stdexcept>
 #include <string>
+#include <utility>
 
 #include "lrbi.h"
 
@@ -126,6 +127,20 @@ struct Call {
         if (other) t.record_stream(stream.unwrap());
         return t;
     }
+    // Two new arrays out of one allocation, the second on a 16-byte boundary (allocations cost more than the checks of a call).
+    std::pair<at::Tensor, at::Tensor> make_two(at::IntArrayRef a, at::ScalarType a_type, at::IntArrayRef b, at::ScalarType b_type) const
+    {
+        const int64_t a_bytes = c10::multiply_integers(a) * (int64_t)c10::elementSize(a_type), at_b = (a_bytes + 15) / 16 * 16;
+        const at::Tensor all = make({at_b + c10::multiply_integers(b) * (int64_t)c10::elementSize(b_type)}, at::kByte);
+        return {part(all, 0, a, a_type), part(all, at_b / (int64_t)c10::elementSize(b_type), b, b_type)};
+    }
+    static at::Tensor part(const at::Tensor &all, int64_t offset, at::IntArrayRef sizes, at::ScalarType type)
+    {
+        at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(type));
+        t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+        t.unsafeGetTensorImpl()->set_storage_offset(offset);
+        return t;
+    }
     void *handle() const { return stream.stream(); }
 };
 
@@ -168,7 +183,8 @@ struct Copy {
 
 Copy make_copy(const Call &c, int rows, int cols)
 {
-    return {c.make({rows, lrbi_checkpoint_pitch(cols)}, at::kChar), c.make({rows, lrbi_checkpoint_groups(cols)}, at::kFloat)};
+    auto both = c.make_two({rows, lrbi_checkpoint_pitch(cols)}, at::kChar, {rows, lrbi_checkpoint_groups(cols)}, at::kFloat);
+    return {std::move(both.first), std::move(both.second)};
 }
 
 Copy read_copy(PyObject *q, PyObject *scale, const at::Device &device)
@@ -240,7 +256,8 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int keep = PyObject_IsTrue(a[5]);
         if (keep < 0) throw Raised();
         const Call c(x.device, a[6]);
-        at::Tensor y = c.make({x.rows, x.cols}, type), mean = c.make({x.rows}, at::kFloat), rstd = c.make({x.rows}, at::kFloat);
+        at::Tensor y = c.make({x.rows, x.cols}, type);
+        auto [mean, rstd] = c.make_two({x.rows}, at::kFloat, {x.rows}, at::kFloat);
         Copy k;
         if (keep) k = make_copy(c, x.rows, x.cols);
         check(lrbi_layer_norm(x.data, x.dtype, x.stride, x.rows, x.cols, p.gamma, p.beta, p.dtype, (float)eps, y.data_ptr(), type_code(type), x.cols,
@@ -271,7 +288,8 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int restore = PyObject_IsTrue(a[9]);
         if (restore < 0) throw Raised();
         const Call c(dy.device, a[11]);
-        at::Tensor dx = c.make({dy.rows, dy.cols}, type), dgamma = c.make({dy.cols}, at::kFloat), dbeta = c.make({dy.cols}, at::kFloat), y;
+        at::Tensor dx = c.make({dy.rows, dy.cols}, type), y;
+        auto [dgamma, dbeta] = c.make_two({dy.cols}, at::kFloat, {dy.cols}, at::kFloat);
         if (restore) y = c.make({dy.rows, dy.cols}, dy.type);
         const size_t need = lrbi_layer_norm_backward_workspace(dy.rows, dy.cols);
         const at::Tensor work = c.make({(int64_t)need}, at::kByte);
