@@ -286,6 +286,149 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
     }
 }
 
+// Rows of 8193 to 16384 columns in 16 or 8 bits, whole vectors: a thread has four chunks, whose sums over rows take half of
+// its registers; it reads a row's values twice out of the ring in shared memory, where gamma is too.
+// 4000 x 16384 in bf16: 139 us with the values read twice from memory (below), YYY so.
+template <int SRC, int OUT, bool EXTRA>
+__global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(NormBackward a)
+{
+    begin();
+    constexpr int NV = 4, STAGES = 2, OSIZE = OUT == LRBI_Y_F32 ? 4 : 2, XSIZE = SRC == SRC_KEPT ? 1 : 2, XBYTES = CHUNK * XSIZE;
+    extern __shared__ float4 shared[];          // gamma: [NV][2][threads]; the ring: [STAGES][NV][dy, x][threads], scales: [STAGES][NV][threads / 16]
+    __shared__ float part[2][2 * (BACK_THREADS / 32)];
+    const int lane = kept_lane(), warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), warps = blockDim.x >> 5, apart = warps * SPAN;
+    const int threads = blockDim.x, me = warp * 32 + lane, c0 = me * CHUNK, left = a.cols - c0;
+    const float over = 1.f / (float)a.cols;
+    F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS];
+    float4 *gammas = shared + me;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        F2 g[PAIRS];
+        load_param<false>(a.p.gamma, a.p, c0 + j * apart, a.cols, 0.f, g);
+        float f[CHUNK];
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            split(g[i], f[2 * i], f[2 * i + 1]);
+            dgamma[j][i] = f2(0.f);
+            dbeta[j][i] = f2(0.f);
+        }
+        gammas[2 * j * threads] = make_float4(f[0], f[1], f[2], f[3]);      // read by this thread alone
+        gammas[(2 * j + 1) * threads] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    auto gamma = [&](int j, F2 (&g)[PAIRS]) {
+        const float4 lo = gammas[2 * j * threads], hi = gammas[(2 * j + 1) * threads];
+        g[0] = f2(lo.x, lo.y); g[1] = f2(lo.z, lo.w); g[2] = f2(hi.x, hi.y); g[3] = f2(hi.z, hi.w);
+    };
+    const char *dy0 = static_cast<const char *>(a.dy.data) + c0 * 2;
+    const char *x0 = SRC == SRC_KEPT ? reinterpret_cast<const char *>(a.kept.q + c0) : static_cast<const char *>(a.x.data) + c0 * XSIZE;
+    char *dx0 = static_cast<char *>(a.dx.data) + c0 * OSIZE;
+    const uint32_t dy_row = (uint32_t)(a.dy.stride * 2), x_row = SRC == SRC_KEPT ? (uint32_t)a.kept.pitch : (uint32_t)(a.x.stride * XSIZE), dx_row = (uint32_t)(a.dx.stride * OSIZE);
+    char *ring = reinterpret_cast<char *>(shared + 2 * NV * threads);
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
+    const int chunk_bytes = (16 + XBYTES) * threads;
+    const int scales = STAGES * NV * chunk_bytes + me / 16 * 4;      // of the 8-bit copy: the place of this thread's group
+    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x;
+    uint32_t row = blockIdx.x;
+    int at = 0;
+    auto ask = [&](uint32_t row, int at) {
+        if (row < rows) {
+            const char *d = dy0 + (uint64_t)row * dy_row, *x = x0 + (uint64_t)row * x_row;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j * apart < left) {
+                    const uint32_t to = ring0 + (at * NV + j) * chunk_bytes, to_x = to + 16 * threads;
+                    copy_async(to + me * 16, d + j * apart * 2, 16);
+                    if (SRC != SRC_KEPT) copy_async(to_x + me * 16, x + j * apart * XSIZE, 16);
+                    else if ((me & 1) == 0) copy_async(to_x + me * 8, x + j * apart, 16);      // a vector for two threads
+                    if (SRC == SRC_KEPT && (me & 15) == 0) copy_async(ring0 + scales + (at * NV + j) * (threads / 16) * 4, a.kept.scale + (uint64_t)row * (uint32_t)a.kept.groups + (c0 + j * apart) / KEEP_GROUP, 4);
+                }
+        }
+        copies_asked();
+    };
+    float mean = 0.f, rstd = 0.f;
+    auto statistics = [&](uint32_t row) {           // of the row to come
+        if (row < rows) { mean = __ldg(a.mean + row); rstd = __ldg(a.rstd + row); }
+    };
+    // dy and the normalised input of chunk j; zeros past the last column, in dy and in gamma
+    auto values = [&](const char *places, int j, F2 less, F2 scale, F2 (&v)[PAIRS], F2 (&n)[PAIRS]) {
+        const char *from = places + j * chunk_bytes;
+        uint4 w = make_uint4(0, 0, 0, 0), x = w;
+        float kept_scale = 0.f;
+        if (j * apart < left) {
+            w = *reinterpret_cast<const uint4 *>(from + me * 16);
+            if constexpr (SRC == SRC_KEPT) { const uint2 t = *reinterpret_cast<const uint2 *>(from + 16 * threads + me * 8); x.x = t.x; x.y = t.y; kept_scale = *reinterpret_cast<const float *>(ring + scales + (at * NV + j) * (threads / 16) * 4); }
+            else x = *reinterpret_cast<const uint4 *>(from + 16 * threads + me * 16);
+        }
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w}, xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            v[i] = f2(bf16_lo(ws[i]), bf16_hi(ws[i]));
+            if constexpr (SRC == SRC_KEPT) {
+                const uint32_t q = xs[i / 2] >> (16 * (i & 1));
+                n[i] = f2((float)(int8_t)q, (float)(int8_t)(q >> 8)) * f2(kept_scale);
+            } else n[i] = f2(bf16_lo(xs[i]), bf16_hi(xs[i]));
+            n[i] = (n[i] + less) * scale;
+        }
+    };
+    ask(row, 0);
+    ask(row + step, 1);
+    statistics(row);
+    for (; row < rows; row += step, at ^= 1) {
+        if (row + step >= rows) let_next();
+        copies_wait<STAGES - 1>();
+        if (SRC == SRC_KEPT) __syncwarp();
+        const char *places = ring + at * NV * chunk_bytes;
+        const F2 less = f2(-mean), scale = f2(rstd);
+        F2 sg = f2(0.f), sgn = f2(0.f);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            F2 v[PAIRS], n[PAIRS], g[PAIRS];
+            gamma(j, g);
+            values(places, j, less, scale, v, n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                dgamma[j][i] = fma2(v[i], n[i], dgamma[j][i]);
+                dbeta[j][i] = dbeta[j][i] + v[i];
+                v[i] = v[i] * g[i];
+                sg = sg + v[i];
+                sgn = fma2(v[i], n[i], sgn);
+            }
+        }
+        float both[2] = {sum2(sg), sum2(sgn)};
+        statistics(row + step);
+        row_sums<2, BACK_THREADS / 32>(both, part[at], lane, warp, warps, 1);
+        const F2 mg = f2(-both[0] * over), mgn = f2(-both[1] * over);
+        char *dx = dx0 + (uint64_t)row * dx_row;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = c0 + j * apart;
+            F2 v[PAIRS], n[PAIRS], g[PAIRS];
+            gamma(j, g);
+            values(places, j, less, scale, v, n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) v[i] = fma2(n[i], mgn, fma2(v[i], g[i], mg)) * scale;
+            if (EXTRA && a.dres.data) add_residual<false>(a, row, c, v);
+            store_at<OSIZE, false>(dx + j * apart * OSIZE, left - j * apart, v);
+            if (EXTRA && a.y.data) {
+                F2 beta[PAIRS];
+                load_param<false>(a.p.beta, a.p, c, a.cols, 0.f, beta);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) n[i] = fma2(n[i], g[i], beta[i]);
+                store_chunk<false>(a.y, row, c, a.cols, n);
+            }
+        }
+        if (SRC == SRC_KEPT) __syncwarp();      // before another lane asks for the place again
+        ask(row + STAGES * step, at);
+    }
+    copies_wait<0>();
+    const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        store_chunk<false>(to, 0, c0 + j * apart, a.pitch, dgamma[j]);
+        store_chunk<false>(to, 1, c0 + j * apart, a.pitch, dbeta[j]);
+    }
+}
+
 // Rows of more columns than a thread can hold values of: NV chunks a thread, the sums over rows in registers, dy and x read
 // a second time (from L2) for the result.
 template <int DY, int SRC, bool STRIDED, int NV>
@@ -493,6 +636,15 @@ lrbi_status backward_launch(const NormBackward &a, const Shape &sh, int grid, cu
     const bool f32 = a.dx.dtype == LRBI_Y_F32;
     if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s);
     if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
+    if constexpr (!STRIDED && DY == SRC_BF16 && SRC != SRC_F32)
+        if (sh.chunks == 4) {
+            const size_t smem = (size_t)sh.threads * 4 * (2 * 16 + 2 * (16 + (SRC == SRC_KEPT ? 8 : 16))) + (SRC == SRC_KEPT ? sh.threads / 16 * 4 * 2 * 4 : 0);
+            const auto launch = [&](auto extra) {
+                constexpr bool EXTRA = decltype(extra)::value;
+                return f32 ? norm_launch(norm_backward_held_kernel<SRC, LRBI_Y_F32, EXTRA>, grid, dim3(sh.threads), smem, s, a) : norm_launch(norm_backward_held_kernel<SRC, LRBI_Y_BF16, EXTRA>, grid, dim3(sh.threads), smem, s, a);
+            };
+            return a.dres.data || a.y.data ? launch(std::true_type()) : launch(std::false_type());
+        }
     if (sh.chunks == 4) return norm_launch(norm_backward_again_kernel<DY, SRC, STRIDED, 4>, grid, dim3(sh.threads), 0, s, a);
     return norm_launch(norm_backward_wide_kernel<DY, SRC, STRIDED>, grid, dim3(1024), 0, s, a);
 }

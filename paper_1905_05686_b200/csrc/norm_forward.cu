@@ -20,7 +20,7 @@ namespace lrbi {
 // How bf16 values are unpacked: by 16 bits and a mask of the upper half.  Each use in a kernel has its own copy, which the
 // compiler takes for another one, and so unpacks the words anew: kept from one use to the next the values would take twice
 // the registers of the words (and were spilled).
-struct Unpack { uint32_t shift, mask; };
+struct Unpack { uint32_t shift, mask; };      // 16, 0xFFFF0000
 
 struct NormForward {
     RowsIn x;
@@ -88,15 +88,15 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
     constexpr int WARPS = Tall<SRC, STRIDED, K>::WARPS, SIZE = SRC == SRC_F32 ? 4 : 2, VECTORS = CHUNK * SIZE / 16;   // of a chunk
     extern __shared__ float4 params[];   // [chunks of a row][gamma, gamma, beta, beta][32]: a lane's 8 columns as 4 vectors
     __shared__ float part[WARPS][2][WARPS];
-    const int lane = kept_lane(), warp = threadIdx.y, warps = blockDim.y;
+    const int lane = kept_lane(), warp = kept(threadIdx.y), warps = blockDim.y, side = kept(threadIdx.z);      // side: the row's place in the block
     const int first = warp * a.each * SPAN, end = min(first + a.each * SPAN, a.cols), c = lane_column<STRIDED>(first, lane);
-    long long row = (long long)blockIdx.x * blockDim.z + threadIdx.z;
+    long long row = (long long)blockIdx.x * blockDim.z + side;
     const long long step = (long long)gridDim.x * blockDim.z;
     // then a place for each warp's part of the row to come.  Vector: [chunks][VECTORS][32].  Strided: the 16-byte vectors of
     // memory that lie in the part, at the same distance from a boundary; lanes hold the values before and after them until
     // the row's turn.
     const int place = a.each * VECTORS * 512 + (STRIDED ? 16 : 0);
-    char *ahead = reinterpret_cast<char *>(params + (a.cols + SPAN - 1) / SPAN * 4 * 32) + (threadIdx.z * warps + warp) * place;
+    char *ahead = reinterpret_cast<char *>(params + (a.cols + SPAN - 1) / SPAN * 4 * 32) + (side * warps + warp) * place;
     const uint32_t ahead_at = (uint32_t)__cvta_generic_to_shared(ahead);
     uint32_t edge = 0;
     int edge_at = -1, move = 0;
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
         copies_asked();
     };
     ask(row);
-    for (int q = threadIdx.z * warps + warp; q * SPAN < a.cols; q += warps * blockDim.z) {
+    for (int q = side * warps + warp; q * SPAN < a.cols; q += warps * blockDim.z) {
         F2 v[PAIRS];
         float f[CHUNK];
 #pragma unroll
@@ -132,13 +132,8 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             load_param<STRIDED>(which ? a.p.beta : a.p.gamma, a.p, lane_column<STRIDED>(q * SPAN, lane), a.cols, which ? 0.f : 1.f, v);
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
-            if (STRIDED) {
-#pragma unroll
-                for (int e = 0; e < CHUNK; ++e) reinterpret_cast<float *>(params + (q * 4 + which * 2) * 32)[32 * e + lane] = f[e];
-            } else {
-                params[(q * 4 + which * 2) * 32 + lane] = make_float4(f[0], f[1], f[2], f[3]);
-                params[(q * 4 + which * 2 + 1) * 32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
-            }
+            params[(q * 4 + which * 2) * 32 + lane] = make_float4(f[0], f[1], f[2], f[3]);
+            params[(q * 4 + which * 2 + 1) * 32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
         }
     }
     __syncthreads();
@@ -173,7 +168,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
         float s[1] = {sum2(t)};       // all of the row is in registers
         if (STRIDED) __syncwarp();
         ask(row + step);
-        row_sums<1, WARPS>(s, part[threadIdx.z][0], lane, warp, warps, 1 + threadIdx.z);
+        row_sums<1, WARPS>(s, part[side][0], lane, warp, warps, 1 + side);
         const float mean = s[0] * over;
         t = f2(0.f);
 #pragma unroll
@@ -188,7 +183,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             for (int i = 0; i < PAIRS; ++i) t = fma2(v[i], v[i], t);
         }
         s[0] = sum2(t);
-        row_sums<1, WARPS>(s, part[threadIdx.z][1], lane, warp, warps, 1 + threadIdx.z);
+        row_sums<1, WARPS>(s, part[side][1], lane, warp, warps, 1 + side);
         const float rstd = inverse_root(fmaf(s[0], over, a.eps));
         if (a.mean && lane == 0 && warp == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
         constexpr int YSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
@@ -224,17 +219,10 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
         for (int j = 0; j < K; ++j) {
             if (first + j * SPAN < end) {
                 x.get(j, a.use[2], v);
-                F2 gamma[PAIRS], beta[PAIRS];
-                if constexpr (STRIDED) {
-                    const float *g = reinterpret_cast<const float *>(own + j * 4 * 32) + lane;
-#pragma unroll
-                    for (int i = 0; i < PAIRS; ++i) { gamma[i] = f2(g[64 * i], g[64 * i + 32]); beta[i] = f2(g[256 + 64 * i], g[256 + 64 * i + 32]); }
-                } else {
-                    const float4 *g = own + j * 4 * 32 + lane;
-                    const float4 g0 = g[0], g1 = g[32], b0 = g[64], b1 = g[96];
-                    gamma[0] = f2(g0.x, g0.y); gamma[1] = f2(g0.z, g0.w); gamma[2] = f2(g1.x, g1.y); gamma[3] = f2(g1.z, g1.w);
-                    beta[0] = f2(b0.x, b0.y); beta[1] = f2(b0.z, b0.w); beta[2] = f2(b1.x, b1.y); beta[3] = f2(b1.z, b1.w);
-                }
+                const float4 *g = own + j * 4 * 32 + lane;
+                const float4 g0 = g[0], g1 = g[32], b0 = g[64], b1 = g[96];
+                const F2 gamma[PAIRS] = {f2(g0.x, g0.y), f2(g0.z, g0.w), f2(g1.x, g1.y), f2(g1.z, g1.w)};
+                const F2 beta[PAIRS] = {f2(b0.x, b0.y), f2(b0.z, b0.w), f2(b1.x, b1.y), f2(b1.z, b1.w)};
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[i] = fma2((v[i] + f2(-mean)) * f2(rstd), gamma[i], beta[i]);
                 store_at<YSIZE, STRIDED>(y + j * SPAN * YSIZE, end - c - j * SPAN, v, first + (j + 1) * SPAN <= end);

@@ -224,6 +224,7 @@ __device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch
 // The lane, as a value that stays in a register: out of threadIdx.x the compiler reads it from its special register again and
 // again where registers are short (60 times a row in the layer norm), and spills more for it.
 __device__ __forceinline__ int kept_lane() { return __shfl_sync(0xFFFFFFFFu, threadIdx.x & 31, threadIdx.x & 31); }
+__device__ __forceinline__ int kept(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }      // what is the same in all lanes
 
 // Asynchronous copies into shared memory: later rows are under way without registers to wait for them.
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)   // bytes: 4, 8 or 16
