@@ -286,25 +286,38 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
     }
 }
 
-// Rows of 8193 to 16384 columns in 16 or 8 bits, whole vectors: a thread has four chunks, whose sums over rows take half of
-// its registers; it reads a row's values twice out of the ring in shared memory, where gamma is too.
-// 4000 x 16384 in bf16: 139 us with the values read twice from memory (below), YYY so.
-template <int SRC, int OUT, bool EXTRA>
+// Shared memory of the kernel below.
+template <int TYPE, bool STRIDED>
+constexpr int HELD_BYTES = SPAN * (TYPE == SRC_F32 ? 4 : TYPE == SRC_BF16 ? 2 : 1) + (STRIDED && TYPE != SRC_KEPT ? 16 : 0);      // of a warp's chunk
+template <int DY, int SRC, bool STRIDED>
+constexpr int HELD_PLACE = HELD_BYTES<DY, STRIDED> + HELD_BYTES<SRC, STRIDED> + 16;      // of dy and x, and the two scales
+template <int DY, int SRC>
+constexpr int HELD_STAGES = DY == SRC_F32 || SRC == SRC_F32 ? 1 : 2;
+
+// Rows of 8193 to 16384 columns: a thread has four chunks, whose sums over rows take half of its registers; it reads a row's
+// values twice out of shared memory, where gamma is too.  A chunk's place is filled with the row after next (16 and 8 bits) or
+// the next row (32 bits, which fill the memory) as soon as its second reading is through, so that copies are always under way.
+// Warps have neighbouring chunks.  Strided: the 16-byte vectors of memory that hold a warp's chunk are copied, at the same
+// distance from a boundary; vectors that begin before the row are not, and lanes hold the values in them until the row's turn.
+// 4000 x 16384: bf16 100 us, with the values read twice from memory 139; fp32 WWW and 309; 16383 columns ZZZ and 374.
+template <int DY, int SRC, bool STRIDED, bool EXTRA, int NV>
 __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(NormBackward a)
 {
     begin();
-    constexpr int NV = 4, STAGES = 2, OSIZE = OUT == LRBI_Y_F32 ? 4 : 2, XSIZE = SRC == SRC_KEPT ? 1 : 2, XBYTES = CHUNK * XSIZE;
-    extern __shared__ float4 shared[];          // gamma: [NV][2][threads]; the ring: [STAGES][NV][dy, x][threads], scales: [STAGES][NV][threads / 16]
-    __shared__ float part[2][2 * (BACK_THREADS / 32)];
-    const int lane = kept_lane(), warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), warps = blockDim.x >> 5, apart = warps * SPAN;
-    const int threads = blockDim.x, me = warp * 32 + lane, c0 = me * CHUNK, left = a.cols - c0;
+    constexpr int STAGES = HELD_STAGES<DY, SRC>, WARPS = BACK_THREADS / 32;
+    constexpr int DSIZE = DY == SRC_F32 ? 4 : 2, XSIZE = SRC == SRC_F32 ? 4 : SRC == SRC_BF16 ? 2 : 1;
+    constexpr int DBYTES = HELD_BYTES<DY, STRIDED>, XBYTES = HELD_BYTES<SRC, STRIDED>, PLACE = HELD_PLACE<DY, SRC, STRIDED>;
+    extern __shared__ float4 shared[];          // gamma: [NV][2][threads]; then [STAGES][warps][NV][PLACE]
+    __shared__ float part[2][2 * WARPS];
+    const int lane = kept_lane(), warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), warps = blockDim.x >> 5;
+    const int threads = blockDim.x, first = warp * NV * SPAN, c0 = lane_column<STRIDED>(first, lane);
     const float over = 1.f / (float)a.cols;
     F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS];
-    float4 *gammas = shared + me;
+    float4 *gammas = shared + warp * 32 + lane;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         F2 g[PAIRS];
-        load_param<false>(a.p.gamma, a.p, c0 + j * apart, a.cols, 0.f, g);
+        load_param<STRIDED>(a.p.gamma, a.p, c0 + j * SPAN, a.cols, 0.f, g);
         float f[CHUNK];
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
@@ -315,76 +328,141 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
         gammas[2 * j * threads] = make_float4(f[0], f[1], f[2], f[3]);      // read by this thread alone
         gammas[(2 * j + 1) * threads] = make_float4(f[4], f[5], f[6], f[7]);
     }
+    char *own = reinterpret_cast<char *>(shared + 2 * NV * threads) + warp * NV * PLACE;       // of this warp, in the first stage
+    const uint32_t own_at = (uint32_t)__cvta_generic_to_shared(own);
+    const int stage = warps * NV * PLACE;
+    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x;
+    const char *dy_data = static_cast<const char *>(a.dy.data), *x_data = SRC == SRC_KEPT ? reinterpret_cast<const char *>(a.kept.q) : static_cast<const char *>(a.x.data);
+    const uint32_t dy_row = (uint32_t)(a.dy.stride * DSIZE), x_row = SRC == SRC_KEPT ? (uint32_t)a.kept.pitch : (uint32_t)(a.x.stride * XSIZE);
+
+    // Values of a row that share their 16 bytes with what is before the row: held by the lanes of the first warp.
+    uint32_t dy_edge = 0, x_edge = 0;
+    auto ask_span = [&](const char *p, int size, int j, uint32_t to, uint32_t &edge) {      // p: the row; to: the place
+        const int c = first + j * SPAN, bytes = min(SPAN, a.cols - c) * size;
+        const char *from = p + c * size;
+        const int move = (int)(reinterpret_cast<intptr_t>(from) & 15);
+        from -= move;
+        for (int i = lane * 16; i < move + bytes; i += 512)
+            if (i > 0 || c > 0 || move == 0) copy_async_some(to + i, from + i, min(16, move + bytes - i));
+        if (c == 0 && move && lane * size < min(16 - move, bytes)) edge = size == 4 ? __ldg(reinterpret_cast<const uint32_t *>(p) + lane) : (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(p) + lane);
+    };
+    auto put_edge = [&](const char *p, int size, char *place, uint32_t edge) {
+        const int move = (int)(reinterpret_cast<intptr_t>(p) & 15);
+        if (move && lane * size < min(16 - move, a.cols * size)) {
+            if (size == 4) *reinterpret_cast<uint32_t *>(place + move + lane * 4) = edge;
+            else *reinterpret_cast<uint16_t *>(place + move + lane * 2) = (uint16_t)edge;
+        }
+    };
+    auto put_edges = [&](uint32_t row, char *places) {
+        if (row >= rows) return;
+        put_edge(dy_data + (uint64_t)row * dy_row, DSIZE, places, dy_edge);
+        if (SRC != SRC_KEPT) put_edge(x_data + (uint64_t)row * x_row, XSIZE, places + DBYTES, x_edge);
+    };
+    auto ask = [&](uint32_t row, int j, int at) {
+        const int c = first + j * SPAN;
+        if (STRIDED && STAGES == 2 && c == 0 && row != blockIdx.x) put_edges(row - step, own + (at ^ 1) * stage);      // those asked for last
+        if (row < rows && c < a.cols) {
+            const char *d = dy_data + (uint64_t)row * dy_row, *x = x_data + (uint64_t)row * x_row;
+            const uint32_t to = own_at + at * stage + j * PLACE, to_x = to + DBYTES;
+            if constexpr (STRIDED) ask_span(d, DSIZE, j, to, dy_edge);
+            else if (c0 + j * SPAN < a.cols) {
+#pragma unroll
+                for (int i = 0; i < DSIZE / 2; ++i) copy_async(to + (i * 32 + lane) * 16, d + (c0 + j * SPAN) * DSIZE + 16 * i, 16);
+            }
+            if constexpr (SRC == SRC_KEPT) {
+                const int q = c + lane * 16;        // 16 columns a lane; rows of the copy are whole vectors
+                if (lane < 16 && q < a.kept.pitch) copy_async(to_x + lane * 16, x + q, 16);
+                if (lane < 2 && c + lane * KEEP_GROUP < a.cols) copy_async(to_x + XBYTES + lane * 4, a.kept.scale + (uint64_t)row * (uint32_t)a.kept.groups + c / KEEP_GROUP + lane, 4);
+            } else if constexpr (STRIDED) ask_span(x, XSIZE, j, to_x, x_edge);
+            else if (c0 + j * SPAN < a.cols) {
+#pragma unroll
+                for (int i = 0; i < XSIZE / 2; ++i) copy_async(to_x + (i * 32 + lane) * 16, x + (c0 + j * SPAN) * XSIZE + 16 * i, 16);
+            }
+        }
+        copies_asked();
+    };
+    // A chunk out of shared memory: `at` its place, `move` where its first value is (strided).
+    auto chunk = [&](auto type, const char *at, int move, int left, int warp_left, F2 (&v)[PAIRS]) {
+        constexpr int TYPE = decltype(type)::value;
+        if constexpr (STRIDED && TYPE != SRC_KEPT) {
+            constexpr int SIZE = TYPE == SRC_F32 ? 4 : 2;
+            const char *p = at + move + lane * SIZE;
+            float f[CHUNK];
+#pragma unroll
+            for (int e = 0; e < CHUNK; ++e) f[e] = SIZE == 4 ? reinterpret_cast<const float *>(p)[32 * e] : __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[32 * e] << 16);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
+        } else if constexpr (TYPE == SRC_F32) {
+            const float4 x = reinterpret_cast<const float4 *>(at)[lane], y = reinterpret_cast<const float4 *>(at)[32 + lane];
+            v[0] = f2(x.x, x.y); v[1] = f2(x.z, x.w); v[2] = f2(y.x, y.y); v[3] = f2(y.z, y.w);
+        } else if constexpr (TYPE == SRC_BF16) {
+            const uint4 x = reinterpret_cast<const uint4 *>(at)[lane];
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) v[i] = f2(bf16_lo(w[i]), bf16_hi(w[i]));
+        } else {
+            const float *scale = reinterpret_cast<const float *>(at + XBYTES);
+            if constexpr (STRIDED) {
+                const int8_t *q = reinterpret_cast<const int8_t *>(at) + lane;
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[i] = f2((float)q[64 * i], (float)q[64 * i + 32]) * f2(scale[i / 2]);
+            } else {
+                const uint2 x = reinterpret_cast<const uint2 *>(at)[lane];
+                const F2 s = f2(scale[lane >> 4]);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    const uint32_t q = (i < 2 ? x.x : x.y) >> (16 * (i & 1));
+                    v[i] = f2((float)(int8_t)q, (float)(int8_t)(q >> 8)) * s;
+                }
+            }
+        }
+        if (warp_left < SPAN) {                 // zeros past the last column
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                float lo, hi;
+                split(v[i], lo, hi);
+                v[i] = f2(chunk_column<STRIDED>(0, 2 * i) < left ? lo : 0.f, chunk_column<STRIDED>(0, 2 * i + 1) < left ? hi : 0.f);
+            }
+        }
+    };
     auto gamma = [&](int j, F2 (&g)[PAIRS]) {
         const float4 lo = gammas[2 * j * threads], hi = gammas[(2 * j + 1) * threads];
         g[0] = f2(lo.x, lo.y); g[1] = f2(lo.z, lo.w); g[2] = f2(hi.x, hi.y); g[3] = f2(hi.z, hi.w);
     };
-    const char *dy0 = static_cast<const char *>(a.dy.data) + c0 * 2;
-    const char *x0 = SRC == SRC_KEPT ? reinterpret_cast<const char *>(a.kept.q + c0) : static_cast<const char *>(a.x.data) + c0 * XSIZE;
-    char *dx0 = static_cast<char *>(a.dx.data) + c0 * OSIZE;
-    const uint32_t dy_row = (uint32_t)(a.dy.stride * 2), x_row = SRC == SRC_KEPT ? (uint32_t)a.kept.pitch : (uint32_t)(a.x.stride * XSIZE), dx_row = (uint32_t)(a.dx.stride * OSIZE);
-    char *ring = reinterpret_cast<char *>(shared + 2 * NV * threads);
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(ring);
-    const int chunk_bytes = (16 + XBYTES) * threads;
-    const int scales = STAGES * NV * chunk_bytes + me / 16 * 4;      // of the 8-bit copy: the place of this thread's group
-    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x;
     uint32_t row = blockIdx.x;
-    int at = 0;
-    auto ask = [&](uint32_t row, int at) {
-        if (row < rows) {
-            const char *d = dy0 + (uint64_t)row * dy_row, *x = x0 + (uint64_t)row * x_row;
+    int at = 0, turn = 0;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (j * apart < left) {
-                    const uint32_t to = ring0 + (at * NV + j) * chunk_bytes, to_x = to + 16 * threads;
-                    copy_async(to + me * 16, d + j * apart * 2, 16);
-                    if (SRC != SRC_KEPT) copy_async(to_x + me * 16, x + j * apart * XSIZE, 16);
-                    else if ((me & 1) == 0) copy_async(to_x + me * 8, x + j * apart, 16);      // a vector for two threads
-                    if (SRC == SRC_KEPT && (me & 15) == 0) copy_async(ring0 + scales + (at * NV + j) * (threads / 16) * 4, a.kept.scale + (uint64_t)row * (uint32_t)a.kept.groups + (c0 + j * apart) / KEEP_GROUP, 4);
-                }
-        }
-        copies_asked();
-    };
+    for (int i = 0; i < STAGES * NV; ++i) ask(row + i / NV * step, i % NV, i / NV);
     float mean = 0.f, rstd = 0.f;
-    auto statistics = [&](uint32_t row) {           // of the row to come
-        if (row < rows) { mean = __ldg(a.mean + row); rstd = __ldg(a.rstd + row); }
-    };
-    // dy and the normalised input of chunk j; zeros past the last column, in dy and in gamma
-    auto values = [&](const char *places, int j, F2 less, F2 scale, F2 (&v)[PAIRS], F2 (&n)[PAIRS]) {
-        const char *from = places + j * chunk_bytes;
-        uint4 w = make_uint4(0, 0, 0, 0), x = w;
-        float kept_scale = 0.f;
-        if (j * apart < left) {
-            w = *reinterpret_cast<const uint4 *>(from + me * 16);
-            if constexpr (SRC == SRC_KEPT) { const uint2 t = *reinterpret_cast<const uint2 *>(from + 16 * threads + me * 8); x.x = t.x; x.y = t.y; kept_scale = *reinterpret_cast<const float *>(ring + scales + (at * NV + j) * (threads / 16) * 4); }
-            else x = *reinterpret_cast<const uint4 *>(from + 16 * threads + me * 16);
-        }
-        const uint32_t ws[4] = {w.x, w.y, w.z, w.w}, xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < PAIRS; ++i) {
-            v[i] = f2(bf16_lo(ws[i]), bf16_hi(ws[i]));
-            if constexpr (SRC == SRC_KEPT) {
-                const uint32_t q = xs[i / 2] >> (16 * (i & 1));
-                n[i] = f2((float)(int8_t)q, (float)(int8_t)(q >> 8)) * f2(kept_scale);
-            } else n[i] = f2(bf16_lo(xs[i]), bf16_hi(xs[i]));
-            n[i] = (n[i] + less) * scale;
-        }
-    };
-    ask(row, 0);
-    ask(row + step, 1);
+    auto statistics = [&](uint32_t r) { if (r < rows) { mean = __ldg(a.mean + r); rstd = __ldg(a.rstd + r); } };       // of the row to come
     statistics(row);
-    for (; row < rows; row += step, at ^= 1) {
+    for (; row < rows; row += step) {
         if (row + step >= rows) let_next();
-        copies_wait<STAGES - 1>();
-        if (SRC == SRC_KEPT) __syncwarp();
-        const char *places = ring + at * NV * chunk_bytes;
+        char *places = own + at * stage;
+        const int dy_move = STRIDED ? (int)(reinterpret_cast<intptr_t>(dy_data + (uint64_t)row * dy_row) & 15) : 0;
+        const int x_move = STRIDED ? (int)(reinterpret_cast<intptr_t>(x_data + (uint64_t)row * x_row) & 15) : 0;
         const F2 less = f2(-mean), scale = f2(rstd);
+        // dy and the normalised input of chunk j
+        auto values = [&](int j, F2 (&v)[PAIRS], F2 (&n)[PAIRS]) {
+            const int left = a.cols - c0 - j * SPAN, warp_left = a.cols - first - j * SPAN;
+            chunk(std::integral_constant<int, DY>(), places + j * PLACE, dy_move, left, warp_left, v);
+            chunk(std::integral_constant<int, SRC>(), places + j * PLACE + DBYTES, x_move, left, warp_left, n);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) n[i] = (n[i] + less) * scale;
+        };
         F2 sg = f2(0.f), sgn = f2(0.f);
+        if (STRIDED && STAGES == 1 && warp == 0) put_edges(row, places);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (j == 0) copies_wait<STAGES * NV - 1>();
+            if (j == 1) copies_wait<STAGES * NV - 2>();
+            if (j == 2) copies_wait<STAGES * NV - 3>();
+            if (j == 3) copies_wait<STAGES * NV - 4>();
+            if (STRIDED || SRC == SRC_KEPT) __syncwarp();
+            if (first + j * SPAN >= a.cols) continue;
             F2 v[PAIRS], n[PAIRS], g[PAIRS];
             gamma(j, g);
-            values(places, j, less, scale, v, n);
+            values(j, v, n);
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) {
                 dgamma[j][i] = fma2(v[i], n[i], dgamma[j][i]);
@@ -396,114 +474,39 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
         }
         float both[2] = {sum2(sg), sum2(sgn)};
         statistics(row + step);
-        row_sums<2, BACK_THREADS / 32>(both, part[at], lane, warp, warps, 1);
+        row_sums<2, WARPS>(both, part[turn], lane, warp, warps, 1);
+        turn ^= 1;
         const F2 mg = f2(-both[0] * over), mgn = f2(-both[1] * over);
-        char *dx = dx0 + (uint64_t)row * dx_row;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = c0 + j * apart;
-            F2 v[PAIRS], n[PAIRS], g[PAIRS];
-            gamma(j, g);
-            values(places, j, less, scale, v, n);
+            const int c = c0 + j * SPAN;
+            if (first + j * SPAN < a.cols) {
+                F2 v[PAIRS], n[PAIRS], g[PAIRS];
+                gamma(j, g);
+                values(j, v, n);
+                if (STRIDED || SRC == SRC_KEPT) __syncwarp();      // before another lane asks for the place again
+                ask(row + STAGES * step, j, at);
 #pragma unroll
-            for (int i = 0; i < PAIRS; ++i) v[i] = fma2(n[i], mgn, fma2(v[i], g[i], mg)) * scale;
-            if (EXTRA && a.dres.data) add_residual<false>(a, row, c, v);
-            store_at<OSIZE, false>(dx + j * apart * OSIZE, left - j * apart, v);
-            if (EXTRA && a.y.data) {
-                F2 beta[PAIRS];
-                load_param<false>(a.p.beta, a.p, c, a.cols, 0.f, beta);
+                for (int i = 0; i < PAIRS; ++i) v[i] = fma2(n[i], mgn, fma2(v[i], g[i], mg)) * scale;
+                if (EXTRA && a.dres.data) add_residual<STRIDED>(a, row, c, v);
+                store_chunk<STRIDED>(a.dx, row, c, a.cols, v);
+                if (EXTRA && a.y.data) {
+                    F2 beta[PAIRS];
+                    load_param<STRIDED>(a.p.beta, a.p, c, a.cols, 0.f, beta);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) n[i] = fma2(n[i], g[i], beta[i]);
-                store_chunk<false>(a.y, row, c, a.cols, n);
-            }
+                    for (int i = 0; i < PAIRS; ++i) n[i] = fma2(n[i], g[i], beta[i]);
+                    store_chunk<STRIDED>(a.y, row, c, a.cols, n);
+                }
+            } else copies_asked();
         }
-        if (SRC == SRC_KEPT) __syncwarp();      // before another lane asks for the place again
-        ask(row + STAGES * step, at);
+        at = at + 1 == STAGES ? 0 : at + 1;
     }
     copies_wait<0>();
     const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        store_chunk<false>(to, 0, c0 + j * apart, a.pitch, dgamma[j]);
-        store_chunk<false>(to, 1, c0 + j * apart, a.pitch, dbeta[j]);
-    }
-}
-
-// Rows of more columns than a thread can hold values of: NV chunks a thread, the sums over rows in registers, dy and x read
-// a second time (from L2) for the result.
-template <int DY, int SRC, bool STRIDED, int NV>
-__global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_again_kernel(NormBackward a)
-{
-    begin();
-    __shared__ float part[2][2 * (BACK_THREADS / 32)];
-    const int lane = kept_lane(), warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), warps = blockDim.x >> 5, apart = warps * SPAN;
-    const float over = 1.f / (float)a.cols;
-    const int c0 = lane_column<STRIDED>(warp * SPAN, lane);
-    F2 dgamma[NV][PAIRS], dbeta[NV][PAIRS];
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < PAIRS; ++i) { dgamma[j][i] = f2(0.f); dbeta[j][i] = f2(0.f); }
-    Raw<DY, STRIDED> raw_dy[NV];
-    Raw<SRC, STRIDED> raw_x[NV];
-    auto load = [&](long long row) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            raw_dy[j].load(a.dy, a.kept, row, c0 + j * apart, a.cols);
-            raw_x[j].load(a.x, a.kept, row, c0 + j * apart, a.cols);
-        }
-    };
-    int turn = 0;
-    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        load(row);
-        const F2 less = f2(-__ldg(a.mean + row)), scale = f2(__ldg(a.rstd + row));
-        F2 dy[PAIRS], n[PAIRS], gamma[PAIRS], sg = f2(0.f), sgn = f2(0.f);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            load_param<STRIDED>(a.p.gamma, a.p, c0 + j * apart, a.cols, 0.f, gamma);
-            raw_dy[j].get(dy);
-            raw_x[j].get(n);
-#pragma unroll
-            for (int i = 0; i < PAIRS; ++i) {
-                n[i] = (n[i] + less) * scale;
-                dgamma[j][i] = fma2(dy[i], n[i], dgamma[j][i]);
-                dbeta[j][i] = dbeta[j][i] + dy[i];
-                dy[i] = dy[i] * gamma[i];
-                sg = sg + dy[i];
-                sgn = fma2(dy[i], n[i], sgn);
-            }
-        }
-        float both[2] = {sum2(sg), sum2(sgn)};
-        row_sums<2, BACK_THREADS / 32>(both, part[turn], lane, warp, warps, 1);
-        const F2 mg = f2(-both[0] * over), mgn = f2(-both[1] * over);
-        load(row);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int c = c0 + j * apart;
-            load_param<STRIDED>(a.p.gamma, a.p, c, a.cols, 0.f, gamma);
-            raw_dy[j].get(dy);
-            raw_x[j].get(n);
-#pragma unroll
-            for (int i = 0; i < PAIRS; ++i) {
-                n[i] = (n[i] + less) * scale;
-                dy[i] = fma2(n[i], mgn, fma2(dy[i], gamma[i], mg)) * scale;
-            }
-            if (a.dres.data) add_residual<STRIDED>(a, row, c, dy);
-            store_chunk<STRIDED>(a.dx, row, c, a.cols, dy);
-            if (a.y.data) {
-                F2 beta[PAIRS];
-                load_param<STRIDED>(a.p.beta, a.p, c, a.cols, 0.f, beta);
-#pragma unroll
-                for (int i = 0; i < PAIRS; ++i) n[i] = fma2(n[i], gamma[i], beta[i]);
-                store_chunk<STRIDED>(a.y, row, c, a.cols, n);
-            }
-        }
-    }
-    const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        store_chunk<STRIDED>(to, 0, c0 + j * apart, a.pitch, dgamma[j]);
-        store_chunk<STRIDED>(to, 1, c0 + j * apart, a.pitch, dbeta[j]);
+        store_chunk<STRIDED>(to, 0, c0 + j * SPAN, a.pitch, dgamma[j]);
+        store_chunk<STRIDED>(to, 1, c0 + j * SPAN, a.pitch, dbeta[j]);
     }
 }
 
@@ -630,22 +633,23 @@ lrbi_status ring_launch(const NormBackward &a, const Shape &sh, int grid, cudaSt
     return norm_launch(norm_backward_kernel<DY, SRC, OUT, STRIDED, false, NV, R>, grid, block, std::max(ring, sums), s, a);
 }
 
+template <int DY, int SRC, bool STRIDED, int NV>
+lrbi_status held_launch(const NormBackward &a, const Shape &sh, int grid, cudaStream_t s)
+{
+    const size_t smem = (size_t)sh.threads * NV * 32 + (size_t)sh.threads / 32 * NV * HELD_STAGES<DY, SRC> * HELD_PLACE<DY, SRC, STRIDED>;
+    if (a.dres.data || a.y.data) return norm_launch(norm_backward_held_kernel<DY, SRC, STRIDED, true, NV>, grid, dim3(sh.threads), smem, s, a);
+    return norm_launch(norm_backward_held_kernel<DY, SRC, STRIDED, false, NV>, grid, dim3(sh.threads), smem, s, a);
+}
+
 template <int DY, int SRC, bool STRIDED>
 lrbi_status backward_launch(const NormBackward &a, const Shape &sh, int grid, cudaStream_t s)
 {
     const bool f32 = a.dx.dtype == LRBI_Y_F32;
     if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s);
-    if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
-    if constexpr (!STRIDED && DY == SRC_BF16 && SRC != SRC_F32)
-        if (sh.chunks == 4) {
-            const size_t smem = (size_t)sh.threads * 4 * (2 * 16 + 2 * (16 + (SRC == SRC_KEPT ? 8 : 16))) + (SRC == SRC_KEPT ? sh.threads / 16 * 4 * 2 * 4 : 0);
-            const auto launch = [&](auto extra) {
-                constexpr bool EXTRA = decltype(extra)::value;
-                return f32 ? norm_launch(norm_backward_held_kernel<SRC, LRBI_Y_F32, EXTRA>, grid, dim3(sh.threads), smem, s, a) : norm_launch(norm_backward_held_kernel<SRC, LRBI_Y_BF16, EXTRA>, grid, dim3(sh.threads), smem, s, a);
-            };
-            return a.dres.data || a.y.data ? launch(std::true_type()) : launch(std::false_type());
-        }
-    if (sh.chunks == 4) return norm_launch(norm_backward_again_kernel<DY, SRC, STRIDED, 4>, grid, dim3(sh.threads), 0, s, a);
+    if (sh.chunks == 2)
+        if constexpr (STRIDED) return held_launch<DY, SRC, true, 2>(a, sh, grid, s);
+        else return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
+    if (sh.chunks == 4) return held_launch<DY, SRC, STRIDED, 4>(a, sh, grid, s);
     return norm_launch(norm_backward_wide_kernel<DY, SRC, STRIDED>, grid, dim3(1024), 0, s, a);
 }
 
