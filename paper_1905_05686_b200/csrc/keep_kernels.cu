@@ -185,7 +185,7 @@ lrbi_status launch_checkpoint_store(const void *x, int dtype, long long stride, 
     k.h = {x, stride};
     k.kept = {q, scale, checkpoint_pitch(cols), checkpoint_groups(cols)};
     k.rows = rows; k.cols = cols;
-    const bool strided = cols % CHUNK != 0 || !rows16(x, stride, dtype);
+    const bool strided = cols % CHUNK != 0 || !vector_rows(x, stride, dtype);
 #define STORE(SRC) strided ? keep_launch<SRC, ACT_NONE, false, SRC_BF16, LRBI_Y_BF16, true, true>(k, s) : keep_launch<SRC, ACT_NONE, false, SRC_BF16, LRBI_Y_BF16, true, false>(k, s)
     return dtype == LRBI_Y_BF16 ? (STORE(SRC_BF16)) : (STORE(SRC_F32));
 #undef STORE
@@ -197,7 +197,7 @@ lrbi_status launch_checkpoint_load(const int8_t *q, const float *scale, int rows
     k.from = {q, scale, checkpoint_pitch(cols), checkpoint_groups(cols)};
     k.a = {x, stride, dtype};
     k.rows = rows; k.cols = cols;
-    const bool strided = cols % CHUNK != 0 || !rows16(x, stride, dtype);
+    const bool strided = cols % CHUNK != 0 || !vector_rows(x, stride, dtype);
 #define LOAD(OUT) strided ? keep_launch<SRC_KEPT, ACT_NONE, false, SRC_BF16, OUT, false, true>(k, s) : keep_launch<SRC_KEPT, ACT_NONE, false, SRC_BF16, OUT, false, false>(k, s)
     return dtype == LRBI_Y_BF16 ? (LOAD(LRBI_Y_BF16)) : (LOAD(LRBI_Y_F32));
 #undef LOAD
@@ -210,7 +210,7 @@ lrbi_status launch_activation(const ActArgs &n, cudaStream_t s)
     k.a = {n.a, n.a_stride, n.a_dtype};
     k.kept = {n.q_out, n.scale_out, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)};
     k.rows = n.rows; k.cols = n.cols;
-    const bool strided = n.cols % CHUNK != 0 || !rows16(n.h, n.h_stride, n.h_dtype) || !rows16(n.a, n.a_stride, n.a_dtype);
+    const bool strided = n.cols % CHUNK != 0 || !vector_rows(n.h, n.h_stride, n.h_dtype) || !vector_rows(n.a, n.a_stride, n.a_dtype);
 #define FORWARD(SRC, OUT) n.q_out ? act_launch<SRC, false, SRC_BF16, OUT, true>(k, n.act, strided, s) : act_launch<SRC, false, SRC_BF16, OUT, false>(k, n.act, strided, s)
     if (n.h_dtype == LRBI_Y_BF16) return n.a_dtype == LRBI_Y_BF16 ? (FORWARD(SRC_BF16, LRBI_Y_BF16)) : (FORWARD(SRC_BF16, LRBI_Y_F32));
     return n.a_dtype == LRBI_Y_BF16 ? (FORWARD(SRC_F32, LRBI_Y_BF16)) : (FORWARD(SRC_F32, LRBI_Y_F32));
@@ -226,8 +226,8 @@ lrbi_status launch_activation_backward(const ActArgs &n, cudaStream_t s)
     k.dh = {n.dh, n.dh_stride, n.dh_dtype};
     k.a = {n.a, n.a_stride, n.a_dtype};
     k.rows = n.rows; k.cols = n.cols;
-    const bool strided = n.cols % CHUNK != 0 || (!n.q && !rows16(n.h, n.h_stride, n.h_dtype)) || !rows16(n.da, n.da_stride, n.da_dtype) ||
-                       !rows16(n.dh, n.dh_stride, n.dh_dtype) || (n.a && !rows16(n.a, n.a_stride, n.a_dtype));
+    const bool strided = n.cols % CHUNK != 0 || (!n.q && !vector_rows(n.h, n.h_stride, n.h_dtype)) || !vector_rows(n.da, n.da_stride, n.da_dtype) ||
+                       !vector_rows(n.dh, n.dh_stride, n.dh_dtype) || (n.a && !vector_rows(n.a, n.a_stride, n.a_dtype));
     const int src = n.q ? SRC_KEPT : n.h_dtype;
 #define BACKWARD(SRC, DA) n.dh_dtype == LRBI_Y_BF16 ? act_launch<SRC, true, DA, LRBI_Y_BF16, false>(k, n.act, strided, s) : act_launch<SRC, true, DA, LRBI_Y_F32, false>(k, n.act, strided, s)
     if (n.da_dtype == LRBI_Y_BF16) {

@@ -35,6 +35,21 @@ __device__ __forceinline__ void add_residual(const NormBackward &a, long long ro
     for (int i = 0; i < PAIRS; ++i) v[i] = v[i] + r[i];
 }
 
+// A chunk's sums over the rows of this block: 0 of dgamma, 1 of dbeta.
+template <bool STRIDED>
+__device__ __forceinline__ void store_part(const NormBackward &a, int which, int c, const F2 (&v)[PAIRS])
+{
+    float *p = a.part + ((long long)blockIdx.x * 2 + which) * a.pitch + c;
+    if constexpr (STRIDED) store_at<4, true>(reinterpret_cast<char *>(p), a.pitch - c, v);
+    else if (c < a.pitch) {
+        float f[CHUNK];
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
+        reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+}
+
 // Threads of a block: vector rows 16 warps of up to 128 registers; strided rows 20 of up to 96, without a ring to hide latency.
 constexpr int BACK_THREADS = 512, BACK_THREADS_STRIDED = 640;
 
@@ -85,15 +100,24 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
                 if (first + r < rows && j * apart < left) {
                     const char *d = dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, *x = x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE;
                     const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes, to_x = to + DBYTES * threads;
-#pragma unroll
-                    for (int i = 0; i < DBYTES / 16; ++i) copy_async(to + (i * threads + me) * 16, d + 16 * i, 16);
-                    if constexpr (SRC == SRC_KEPT) {       // a vector for two threads; rows of the copy are whole vectors
-                        if ((me & 1) == 0) copy_async(to_x + me * 8, x, 16);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < XBYTES / 16; ++i) copy_async(to_x + (i * threads + me) * 16, x + 16 * i, 16);
-                    }
+                    if (DSIZE == 2) copy_async(to + me * 16, d, 16);
+                    if (SRC == SRC_BF16) copy_async(to_x + me * 16, x, 16);
+                    if (SRC == SRC_KEPT && (me & 1) == 0) copy_async(to_x + me * 8, x, 16);       // a vector for two threads; rows of the copy are whole vectors
                 }
+        if constexpr (DSIZE == 4 || SRC == SRC_F32) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (first + r < rows && j * apart + i * 128 + lane * 4 < warp_left) {
+                            const int c = warp * SPAN + j * apart + i * 128 + lane * 4;
+                            const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes + (me >> 5) * 1024 + i * 512 + fp32_copied(lane);
+                            if (DSIZE == 4) copy_async(to, static_cast<const char *>(a.dy.data) + (uint64_t)(first + r) * dy_row + c * 4, 16);
+                            if (SRC == SRC_F32) copy_async(to + DBYTES * threads, static_cast<const char *>(a.x.data) + (uint64_t)(first + r) * x_row + c * 4, 16);
+                        }
+        }
         copies_asked();
     };
     float mean[R], rstd[R], scales[R][NV];      // of the round to come; a vector row's scales of its 8-bit copy
@@ -111,7 +135,7 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
     Raw<DY, STRIDED> raw_dy[R][NV];
     Raw<SRC, STRIDED> raw_x[R][NV];
     auto take = [&](int at) {
-        if (SRC == SRC_KEPT) __syncwarp();
+        if (SRC != SRC_BF16 || DSIZE == 4) __syncwarp();         // lanes read what others copied
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -122,7 +146,7 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
                 if (j * apart < left) {
 #pragma unroll
                     for (int i = 0; i < DBYTES / 16; ++i) {
-                        const uint4 v = *reinterpret_cast<const uint4 *>(from + (i * threads + me) * 16);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(from + (DSIZE == 4 ? (me >> 5) * 1024 + fp32_read(lane, i) : me * 16));
                         uint32_t *w = raw_dy[r][j].w + (STRIDED ? 0 : 4 * i);
                         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
                     }
@@ -134,7 +158,7 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
                     } else {
 #pragma unroll
                         for (int i = 0; i < XBYTES / 16; ++i) {
-                            const uint4 v = *reinterpret_cast<const uint4 *>(from_x + (i * threads + me) * 16);
+                            const uint4 v = *reinterpret_cast<const uint4 *>(from_x + (XSIZE == 4 ? (me >> 5) * 1024 + fp32_read(lane, i) : me * 16));
                             uint32_t *w = raw_x[r][j].w + (STRIDED ? 0 : 4 * i);
                             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
                         }
@@ -278,15 +302,15 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
                 }
         }
     }
-    const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        store_chunk<STRIDED>(to, 0, c0 + j * apart, a.pitch, dgamma[j]);
-        store_chunk<STRIDED>(to, 1, c0 + j * apart, a.pitch, dbeta[j]);
+        store_part<STRIDED>(a, 0, c0 + j * apart, dgamma[j]);
+        store_part<STRIDED>(a, 1, c0 + j * apart, dbeta[j]);
     }
 }
 
-// Shared memory of the kernel below.
+// Threads and shared memory of the kernel below.
+template <int NV> constexpr int HELD_THREADS = NV == 2 ? 640 : 512;
 template <int TYPE, bool STRIDED>
 constexpr int HELD_BYTES = SPAN * (TYPE == SRC_F32 ? 4 : TYPE == SRC_BF16 ? 2 : 1) + (STRIDED && TYPE != SRC_KEPT ? 16 : 0);      // of a warp's chunk
 template <int DY, int SRC, bool STRIDED>
@@ -301,11 +325,12 @@ constexpr int HELD_STAGES = DY == SRC_F32 || SRC == SRC_F32 ? 1 : 2;
 // distance from a boundary; vectors that begin before the row are not, and lanes hold the values in them until the row's turn.
 // 4000 x 16384: bf16 100 us, with the values read twice from memory 139; fp32 WWW and 309; 16383 columns ZZZ and 374.
 template <int DY, int SRC, bool STRIDED, bool EXTRA, int NV>
-__global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(NormBackward a)
+__global__ void __launch_bounds__(HELD_THREADS<NV>, 1) norm_backward_held_kernel(NormBackward a)
 {
     begin();
-    constexpr int STAGES = HELD_STAGES<DY, SRC>, WARPS = BACK_THREADS / 32;
+    constexpr int STAGES = HELD_STAGES<DY, SRC>, WARPS = HELD_THREADS<NV> / 32;
     constexpr int DSIZE = DY == SRC_F32 ? 4 : 2, XSIZE = SRC == SRC_F32 ? 4 : SRC == SRC_BF16 ? 2 : 1;
+    constexpr bool SHARED = STRIDED || SRC != SRC_BF16 || DY == SRC_F32;     // lanes read what others copied
     constexpr int DBYTES = HELD_BYTES<DY, STRIDED>, XBYTES = HELD_BYTES<SRC, STRIDED>, PLACE = HELD_PLACE<DY, SRC, STRIDED>;
     extern __shared__ float4 shared[];          // gamma: [NV][2][threads]; then [STAGES][warps][NV][PLACE]
     __shared__ float part[2][2 * WARPS];
@@ -335,6 +360,11 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
     const char *dy_data = static_cast<const char *>(a.dy.data), *x_data = SRC == SRC_KEPT ? reinterpret_cast<const char *>(a.kept.q) : static_cast<const char *>(a.x.data);
     const uint32_t dy_row = (uint32_t)(a.dy.stride * DSIZE), x_row = SRC == SRC_KEPT ? (uint32_t)a.kept.pitch : (uint32_t)(a.x.stride * XSIZE);
 
+    auto ask_vectors = [&](const char *p, int size, int c, uint32_t to) {      // p: the row; c: the span's first column; to: the place
+#pragma unroll
+        for (int i = 0; i < size / 2; ++i)
+            if (c + (i * 32 + lane) * 16 / size < a.cols) copy_async(to + i * 512 + (size == 4 ? fp32_copied(lane) : lane * 16), p + c * size + i * 512 + lane * 16, 16);
+    };
     // Values of a row that share their 16 bytes with what is before the row: held by the lanes of the first warp.
     uint32_t dy_edge = 0, x_edge = 0;
     auto ask_span = [&](const char *p, int size, int j, uint32_t to, uint32_t &edge) {      // p: the row; to: the place
@@ -365,19 +395,13 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
             const char *d = dy_data + (uint64_t)row * dy_row, *x = x_data + (uint64_t)row * x_row;
             const uint32_t to = own_at + at * stage + j * PLACE, to_x = to + DBYTES;
             if constexpr (STRIDED) ask_span(d, DSIZE, j, to, dy_edge);
-            else if (c0 + j * SPAN < a.cols) {
-#pragma unroll
-                for (int i = 0; i < DSIZE / 2; ++i) copy_async(to + (i * 32 + lane) * 16, d + (c0 + j * SPAN) * DSIZE + 16 * i, 16);
-            }
+            else ask_vectors(d, DSIZE, c, to);
             if constexpr (SRC == SRC_KEPT) {
                 const int q = c + lane * 16;        // 16 columns a lane; rows of the copy are whole vectors
                 if (lane < 16 && q < a.kept.pitch) copy_async(to_x + lane * 16, x + q, 16);
                 if (lane < 2 && c + lane * KEEP_GROUP < a.cols) copy_async(to_x + XBYTES + lane * 4, a.kept.scale + (uint64_t)row * (uint32_t)a.kept.groups + c / KEEP_GROUP + lane, 4);
             } else if constexpr (STRIDED) ask_span(x, XSIZE, j, to_x, x_edge);
-            else if (c0 + j * SPAN < a.cols) {
-#pragma unroll
-                for (int i = 0; i < XSIZE / 2; ++i) copy_async(to_x + (i * 32 + lane) * 16, x + (c0 + j * SPAN) * XSIZE + 16 * i, 16);
-            }
+            else ask_vectors(x, XSIZE, c, to_x);
         }
         copies_asked();
     };
@@ -393,7 +417,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) v[i] = f2(f[2 * i], f[2 * i + 1]);
         } else if constexpr (TYPE == SRC_F32) {
-            const float4 x = reinterpret_cast<const float4 *>(at)[lane], y = reinterpret_cast<const float4 *>(at)[32 + lane];
+            const float4 x = *reinterpret_cast<const float4 *>(at + fp32_read(lane, 0)), y = *reinterpret_cast<const float4 *>(at + fp32_read(lane, 1));
             v[0] = f2(x.x, x.y); v[1] = f2(x.z, x.w); v[2] = f2(y.x, y.y); v[3] = f2(y.z, y.w);
         } else if constexpr (TYPE == SRC_BF16) {
             const uint4 x = reinterpret_cast<const uint4 *>(at)[lane];
@@ -458,7 +482,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
             if (j == 1) copies_wait<STAGES * NV - 2>();
             if (j == 2) copies_wait<STAGES * NV - 3>();
             if (j == 3) copies_wait<STAGES * NV - 4>();
-            if (STRIDED || SRC == SRC_KEPT) __syncwarp();
+            if (SHARED) __syncwarp();
             if (first + j * SPAN >= a.cols) continue;
             F2 v[PAIRS], n[PAIRS], g[PAIRS];
             gamma(j, g);
@@ -484,7 +508,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
                 F2 v[PAIRS], n[PAIRS], g[PAIRS];
                 gamma(j, g);
                 values(j, v, n);
-                if (STRIDED || SRC == SRC_KEPT) __syncwarp();      // before another lane asks for the place again
+                if (SHARED) __syncwarp();      // before another lane asks for the place again
                 ask(row + STAGES * step, j, at);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[i] = fma2(n[i], mgn, fma2(v[i], g[i], mg)) * scale;
@@ -502,11 +526,10 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_backward_held_kernel(Nor
         at = at + 1 == STAGES ? 0 : at + 1;
     }
     copies_wait<0>();
-    const RowsOut to = {a.part + (long long)blockIdx.x * 2 * a.pitch, a.pitch, LRBI_Y_F32};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        store_chunk<STRIDED>(to, 0, c0 + j * SPAN, a.pitch, dgamma[j]);
-        store_chunk<STRIDED>(to, 1, c0 + j * SPAN, a.pitch, dbeta[j]);
+        store_part<STRIDED>(a, 0, c0 + j * SPAN, dgamma[j]);
+        store_part<STRIDED>(a, 1, c0 + j * SPAN, dbeta[j]);
     }
 }
 
@@ -611,8 +634,9 @@ Shape backward_shape(int cols, bool strided)
     const int spans = (cols + SPAN - 1) / SPAN, most = BACK_THREADS / 32, most_strided = BACK_THREADS_STRIDED / 32;
     if (strided && spans <= most_strided) return {32 * spans, most_strided / spans, 1, 1};
     if (spans <= most) return {32 * spans, most / spans, 1, 2};
-    if (spans <= 2 * most) return {32 * ((spans + 1) / 2), 1, 2, 1};
-    if (spans <= 4 * most) return {32 * ((spans + 3) / 4), 1, 4, 1};
+    if (spans <= 40) return {32 * ((spans + 1) / 2), 1, 2, 1};
+    if (spans <= 48) return {32 * ((spans + 2) / 3), 1, 3, 1};
+    if (spans <= 64) return {32 * ((spans + 3) / 4), 1, 4, 1};
     return {1024, 1, 0, 1};
 }
 
@@ -646,9 +670,10 @@ lrbi_status backward_launch(const NormBackward &a, const Shape &sh, int grid, cu
 {
     const bool f32 = a.dx.dtype == LRBI_Y_F32;
     if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s);
-    if (sh.chunks == 2)
-        if constexpr (STRIDED) return held_launch<DY, SRC, true, 2>(a, sh, grid, s);
-        else return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
+    if (sh.chunks == 2 && (STRIDED || sh.threads > BACK_THREADS)) return held_launch<DY, SRC, STRIDED, 2>(a, sh, grid, s);
+    if (sh.chunks == 3) return held_launch<DY, SRC, STRIDED, 3>(a, sh, grid, s);
+    if constexpr (!STRIDED)
+        if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
     if (sh.chunks == 4) return held_launch<DY, SRC, STRIDED, 4>(a, sh, grid, s);
     return norm_launch(norm_backward_wide_kernel<DY, SRC, STRIDED>, grid, dim3(1024), 0, s, a);
 }
@@ -666,9 +691,9 @@ lrbi_status launch_layer_norm_backward(const NormArgs &n, float *workspace, cuda
     const NormBackward a = {{n.dy, n.dy_stride}, {n.x, n.x_stride}, {n.dres, n.dres_stride}, {n.q, n.scale, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)},
                             make_params(n), n.mean, n.rstd, {n.dx, n.dx_stride, n.dx_dtype}, {n.y, n.y_stride, n.dy_dtype},
                             n.dx_dtype, workspace, n.rows, n.cols, pitch};
-    const bool strided = n.cols % CHUNK != 0 || !rows16(n.dy, n.dy_stride, n.dy_dtype) || (!n.q && !rows16(n.x, n.x_stride, n.x_dtype)) ||
-                       (n.dres && !rows16(n.dres, n.dres_stride, n.dx_dtype)) || !rows16(n.dx, n.dx_stride, n.dx_dtype) ||
-                       (n.y && !rows16(n.y, n.y_stride, n.dy_dtype));
+    const bool strided = n.cols % CHUNK != 0 || !vector_rows(n.dy, n.dy_stride, n.dy_dtype) || (!n.q && !vector_rows(n.x, n.x_stride, n.x_dtype)) ||
+                       (n.dres && !vector_rows(n.dres, n.dres_stride, n.dx_dtype)) || !vector_rows(n.dx, n.dx_stride, n.dx_dtype) ||
+                       (n.y && !vector_rows(n.y, n.y_stride, n.dy_dtype));
     const Shape sh = backward_shape(n.cols, strided);
     const int grid = backward_grid(n.rows, sh), src = n.q ? SRC_KEPT : n.x_dtype;
     lrbi_status st;

@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
     const int first = warp * a.each * SPAN, end = min(first + a.each * SPAN, a.cols), c = lane_column<STRIDED>(first, lane);
     long long row = (long long)blockIdx.x * blockDim.z + side;
     const long long step = (long long)gridDim.x * blockDim.z;
-    // then a place for each warp's part of the row to come.  Vector: [chunks][VECTORS][32].  Strided: the 16-byte vectors of
+    // then a place for each warp's part of the row to come.  Vector: [chunks][VECTORS][32] of 16 bytes.  Strided: the 16-byte vectors of
     // memory that lie in the part, at the same distance from a boundary; lanes hold the values before and after them until
     // the row's turn.
     const int place = a.each * VECTORS * 512 + (STRIDED ? 16 : 0);
@@ -103,13 +103,13 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
     auto ask = [&](long long r) {
         if (r < a.rows && first < end) {
             if constexpr (!STRIDED) {
-                const char *from = static_cast<const char *>(a.x.data) + (r * a.x.stride + c) * SIZE;
+                const char *from = static_cast<const char *>(a.x.data) + (r * a.x.stride + first) * SIZE + lane * 16;
+                const uint32_t to = ahead_at + (SIZE == 4 ? fp32_copied(lane) : lane * 16);
 #pragma unroll
                 for (int j = 0; j < K; ++j)
-                    if (c + j * SPAN < end) {
 #pragma unroll
-                        for (int i = 0; i < VECTORS; ++i) copy_async(ahead_at + ((j * VECTORS + i) * 32 + lane) * 16, from + j * SPAN * SIZE + 16 * i, 16);
-                    }
+                    for (int i = 0; i < VECTORS; ++i)
+                        if (first + j * SPAN + (i * 32 + lane) * 16 / SIZE < end) copy_async(to + (j * VECTORS + i) * 512, from + (j * VECTORS + i) * 512, 16);
             } else {
                 const char *p = static_cast<const char *>(a.x.data) + (r * a.x.stride + first) * SIZE;
                 const int bytes = (end - first) * SIZE, skip = (int)(-reinterpret_cast<intptr_t>(p) & 15), rest = skip + ((bytes - skip) & ~15);
@@ -151,11 +151,12 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             __syncwarp();
             x.load(ahead + move + lane * SIZE, c, first, end);
         } else {
+            if (SIZE == 4) __syncwarp();        // lanes read what others copied
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
                 for (int i = 0; i < VECTORS; ++i)
-                    x.put(j, i, c + j * SPAN < end ? *reinterpret_cast<const uint4 *>(ahead + ((j * VECTORS + i) * 32 + lane) * 16) : make_uint4(0, 0, 0, 0));
+                    x.put(j, i, c + j * SPAN < end ? *reinterpret_cast<const uint4 *>(ahead + j * VECTORS * 512 + (SIZE == 4 ? fp32_read(lane, i) : lane * 16)) : make_uint4(0, 0, 0, 0));
         }
         F2 v[PAIRS], t = f2(0.f);
 #pragma unroll
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             for (int i = 0; i < PAIRS; ++i) t = t + v[i];
         }
         float s[1] = {sum2(t)};       // all of the row is in registers
-        if (STRIDED) __syncwarp();
+        if (STRIDED || SIZE == 4) __syncwarp();
         ask(row + step);
         row_sums<1, WARPS>(s, part[side][0], lane, warp, warps, 1 + side);
         const float mean = s[0] * over;
@@ -409,7 +410,7 @@ lrbi_status launch_layer_norm(const NormArgs &n, cudaStream_t s)
 {
     const NormForward a = {{n.x, n.x_stride}, make_params(n), {n.y, n.y_stride, n.y_dtype},
                            {n.q_out, n.scale_out, checkpoint_pitch(n.cols), checkpoint_groups(n.cols)}, n.mean_out, n.rstd_out, n.eps, n.rows, n.cols, 1, 1, {{16, 0xFFFF0000u}, {16, 0xFFFF0000u}, {16, 0xFFFF0000u}, {16, 0xFFFF0000u}}};
-    const bool strided = n.cols % CHUNK != 0 || !rows16(n.x, n.x_stride, n.x_dtype) || !rows16(n.y, n.y_stride, n.y_dtype);
+    const bool strided = n.cols % CHUNK != 0 || !vector_rows(n.x, n.x_stride, n.x_dtype) || !vector_rows(n.y, n.y_stride, n.y_dtype);
     if (n.x_dtype == LRBI_Y_BF16) {
         if (n.y_dtype == LRBI_Y_BF16) return strided ? forward_launch<SRC_BF16, LRBI_Y_BF16, true>(a, s) : forward_launch<SRC_BF16, LRBI_Y_BF16, false>(a, s);
         return strided ? forward_launch<SRC_BF16, LRBI_Y_F32, true>(a, s) : forward_launch<SRC_BF16, LRBI_Y_F32, false>(a, s);

@@ -2,8 +2,8 @@
 // load and store them in 16 or 32 bits, and keep them in 8 bits.
 //
 // A warp takes 256 columns at a time (a span), 8 a lane (a chunk), in one of two ways:
-//   vector    a lane has 8 neighbouring columns: one 16-byte access in bf16, two in fp32.  For rows that start on 16-byte
-//             boundaries and hold a multiple of 8 columns.
+//   vector    a lane has 8 neighbouring columns: one access of 16 bytes in bf16, of 32 in fp32.  For rows that start on
+//             boundaries of that many bytes and hold a multiple of 8 columns.
 //   strided   a lane has columns lane, lane + 32, ..: any alignment and any width; an access of the warp is 64 or 128
 //             neighbouring bytes.  (Aligned vectors moved into place by shuffles and funnel shifts were built too: 35
 //             instructions a value in the layer norm against 9.)
@@ -38,6 +38,16 @@ __device__ __forceinline__ uint4 ld_once16(const void *p)   // read once: does n
     uint4 v;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
+}
+// 32 bytes at once: in two accesses of 16 every 32-byte sector is asked for twice (layer norm 8192 x 4096 fp32, QQQ).
+__device__ __forceinline__ void ld_once32(const void *p, uint32_t (&w)[8])
+{
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+__device__ __forceinline__ void st32(void *p, const float (&f)[8])
+{
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
 }
 __device__ __forceinline__ uint2 ld_once8(const void *p)
 {
@@ -109,13 +119,13 @@ struct Raw {
     // span is there (nothing is checked).
     __device__ __forceinline__ void load_at(const char *p, int left, bool whole = false)
     {
-        if constexpr (!STRIDED) {
-#pragma unroll
-            for (int i = 0; i < WORDS / 4; ++i) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (left > 0) v = ld_once16(p + 16 * i);
-                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-            }
+        if constexpr (!STRIDED && SIZE == 4) {
+            clear();
+            if (left > 0) ld_once32(p, w);
+        } else if constexpr (!STRIDED) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (left > 0) v = ld_once16(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
         } else {
             if (whole) {
 #pragma unroll
@@ -237,6 +247,11 @@ __device__ __forceinline__ void copy_async_some(uint32_t to, const void *from, i
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
+// A span of fp32 vectors goes over in two accesses of 512 neighbouring bytes: a lane copies 16 bytes of either (from its byte
+// 512 i + 16 lane) and reads its own 32 bytes after the warp's copies are there.  Vectors are placed so that neither has bank
+// conflicts: copies at fp32_copied(lane) + 512 i, read at fp32_read(lane, i).
+__device__ __forceinline__ int fp32_copied(int lane) { return (lane ^ (lane >> 3 & 1)) * 16; }
+__device__ __forceinline__ int fp32_read(int lane, int i) { return lane * 32 + (i ^ (lane >> 2 & 1)) * 16; }
 __device__ __forceinline__ void copies_asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>   // all but the last LEFT groups are there
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
@@ -268,10 +283,8 @@ __device__ __forceinline__ void store_at(char *p, int left, const F2 (&v)[PAIRS]
         float f[CHUNK];
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
-        if (SIZE == 4) {
-            *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
-            *reinterpret_cast<float4 *>(p + 16) = make_float4(f[4], f[5], f[6], f[7]);
-        } else
+        if (SIZE == 4) st32(p, f);
+        else
             *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     }
 }
@@ -396,10 +409,10 @@ lrbi_status launch_kernel(K kernel, dim3 grid, dim3 block, size_t smem, cudaStre
 }
 
 // Host side: whether rows are whole vectors.
-inline bool rows16(const void *p, long long stride, int dtype)
+inline bool vector_rows(const void *p, long long stride, int dtype)
 {
-    const long long bytes = dtype == LRBI_Y_F32 ? 4 : 2;
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (stride * bytes & 15) == 0;
+    const long long size = dtype == LRBI_Y_F32 ? 4 : 2, vector = CHUNK * size;
+    return reinterpret_cast<uintptr_t>(p) % vector == 0 && stride * size % vector == 0;
 }
 
 }  // namespace lrbi

@@ -72,6 +72,8 @@ NORM_SHAPES = [
     (1, 1, 0), (5, 2, 3), (3, 7, 1), (9, 8, 0), (1, 255, 0), (17, 256, 8), (33, 257, 0), (2, 264, 0), (7, 801, 6), (4, 1000, 8),
     (3, 2049, 5), (1, 4096, 0), (600, 512, 0), (5, 8192, 0), (3, 8193, 0), (2, 8200, 0), (3, 12345, 1), (2, 16384, 8), (2, 16385, 0),
     (2, 20000, 0), (300, 129, 2),
+    # several rows a block, of the widths at which the backward pass takes another form
+    (310, 5123, 3), (450, 8193, 1), (300, 8456, 0), (300, 10248, 8), (310, 10753, 7), (450, 16383, 2), (300, 4104, 8),
 ]
 
 
