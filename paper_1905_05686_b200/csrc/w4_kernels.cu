@@ -54,6 +54,13 @@ __device__ __forceinline__ void copy_async32(uint32_t to, const void *from, bool
                  ::"r"(to), "l"(from), "r"((uint32_t)on) : "memory");
 }
 
+__device__ __forceinline__ void copy_activations(uint32_t to, const uint16_t *from, bool on)     // four pieces, 64 bytes apart, to places 512 bytes apart
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q cp.async.cg.shared.global [%0], [%1], 16;\n\t@q cp.async.cg.shared.global [%0+512], [%1+64], 16;\n\t"
+                 "@q cp.async.cg.shared.global [%0+1024], [%1+128], 16;\n\t@q cp.async.cg.shared.global [%0+1536], [%1+192], 16;\n\t}"
+                 ::"r"(to), "l"(from), "r"((uint32_t)on) : "memory");
+}
+
 // Activations of a batch row that a lane needs for a unit: columns c .. c + 7 and c + 32 .. c + 39 (zeros past the last
 // column and for rows past the batch).
 template <bool VEC>
@@ -112,16 +119,22 @@ __device__ __forceinline__ void store(const W4 &w, void *Y, int y_dtype, int o, 
     else static_cast<uint16_t *>(Y)[to] = (uint16_t)pack_bf16(v, 0.f);
 }
 
+// Whether the activations go through the ring too, how many steps it has room for, and the bytes of one.
+template <int NT, int TILES, bool VEC> constexpr bool W4_X_RING = VEC && NT == 1 && TILES == 1;
+template <int NT, int TILES, bool VEC> constexpr int W4_DEPTH = TILES == 1 && !W4_X_RING<NT, TILES, VEC> ? 4 : 3;
+template <int GROUP, int NT, int TILES, bool VEC> constexpr int W4_SLOT = TILES * (1024 + W4_STEP / GROUP * 64) + (W4_X_RING<NT, TILES, VEC> ? 2048 : 0);
+
 // `sharing` warps of a block (and of each block of a cluster) take TILES * 16 rows: the columns in turn, in steps of 128, and
 // add up in shared memory, block by block and then over the cluster, in a fixed order that depends on the layer alone.  A step's weights come through a ring
 // of asynchronous copies, the activations a step ahead in registers.  NT: tiles of 8 batch rows.
 template <int GROUP, int NT, int TILES, bool VEC>
-__global__ void __launch_bounds__(32 * W4_WARPS, NT == 1 && TILES == 1 ? 4 : 2) w4_gemv_kernel(W4 w, const uint16_t *__restrict__ X, int batch, void *__restrict__ Y, int y_dtype, int sharing)
+__global__ void __launch_bounds__(32 * W4_WARPS, NT > 1 || TILES > 1 ? 2 : VEC ? 3 : 4) w4_gemv_kernel(W4 w, const uint16_t *__restrict__ X, int batch, void *__restrict__ Y, int y_dtype, int sharing)
 {
     begin();
     constexpr int PER = W4_STEP / GROUP, IN_UNIT = GROUP >= 64 ? 1 : 64 / GROUP, MMAS = 4 / IN_UNIT;   // groups of a step, of a unit; products of a group in a unit
-    constexpr int DEPTH = TILES == 1 ? 4 : 3;                         // steps under way, with the one that is worked on
-    constexpr int TILE = 1024 + PER * 64, SLOT = TILES * TILE;        // bytes of a step: weights, then scales and zero points, of each tile
+    constexpr bool X_RING = W4_X_RING<NT, TILES, VEC>;
+    constexpr int DEPTH = W4_DEPTH<NT, TILES, VEC>;                   // steps under way, with the one that is worked on
+    constexpr int TILE = 1024 + PER * 64, SLOT = W4_SLOT<GROUP, NT, TILES, VEC>;     // bytes of a step: weights, then scales and zero points, of each tile; activations
     extern __shared__ __align__(16) char ring[];                      // [W4_WARPS][DEPTH][SLOT]
     __shared__ float4 part[W4_WARPS][TILES][NT][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -147,6 +160,10 @@ __global__ void __launch_bounds__(32 * W4_WARPS, NT == 1 && TILES == 1 ? 4 : 2) 
             const uint32_t to = slots_lane + at * SLOT + r * TILE;
             copy_async32(to, packed + r * packed_tile, on && (r == 0 || two));
             copy_async16(to + 1024, meta + r * meta_tile, on && (r == 0 || two) && lane < PER * 4);
+        }
+        if (X_RING) {
+            copy_activations(slots_lane + at * SLOT + TILES * TILE, from, on && g < left);
+            from += stride * W4_STEP;
         }
         copies_asked();
         asked += stride;
@@ -218,9 +235,13 @@ __global__ void __launch_bounds__(32 * W4_WARPS, NT == 1 && TILES == 1 ? 4 : 2) 
         }
         }
     };
+    if (X_RING && g >= left) {              // rows past the batch
+#pragma unroll
+        for (int i = 0; i < DEPTH * 4; ++i) *reinterpret_cast<uint4 *>(slots + i / 4 * SLOT + TILES * TILE + i % 4 * 512 + lane * 16) = make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
     for (int i = 0; i < DEPTH - 1; ++i) ask(i);
-    activations(step);
+    if (!X_RING) activations(step);
     while (step < whole) {
 #pragma unroll
         for (int at = 0; at < DEPTH; ++at) {
@@ -228,9 +249,17 @@ __global__ void __launch_bounds__(32 * W4_WARPS, NT == 1 && TILES == 1 ? 4 : 2) 
             ask((at + DEPTH - 1) % DEPTH);
             copies_wait<DEPTH - 1>();
             __syncwarp();                   // scales and zero points were copied by other lanes
+            if (X_RING) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(slots + at * SLOT + TILES * TILE + i * 512 + lane * 16);
+                    uint32_t *to = x[i / 2][0] + i % 2 * 4;
+                    to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
+                }
+            }
             products(slots + at * SLOT, std::true_type());
             step += stride;
-            activations(step);
+            if (!X_RING) activations(step);
             __syncwarp();                   // before the place is asked for again
         }
     }
@@ -378,7 +407,7 @@ lrbi_status gemv_launch(const W4 &w, const uint16_t *X, int batch, void *Y, int 
 {
     const Cut cut = gemv_cut(w);
     const int rows = 16 * TILES * (W4_WARPS / cut.sharing), split = cut.split;      // of a block
-    constexpr size_t smem = (size_t)W4_WARPS * (TILES == 1 ? 4 : 3) * TILES * (1024 + W4_STEP / GROUP * 64);
+    constexpr size_t smem = (size_t)W4_WARPS * W4_DEPTH<NT, TILES, VEC> * W4_SLOT<GROUP, NT, TILES, VEC>;
     return launch_kernel(w4_gemv_kernel<GROUP, NT, TILES, VEC>, dim3((w.rows + rows - 1) / rows * split, (batch + 8 * NT - 1) / (8 * NT)), dim3(32 * W4_WARPS), smem, s,
                          split, w, X, batch, Y, y_dtype, cut.sharing);
 }
