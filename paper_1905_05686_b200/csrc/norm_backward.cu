@@ -94,29 +94,26 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
     const int chunk_bytes = (DBYTES + XBYTES) * threads, round_bytes = R * NV * chunk_bytes;
     auto ask = [&](uint32_t first, int at) {    // vector rows
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) {
+            const bool there = first + r < rows;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (first + r < rows && j * apart < left) {
-                    const char *d = dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, *x = x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE;
-                    const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes, to_x = to + DBYTES * threads;
-                    if (DSIZE == 2) copy_async(to + me * 16, d, 16);
-                    if (SRC == SRC_BF16) copy_async(to_x + me * 16, x, 16);
-                    if (SRC == SRC_KEPT && (me & 1) == 0) copy_async(to_x + me * 8, x, 16);       // a vector for two threads; rows of the copy are whole vectors
+            for (int j = 0; j < NV; ++j) {
+                const bool on = there && j * apart < left;
+                const char *d = dy0 + (uint64_t)(first + r) * dy_row + j * apart * DSIZE, *x = x0 + (uint64_t)(first + r) * x_row + j * apart * XSIZE;
+                const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes, to_x = to + DBYTES * threads;
+                if (DSIZE == 2) copy_async_if(on, to + me * 16, d);
+                if (SRC == SRC_BF16) copy_async_if(on, to_x + me * 16, x);
+                if (SRC == SRC_KEPT) copy_async_if(on && (me & 1) == 0, to_x + me * 8, x);       // a vector for two threads; rows of the copy are whole vectors
+                if constexpr (DSIZE == 4 || SRC == SRC_F32) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int c = warp * SPAN + j * apart + i * 128 + lane * 4;
+                        const uint32_t mine = (me >> 5) * 1024 + i * 512 + fp32_copied(lane);
+                        if (DSIZE == 4) copy_async_if(there && c < a.cols, to + mine, static_cast<const char *>(a.dy.data) + (uint64_t)(first + r) * dy_row + c * 4);
+                        if (SRC == SRC_F32) copy_async_if(there && c < a.cols, to_x + mine, static_cast<const char *>(a.x.data) + (uint64_t)(first + r) * x_row + c * 4);
+                    }
                 }
-        if constexpr (DSIZE == 4 || SRC == SRC_F32) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (first + r < rows && j * apart + i * 128 + lane * 4 < warp_left) {
-                            const int c = warp * SPAN + j * apart + i * 128 + lane * 4;
-                            const uint32_t to = ring0 + at * round_bytes + (r * NV + j) * chunk_bytes + (me >> 5) * 1024 + i * 512 + fp32_copied(lane);
-                            if (DSIZE == 4) copy_async(to, static_cast<const char *>(a.dy.data) + (uint64_t)(first + r) * dy_row + c * 4, 16);
-                            if (SRC == SRC_F32) copy_async(to + DBYTES * threads, static_cast<const char *>(a.x.data) + (uint64_t)(first + r) * x_row + c * 4, 16);
-                        }
+            }
         }
         copies_asked();
     };

@@ -243,6 +243,10 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void *from, int by
     else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copy_async_if(bool on, uint32_t to, const void *from)      // 16 bytes; a predicate, not a branch
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(to), "l"(from), "r"((uint32_t)on) : "memory");
+}
 __device__ __forceinline__ void copy_async_some(uint32_t to, const void *from, int bytes)   // 1 to 16, and zeros up to 16
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
