@@ -55,8 +55,12 @@ constexpr int BACK_THREADS = 512, BACK_THREADS_STRIDED = 640;
 
 // blockDim = (threads of a row, rows side by side).  A thread has NV chunks of R rows at a time and keeps its columns' sums
 // and their gamma in registers.  Vector rows come through a ring of STAGES rounds in shared memory, each thread copying what
-// it reads itself; strided rows are loaded into registers a round ahead.  What is left to bound it is the number of
-// instructions a value: addresses are one multiply-add each, and rounds that are whole check nothing.
+// it reads itself; strided rows are loaded into registers a round ahead.
+//
+// Bound: memory on paper; half of the issue slots are taken (18 to 20 instructions a value, of which 7 are the sums and the
+// result), and every round waits for its slowest warp once.  16384 x 4096: bf16 73 us (floor 61.5), from the 8-bit copy 80
+// (51.6), with the residual and the restored forward result 116 (92.6); 8192 x 4096 fp32 66 (61.5); 8192 x 4097 bf16, where
+// every access is of one value, 70 (30.8).  Addresses are one multiply-add each, and rounds that are whole check nothing.
 template <int DY, int SRC, int OUT, bool STRIDED, bool EXTRA, int NV, int R>
 __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BACK_THREADS, 1) norm_backward_kernel(NormBackward a)
 {
@@ -217,7 +221,7 @@ __global__ void __launch_bounds__(STRIDED && NV == 1 ? BACK_THREADS_STRIDED : BA
             both[2 * r + 1] = sum2(sgn);
         }
         if constexpr (AHEAD) load(row + step);
-        Raw<OUT, STRIDED> res[EXTRA && !STRIDED ? R * NV : 1];          // the residual's gradient, under way during the sums
+        [[maybe_unused]] Raw<OUT, STRIDED> res[EXTRA && !STRIDED ? R * NV : 1];          // the residual's gradient, under way during the sums
         if constexpr (EXTRA && !STRIDED) {
             if (a.dres.data) {
 #pragma unroll
@@ -320,7 +324,8 @@ constexpr int HELD_STAGES = DY == SRC_F32 || SRC == SRC_F32 ? 1 : 2;
 // the next row (32 bits, which fill the memory) as soon as its second reading is through, so that copies are always under way.
 // Warps have neighbouring chunks.  Strided: the 16-byte vectors of memory that hold a warp's chunk are copied, at the same
 // distance from a boundary; vectors that begin before the row are not, and lanes hold the values in them until the row's turn.
-// 4000 x 16384: bf16 100 us, with the values read twice from memory 139; fp32 WWW and 309; 16383 columns ZZZ and 374.
+// 4000 x 16384 bf16: 100 us (floor 60), with the values read twice from memory 139; 16383 columns: 176 and 374; 2000 x 16384
+// fp32: 88 and 154.  What is left: with 16 warps of 128 registers, reading and unpacking each value twice.
 template <int DY, int SRC, bool STRIDED, bool EXTRA, int NV>
 __global__ void __launch_bounds__(HELD_THREADS<NV>, 1) norm_backward_held_kernel(NormBackward a)
 {
@@ -626,6 +631,10 @@ namespace {
 
 struct Shape { int threads, side, chunks, at_a_time; };   // threads of a row, rows side by side, chunks of a thread (0: wide), R
 
+// As few chunks a thread as 16 warps of 128 registers (20 of 96 with two chunks, or strided rows of one) have room for.
+// 7000 x 9216: two chunks and 18 warps 103 us, four chunks and 9 warps 120.  Beyond 512 threads of two chunks, and from three
+// on, the values stay in shared memory (norm_backward_held_kernel); strided rows of two chunks are faster out of registers:
+// 8000 x 8191 bf16 152 us, through shared memory 177.
 Shape backward_shape(int cols, bool strided)
 {
     const int spans = (cols + SPAN - 1) / SPAN, most = BACK_THREADS / 32, most_strided = BACK_THREADS_STRIDED / 32;
@@ -667,10 +676,9 @@ lrbi_status backward_launch(const NormBackward &a, const Shape &sh, int grid, cu
 {
     const bool f32 = a.dx.dtype == LRBI_Y_F32;
     if (sh.chunks == 1) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 1, STRIDED ? 1 : 2>(a, sh, grid, s);
-    if (sh.chunks == 2 && (STRIDED || sh.threads > BACK_THREADS)) return held_launch<DY, SRC, STRIDED, 2>(a, sh, grid, s);
+    if (sh.chunks == 2 && sh.threads > BACK_THREADS) return held_launch<DY, SRC, STRIDED, 2>(a, sh, grid, s);
     if (sh.chunks == 3) return held_launch<DY, SRC, STRIDED, 3>(a, sh, grid, s);
-    if constexpr (!STRIDED)
-        if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
+    if (sh.chunks == 2) return f32 ? ring_launch<DY, SRC, LRBI_Y_F32, STRIDED, 2, 1>(a, sh, grid, s) : ring_launch<DY, SRC, LRBI_Y_BF16, STRIDED, 2, 1>(a, sh, grid, s);
     if (sh.chunks == 4) return held_launch<DY, SRC, STRIDED, 4>(a, sh, grid, s);
     return norm_launch(norm_backward_wide_kernel<DY, SRC, STRIDED>, grid, dim3(1024), 0, s, a);
 }

@@ -8,7 +8,7 @@
 //   tall  many rows.  A warp has a row, or `warps` of them share one; a lane holds up to 16 chunks (bf16; 8 in fp32), the
 //         sums' shuffles are paid once per row, gamma and beta come from shared memory without bank conflicts, and warps
 //         run apart from one another, so that loads, arithmetic and stores of different rows overlap.
-//   row   few rows (less than two rows a warp for the whole GPU): latency counts, a block has a row, a lane one or two chunks.
+//   row   few rows: latency counts, a block has a row, a lane one or two chunks.
 //   wide  rows beyond the registers of a block: read three times, mostly from L2.
 #include <algorithm>
 #include <atomic>
@@ -366,7 +366,7 @@ lrbi_status tall_kernel_launch(const NormForward &a, cudaStream_t s)
     auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, COPY, K>;
     const long long most = NORM_SMS * blocks_per_sm(kernel, 32 * block.y * block.z, smem);
     // Rows go in rounds over all blocks: the same number of rounds with the fewest rows a block, so that the last is not
-    // nearly empty (4096 x 4096: 3 rounds of 6 rows a block, the last a third full, XX us; of 5 rows, YY us).
+    // nearly empty (4096 x 4096: 3 rounds of 6 rows a block, the last a third full, 18.0 us; of 5 rows, 16.8 us).
     const long long rounds = ((long long)a.rows + most * block.z - 1) / (most * block.z);
     block.z = (unsigned)std::max(1LL, ((long long)a.rows + most * rounds - 1) / (most * rounds));
     const long long need = ((long long)a.rows + block.z - 1) / block.z;
@@ -388,8 +388,10 @@ lrbi_status forward_launch(NormForward a, cudaStream_t s)
     // share more of an SM's memory between fewer blocks, and there 16 are better: 4000 x 16384 in 55 us (8: 69).
     const int most = TWO && spans > 32 ? 16 : 8;
     a.warps = (spans + most - 1) / most;
-    // Few rows leave most of the GPU idle with a warp each: then a block takes one.
-    const bool few = (long long)a.rows * a.warps < 4 * NORM_SMS;
+    // Few rows leave most of the GPU idle with a warp each, and the parameters' way into shared memory is a good part of the
+    // time: then a block takes a row.  Rows of two warps: 300 x 4096 3.9 us (a warp or two: 7.2), 700 6.4 (8.2), 900 8.1 (8.5),
+    // 1300 9.7 (8.6); of one: 590 x 1024 2.5 (2.8), 1200 3.7 (4.0), 1500 x 1157 6.6 (5.7), 2000 x 1024 5.4 (4.4).
+    const bool few = (long long)a.rows * a.warps < (a.warps > 1 ? 12 : 8) * NORM_SMS;
     if (spans > 64) return norm_launch(norm_forward_wide_kernel<SRC, STRIDED>, a.rows, dim3(1024), 0, s, a);
     if (few) {
         if (spans <= 32) return norm_launch(norm_forward_row_kernel<SRC, STRIDED, 1>, a.rows, dim3(32 * spans), 0, s, a);

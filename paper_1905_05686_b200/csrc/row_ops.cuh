@@ -39,7 +39,8 @@ __device__ __forceinline__ uint4 ld_once16(const void *p)   // read once: does n
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
-// 32 bytes at once: in two accesses of 16 every 32-byte sector is asked for twice (layer norm 8192 x 4096 fp32, QQQ).
+// 32 bytes at once: in two accesses of 16 every 32-byte sector is asked for twice (fp32, 8192 x 4096, with the rings below:
+// layer norm 70 us, now 51; its backward 116, now 66).
 __device__ __forceinline__ void ld_once32(const void *p, uint32_t (&w)[8])
 {
     asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"

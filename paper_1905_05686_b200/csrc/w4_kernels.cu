@@ -119,14 +119,20 @@ __device__ __forceinline__ void store(const W4 &w, void *Y, int y_dtype, int o, 
     else static_cast<uint16_t *>(Y)[to] = (uint16_t)pack_bf16(v, 0.f);
 }
 
-// Whether the activations go through the ring too, how many steps it has room for, and the bytes of one.
+// Whether the activations go through the ring too (one tile a warp: 4096 x 9216 7.7 -> 7.4 us; two tiles hide the loads of
+// registers themselves and lose by it: 16384 x 4096, eight rows, 11.9 -> 13.1), how many steps it has room for, and the bytes of one.
 template <int NT, int TILES, bool VEC> constexpr bool W4_X_RING = VEC && NT == 1 && TILES == 1;
 template <int NT, int TILES, bool VEC> constexpr int W4_DEPTH = TILES == 1 && !W4_X_RING<NT, TILES, VEC> ? 4 : 3;
 template <int GROUP, int NT, int TILES, bool VEC> constexpr int W4_SLOT = TILES * (1024 + W4_STEP / GROUP * 64) + (W4_X_RING<NT, TILES, VEC> ? 2048 : 0);
 
 // `sharing` warps of a block (and of each block of a cluster) take TILES * 16 rows: the columns in turn, in steps of 128, and
-// add up in shared memory, block by block and then over the cluster, in a fixed order that depends on the layer alone.  A step's weights come through a ring
-// of asynchronous copies, the activations a step ahead in registers.  NT: tiles of 8 batch rows.
+// add up in shared memory, block by block and then over the cluster, in a fixed order that depends on the layer alone.  A step's
+// weights come through a ring of asynchronous copies, the activations too or a step ahead in registers.  NT: tiles of 8 batch rows.
+//
+// Bound: on paper the weights' bytes (16384 x 16384, one row: 21.5 us).  Measured 33.7 us, and 30.0 with every load taken out:
+// turning four bits into bf16 takes a shift, a logic operation and a subtraction for two weights, and the logic pipe issues
+// every second cycle.  (Leaving the 128 + z in and taking it out of the sums would save the subtraction, and pruned weights
+// would no longer be exact zeros.)  The smaller layers add about 2 us of launch and first latency.
 template <int GROUP, int NT, int TILES, bool VEC>
 __global__ void __launch_bounds__(32 * W4_WARPS, NT > 1 || TILES > 1 ? 2 : VEC ? 3 : 4) w4_gemv_kernel(W4 w, const uint16_t *__restrict__ X, int batch, void *__restrict__ Y, int y_dtype, int sharing)
 {
@@ -391,21 +397,29 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(Geo geo, const uint16_
 
 namespace {
 
-// How a layer is cut: warps of a block that share a tile, and blocks that do.
+// How a layer is cut: warps of a block that share a tile, and blocks (of a cluster) that do.
 struct Cut { int sharing, split; };
-Cut gemv_cut(const W4 &w)
+Cut gemv_cut(const W4 &w, int at_once)      // at_once: tiles of a warp
 {
+    constexpr int SMS = 148;
     const int tiles = (w.rows + 15) / 16, steps = (w.units + 1) / 2;
+    auto blocks = [&](int sharing) { const int each = at_once * (W4_WARPS / sharing); return (tiles + each - 1) / each; };
+    auto most = [&](int sharing) { return (blocks(sharing) + SMS - 1) / SMS * at_once * (W4_WARPS / sharing); };      // tiles of the SM that has the most
     Cut c = {W4_WARPS, 1};
-    while (c.sharing > 1 && tiles * c.sharing > 4736) c.sharing /= 2;
-    while (c.split < 8 && tiles * c.split < 148 && steps >= 2 * c.split * W4_WARPS) c.split *= 2;
+    // Fewer warps share a tile, and each has more steps of it, as long as the SMs have two blocks or more and the one that has
+    // the most tiles hardly more of them.  16384 x 4096: 4 warps 11.1 us, 8 or 2 12.8; 12000 x 9216 (with 4, a few SMs have two
+    // blocks and most one): 8 warps 17.1, 4 19.7; 8192 x 8192, eight rows: 8 warps 11.5, 4 16.8.
+    while (c.sharing > 1 && blocks(c.sharing / 2) > SMS && most(c.sharing / 2) * 7 <= most(c.sharing) * 8) c.sharing /= 2;
+    // Layers of few tiles: blocks share one, while a warp has four steps or more.  64 x 16384: 8 blocks 3.3 us, 4 3.8, 2 4.9;
+    // 1024 x 4096: 1 block 3.1, 2 3.3, 4 3.8; 1024 x 8192: 1 4.7, 2 4.4, 4 4.4.
+    while (c.split < 8 && tiles * c.split < SMS && steps >= 4 * c.split * W4_WARPS) c.split *= 2;
     return c;
 }
 
 template <int GROUP, int NT, int TILES, bool VEC>
 lrbi_status gemv_launch(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, cudaStream_t s)
 {
-    const Cut cut = gemv_cut(w);
+    const Cut cut = gemv_cut(w, TILES);
     const int rows = 16 * TILES * (W4_WARPS / cut.sharing), split = cut.split;      // of a block
     constexpr size_t smem = (size_t)W4_WARPS * W4_DEPTH<NT, TILES, VEC> * W4_SLOT<GROUP, NT, TILES, VEC>;
     return launch_kernel(w4_gemv_kernel<GROUP, NT, TILES, VEC>, dim3((w.rows + rows - 1) / rows * split, (batch + 8 * NT - 1) / (8 * NT)), dim3(32 * W4_WARPS), smem, s,
@@ -415,7 +429,9 @@ lrbi_status gemv_launch(const W4 &w, const uint16_t *X, int batch, void *Y, int 
 template <int GROUP, int NT>
 lrbi_status gemv_tiles(const W4 &w, const uint16_t *X, int batch, void *Y, int y_dtype, bool vec, cudaStream_t s)
 {
-    if ((w.rows + 15) / 16 >= 512)
+    // Two tiles a warp share what is loaded of the activations, where every SM still has a block.  6000 x 4096, eight rows:
+    // 7.6 us, one tile 8.3; 5000 x 9216, sixteen rows: 16.1 and 18.4; with 4500 rows there are 141 blocks: 6.0 and 4.9.
+    if ((w.rows + 15) / 16 >= 2 * 148)
         return vec ? gemv_launch<GROUP, NT, 2, true>(w, X, batch, Y, y_dtype, s) : gemv_launch<GROUP, NT, 2, false>(w, X, batch, Y, y_dtype, s);
     return vec ? gemv_launch<GROUP, NT, 1, true>(w, X, batch, Y, y_dtype, s) : gemv_launch<GROUP, NT, 1, false>(w, X, batch, Y, y_dtype, s);
 }
