@@ -164,6 +164,62 @@ def test_layer_norm_of_no_rows():
     assert dx.shape == (0, 40) and not dgamma.any() and not dbeta.any() and dgamma.numel() == 40
 
 
+@pytest.mark.parametrize("cols", [8, 801, 4096, 5121, 8200, 9000, 10241, 16383, 16384, 20000])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_no_rows_of_any_width(cols, dtype):
+    b = _b()
+    x = torch.empty((0, cols), dtype=dtype, device="cuda")
+    gamma = torch.ones(cols, device="cuda")
+    y, m, r, kept = b.lrbi_layer_norm(x, gamma, checkpoint=True)
+    for src in (x, kept):
+        dx, dgamma, dbeta = b.lrbi_layer_norm_backward(x, src, gamma, m, r)
+        assert y.shape == dx.shape == (0, cols) and not dgamma.any() and not dbeta.any()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("cols", [256, 4096, 9000, 16384])
+@pytest.mark.parametrize("pad,off", [(4, 0), (0, 4), (8, 4), (4, 4), (0, 1)])
+def test_fp32_rows_at_any_distance_from_a_vector(cols, pad, off):
+    """Rows that start on 16-byte boundaries alone, or on none: right, and elementwise results with the bits of packed rows."""
+    b = _b()
+    rows = 5
+    base = torch.randn(rows * (cols + pad) + off, device="cuda", generator=torch.Generator("cuda").manual_seed(cols + pad))
+    x = torch.as_strided(base, (rows, cols), (cols + pad, 1), off)
+    gamma, beta = matrix(1, cols, F32, 0, 1)[0], matrix(1, cols, F32, 0, 2)[0]
+    y, m, r = b.lrbi_layer_norm(x, gamma, beta)
+    want, mean, rstd, n = norm64(np64(x), np64(gamma), np64(beta), 1e-5)
+    top = np.abs(np64(x)).max(1, keepdims=True)
+    off64 = TOL * ((top * rstd + np.abs(n) * (1 + (top * rstd) ** 2)) * np.abs(np64(gamma)) + np.abs(want) + np.abs(np64(beta)))
+    assert (np.abs(np64(y) - want) <= off64).all()
+    own = x.contiguous()
+    a, kept = b.lrbi_activation(x, "gelu", checkpoint=True)
+    a1, kept1 = b.lrbi_activation(own, "gelu", checkpoint=True)
+    assert torch.equal(a, a1) and torch.equal(kept.q, kept1.q) and torch.equal(kept.scale, kept1.scale)
+    assert torch.equal(b.lrbi_activation_backward(x, x, "gelu"), b.lrbi_activation_backward(own, own, "gelu"))
+    assert torch.equal(b.lrbi_checkpoint_store(x).q, b.lrbi_checkpoint_store(own).q)
+
+
+@pytest.mark.parametrize("cols", [800, 801, 9000, 16383])
+def test_offsets_past_32_bits(cols):
+    """Rows so far apart that the last begin beyond 2^32 bytes: the same bits as side by side."""
+    b = _b()
+    rows, stride = 18, (1 << 27) - 8
+    base = torch.empty(rows * stride, dtype=BF16, device="cuda")
+    x = torch.as_strided(base, (rows, cols), (stride, 1))
+    own = matrix(rows, cols, BF16, 0, 3)
+    x.copy_(own)
+    gamma = matrix(1, cols, F32, 0, 1)[0]
+    far, near = b.lrbi_layer_norm(x, gamma, checkpoint=True), b.lrbi_layer_norm(own, gamma, checkpoint=True)
+    same = [(far[i], near[i]) for i in range(3)] + [(far[3].q, near[3].q)]
+    back = [b.lrbi_layer_norm_backward(t, t, gamma, near[1], near[2]) for t in (x, own)]
+    act = [b.lrbi_activation(t, "silu", checkpoint=True) for t in (x, own)]
+    dact = [b.lrbi_activation_backward(t, k, "silu", restore=True) for t, (_, k) in zip((x, own), act)]
+    same += list(zip(*back)) + [(act[0][0], act[1][0]), (act[0][1].q, act[1][1].q)] + list(zip(*dact))
+    for u, v in same:
+        assert torch.equal(u, v)
+    assert not torch.isnan(near[0]).any()
+
+
 def test_layer_norm_of_equal_values_and_far_offsets():
     """Variance 0 leaves beta and finite gradients; an offset of 2^12 times the spread does not cancel in the variance."""
     b = _b()
