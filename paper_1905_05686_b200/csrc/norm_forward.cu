@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             params[(q * 4 + which * 2 + 1) * 32 + lane] = make_float4(f[4], f[5], f[6], f[7]);
         }
     }
-    __syncthreads();
+    bool set = false;       // the parameters are waited for when the first result needs them
     const float over = 1.f / (float)a.cols;
     const float4 *own = params + warp * a.each * 4 * 32;
     for (; row < a.rows; row += step) {
@@ -192,6 +192,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
         row_sums<1, WARPS>(s, part[side][1], lane, warp, warps, 1 + side);
         const float rstd = inverse_root(fmaf(s[0], over, a.eps));
         if (a.mean && lane == 0 && warp == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+        if (!set) { __syncthreads(); set = true; }
         constexpr int YSIZE = OUT == LRBI_Y_F32 ? 4 : 2;
         char *y = static_cast<char *>(a.y.data) + (row * a.y.stride + c) * YSIZE;
         if constexpr (COPY) {
@@ -235,6 +236,7 @@ __global__ void __launch_bounds__(32 * Tall<SRC, STRIDED, K>::WARPS, Tall<SRC, S
             }
         }
     }
+    if (!set) __syncthreads();
     copies_wait<0>();
 }
 
