@@ -12,7 +12,7 @@
 //   wide  rows beyond the registers of a block: read three times, mostly from L2.
 //
 // Bound, tall: memory and issue about alike (10 instructions a value in bf16).  16384 x 4096 bf16 47.5 us (floor 41), with the
-// copy 61 (51.6); 4096 x 4096 15.8 (10.3): three rounds of rows and 5 us to begin and to drain; 8192 x 4096 fp32 51 (41); 8192 x
+// copy 61 (51.6); 4096 x 4096 14.9 (10.3): three rounds of rows and 4 us to begin and to drain; 8192 x 4096 fp32 51 (41); 8192 x
 // 4097 bf16, an access a value, 47.6 (20.5).  row: 2.3 us for one token of 4096, which is the launch, two waits for memory and
 // two sums over a block.
 #include <algorithm>
@@ -78,11 +78,12 @@ struct Part {
     }
 };
 
-// Warps of a block, and blocks of an SM: as many registers as K chunks need.
+// Warps of a block, and blocks of an SM: as many registers as K chunks need.  One block where the parameters are large: they
+// are brought in once an SM (4096 x 4096 bf16: 24 warps 14.9 us, two blocks of 12 15.8; 900 rows: 6.7 and 8.2).
 template <int SRC, bool STRIDED, int K>
 struct Tall {
     static constexpr int WORDS = K * Raw<SRC, STRIDED>::WORDS;    // registers that hold a row's part
-    static constexpr int WARPS = WORDS >= 64 ? 16 : WORDS >= 32 ? 12 : 16, BLOCKS = WORDS >= 64 ? 1 : 2;
+    static constexpr int WARPS = WORDS >= 64 ? 16 : WORDS >= 32 ? 24 : 16, BLOCKS = WORDS >= 32 ? 1 : 2;
 };
 
 // blockDim = (32, warps of a row, rows of a block).  The next row (whole vectors) is copied to shared memory meanwhile.
@@ -373,7 +374,7 @@ lrbi_status tall_kernel_launch(const NormForward &a, cudaStream_t s)
     auto kernel = norm_forward_tall_kernel<SRC, OUT, STRIDED, COPY, K>;
     const long long most = NORM_SMS * blocks_per_sm(kernel, 32 * block.y * block.z, smem);
     // Rows go in rounds over all blocks: the same number of rounds with the fewest rows a block, so that the last is not
-    // nearly empty (4096 x 4096: 3 rounds of 6 rows a block, the last a third full, 18.0 us; of 5 rows, 16.8 us).
+    // nearly empty (4096 x 4096, two blocks an SM: 3 rounds of 6 rows a block, the last a third full, 18.0 us; of 5 rows, 16.8 us).
     const long long rounds = ((long long)a.rows + most * block.z - 1) / (most * block.z);
     block.z = (unsigned)std::max(1LL, ((long long)a.rows + most * rounds - 1) / (most * rounds));
     const long long need = ((long long)a.rows + block.z - 1) / block.z;
@@ -396,9 +397,9 @@ lrbi_status forward_launch(NormForward a, cudaStream_t s)
     const int most = TWO && spans > 32 ? 16 : 8;
     a.warps = (spans + most - 1) / most;
     // Few rows leave most of the GPU idle with a warp each, and the parameters' way into shared memory is a good part of the
-    // time: then a block takes a row.  Rows of two warps: 300 x 4096 3.9 us (a warp or two: 7.2), 700 6.4 (8.2), 900 8.1 (8.5),
-    // 1300 9.7 (8.6); of one: 590 x 1024 2.5 (2.8), 1200 3.7 (4.0), 1500 x 1157 6.6 (5.7), 2000 x 1024 5.4 (4.4).
-    const bool few = (long long)a.rows * a.warps < (a.warps > 1 ? 12 : 8) * NORM_SMS;
+    // time: then a block takes a row.  Rows of two warps: 300 x 4096 3.9 us (two warps: 7.2), 700 6.5, 900 8.1 (6.7), 1300
+    // 9.7 (7.3); of one: 590 x 1024 2.5 (2.8), 1200 3.7 (4.0), 1500 x 1157 6.6 (5.5), 2000 x 1024 5.4 (4.0).
+    const bool few = (long long)a.rows * a.warps < (a.warps > 1 ? 10 : 8) * NORM_SMS;
     if (spans > 64) return norm_launch(norm_forward_wide_kernel<SRC, STRIDED>, a.rows, dim3(1024), 0, s, a);
     if (few) {
         if (spans <= 32) return norm_launch(norm_forward_row_kernel<SRC, STRIDED, 1>, a.rows, dim3(32 * spans), 0, s, a);
