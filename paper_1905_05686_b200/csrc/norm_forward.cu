@@ -355,8 +355,7 @@ int blocks_per_sm(Kernel kernel, int threads, size_t smem)
     const uint64_t key = (uint64_t)threads << 48 | (uint64_t)smem << 8, k = known.load(std::memory_order_relaxed);
     if ((k & ~255ull) == key && k) return (int)(k & 255);
     int n = 1;
-    if (smem > 40 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
+    if ((smem > 32 * 1024 && allow_shared(kernel, smem) != cudaSuccess) || cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
     known.store(key | (uint64_t)n, std::memory_order_relaxed);
     return n;
 }
