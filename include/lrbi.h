@@ -397,8 +397,8 @@ LRBI_API lrbi_status lrbi_activation_backward(const void *da, int32_t da_dtype, 
  *           16 * tile + g and + g + 8; its bits 4j .. 4j + 3 are row g + 8 * (j & 1), column
  *           64 * u + 32 * (s / 2) + 8 * t + 4 * (s & 1) + i with i = 2 * (j / 2 & 1) + j / 4.  Rows past the last hold anything; columns past the last hold their group's z
  *           (where they belong to no group, anything).
- *   meta    device, uint32, [RT][G][16]: row 16 * tile + r of group g has the bits of s in the upper half and z in the
- *           lowest four bits of word (tile, g, r).
+ *   meta    device, uint32, [RT][G][16], 16-byte aligned: row 16 * tile + r of group g has the bits of s in the upper half
+ *           and z in the lowest four bits of word (tile, g, r).
  * lrbi_w4_quantize  W [rows][cols] bf16 -> packed, meta.  Over the kept weights of a group: lo = min(0, W), hi = max(0, W),
  *           s = bf16((hi - lo) / 15), z = clamp(round(-lo / s)), q = clamp(round(W / s) + z), each step one fp32 operation,
  *           rounding to nearest even, clamped to 0 .. 15.  A group without a non-zero kept weight has s = 0, z = 8; a kept

@@ -564,7 +564,8 @@ def lrbi_activation_backward(da: torch.Tensor, h, act: str, restore: bool = Fals
 
 
 class W4Weights:
-    """A layer's weights in 4 bits as the library lays them out (lrbi.h): packed and meta are int32 CUDA tensors."""
+    """A layer's weights in 4 bits as the library lays them out (lrbi.h): packed and meta are int32 CUDA tensors that start on
+    16-byte boundaries (the products refuse others)."""
 
     __slots__ = ("packed", "meta", "rows", "cols", "group")
 

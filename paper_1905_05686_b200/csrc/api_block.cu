@@ -177,7 +177,7 @@ lrbi_status lrbi_w4_quantize(const lrbi_layout *layout, const uint16_t *W, const
                              uint32_t *packed, uint32_t *meta, void *stream)
 {
     if (!layout || layout->rows < 1 || !cols_ok(layout->cols) || !group_ok(group) || !W || !packed || !meta) return LRBI_ERR_INVALID_ARG;
-    if (!aligned(W, 2) || !aligned(packed, 16) || !aligned(meta, 4) || !ip != !iz) return LRBI_ERR_INVALID_ARG;
+    if (!aligned(W, 2) || !aligned(packed, 16) || !aligned(meta, 16) || !ip != !iz) return LRBI_ERR_INVALID_ARG;
     if (ip && (!aligned(ip, 4) || !aligned(iz, 4) || layout->tile_rows < 1 || layout->tile_cols < 1 || layout->rank < 1)) return LRBI_ERR_INVALID_ARG;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     lrbi_layout l = *layout;
@@ -189,7 +189,7 @@ lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, int32_t r
                          void *Y, int32_t y_dtype, void *stream)
 {
     if (rows < 1 || !cols_ok(cols) || !group_ok(group) || batch < 0 || !packed || !meta || !dtype_ok(y_dtype)) return LRBI_ERR_INVALID_ARG;
-    if (!aligned(packed, 16) || !aligned(meta, 4)) return LRBI_ERR_INVALID_ARG;
+    if (!aligned(packed, 16) || !aligned(meta, 16)) return LRBI_ERR_INVALID_ARG;      // both are copied 16 bytes at a time
     if (batch > 0 && (!X || !Y || !aligned(X, 2) || !aligned(Y, y_dtype == LRBI_Y_F32 ? 4 : 2))) return LRBI_ERR_INVALID_ARG;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     if (batch == 0) return LRBI_OK;

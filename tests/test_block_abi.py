@@ -88,3 +88,13 @@ def test_w4_arguments(lib):
     gemv = [P, P, 64, 64, 64, P, 2, P, 0, NULL]
     refused(lib, L.lrbi_w4_gemv, gemv, [(0, NULL), (0, ctypes.c_void_p(0x1008)), (1, NULL), (2, 0), (3, 0), (4, 16), (5, NULL), (5, ODD), (6, -1), (7, NULL), (7, ODD), (8, 2)])
     assert L.lrbi_w4_gemv(*changed(gemv, 6, 0)) == lib.OK
+
+
+def test_w4_meta_alignment(lib):
+    """Scales and zero points are copied 16 bytes at a time: an array that starts elsewhere is refused, not launched."""
+    L = lib.lib()
+    lay = lib.Layout(64, 64, 32, 32, 4)
+    for at in (0x1004, 0x1008, 0x100C):
+        off = ctypes.c_void_p(at)
+        refused(lib, L.lrbi_w4_gemv, [P, P, 64, 64, 64, P, 0, P, 0, NULL], [(1, off)])        # no rows of X: nothing could be launched
+        refused(lib, L.lrbi_w4_quantize, [ctypes.byref(lay), P, P, P, 64, P, P, NULL], [(6, off)])
