@@ -3,7 +3,7 @@
 Every step of the path (decode, pruning, product) runs in the CUDA library; this module turns
 torch CUDA tensors into device pointers and checks return codes.  torch is used for device
 memory and streams.  The calls made per layer and per token around the masked layers are marshalled by a small
-compiled module (_lrbi_torch.so) that calls the same C ABI.  If the library is not built, importing a compute function's first call
+compiled module (_lrbi_torch-*.so) that calls the same C ABI.  If the library is not built, importing a compute function's first call
 raises: there is no CPU fallback.
 """
 from __future__ import annotations
@@ -15,11 +15,12 @@ import os
 import numpy as np
 import torch
 
+from .build import calls_path
 from .synth import Layer
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblrbi.so")
-CALLS_PATH = os.path.join(_HERE, "_lrbi_torch.so")
+CALLS_PATH = calls_path()
 
 ALGO_AUTO, ALGO_GENERIC, ALGO_GEMV, ALGO_TENSOR, ALGO_DECODE_BALLOT, ALGO_DECODE_PLANES, ALGO_DECODE_PLANES_WIDE, ALGO_STREAM, ALGO_TENSOR_PAIR, ALGO_TENSOR_PAIR2, ALGO_TENSOR_PAIR192 = range(11)
 ALGO_NAMES = {0: "auto", 1: "generic", 2: "gemv", 3: "tensor", 4: "decode_ballot", 5: "decode_planes", 6: "decode_planes_wide", 7: "stream", 8: "tensor_pair", 9: "tensor_pair2", 10: "tensor_pair192"}
