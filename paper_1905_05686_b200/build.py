@@ -7,6 +7,8 @@ import re
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -72,17 +74,23 @@ def _build_calls(target: str) -> None:
 
 
 def _build_library(verbose: bool) -> None:
+    """An nvcc a source, as many at a time as there are processors: one after the other they take more than twice as long."""
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [
-        nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-        "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
-        "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-    ]
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = arch + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
+                    "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", tmp]
-    subprocess.run(cmd, check=True)
+        flags += ["-Xptxas", "-v"]
+    tmp = LIB + ".tmp.%d" % os.getpid()
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(os.cpu_count()) as pool:
+        def compiled(source):
+            out = os.path.join(objects, source[:-3] + ".o")
+            subprocess.run([nvcc, *flags, "-c", os.path.join(CSRC, source), "-o", out], check=True)
+            return out
+
+        # the longest first
+        order = sorted(SOURCES, key=lambda f: -os.path.getsize(os.path.join(CSRC, f)))
+        subprocess.run([nvcc, *arch, "-shared", *pool.map(compiled, order), "-o", tmp], check=True)
     os.replace(tmp, LIB)
 
 

@@ -47,6 +47,16 @@ def test_another_torch(built, monkeypatch):
     assert compilers(ran) == {"g++"} and build.calls_path() != own and os.path.exists(build.calls_path())
 
 
+def test_every_source_is_compiled_and_linked(built):
+    build, ran, _ = built
+    build.build()
+    sources = {f for f in os.listdir(build.CSRC) if f.endswith(".cu")}
+    compiled = [os.path.basename(a) for c in ran for a in c if a.endswith(".cu")]
+    assert sorted(compiled) == sorted(sources)
+    link = next(c for c in ran if "-shared" in c and os.path.basename(c[0]) == "nvcc")
+    assert {os.path.basename(a)[:-2] for a in link if a.endswith(".o")} >= {s[:-3] for s in sources}
+
+
 def test_binding_loads_what_was_built():
     torch = pytest.importorskip("torch")
     from paper_1905_05686_b200 import binding, build
