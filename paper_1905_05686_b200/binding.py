@@ -5,6 +5,10 @@ torch CUDA tensors into device pointers and checks return codes.  torch is used 
 memory and streams.  The calls made per layer and per token around the masked layers are marshalled by a small
 compiled module (_lrbi_torch-*.so) that calls the same C ABI.  If the library is not built, importing a compute function's first call
 raises: there is no CPU fallback.
+
+Calls take `stream`, a torch.cuda.Stream (None: the current one).  A call on another stream does not wait for the current one, so
+that the two may overlap: the caller makes that stream wait for whatever writes the inputs (stream.wait_stream), keeps the inputs
+until it is through with them (Tensor.record_stream), and makes the current stream wait before the results are used there.
 """
 from __future__ import annotations
 
@@ -196,6 +200,18 @@ def selftest_bounded_wait(limit_us: int = 1000, stream=None) -> None:
 def _stream_ptr(stream):
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A new tensor that a call on `stream` writes: out of that stream's pool, since the current stream may still be at work on
+    what was freed to its own, and kept until the current stream, which will use it, is through with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
 
 
 def _dev(t: torch.Tensor, dtype, what):
@@ -600,11 +616,8 @@ def lrbi_w4_quantize(layer, W: torch.Tensor, group: int = 128, ip: torch.Tensor 
         raise ValueError("group must be 32, 64 or 128")
     w = _dev(W, torch.bfloat16, "W")
     factors = [None if t is None else _dev(t, torch.int32, what) for t, what in ((ip, "ip"), (iz, "iz"))]
-    packed = torch.empty(L.lrbi_w4_packed_words(lay.rows, lay.cols), dtype=torch.int32, device=W.device)
-    meta = torch.empty(L.lrbi_w4_meta_words(lay.rows, lay.cols, group), dtype=torch.int32, device=W.device)
-    if stream is not None:
-        packed.record_stream(stream)
-        meta.record_stream(stream)
+    packed = _empty(L.lrbi_w4_packed_words(lay.rows, lay.cols), torch.int32, W.device, stream)
+    meta = _empty(L.lrbi_w4_meta_words(lay.rows, lay.cols, group), torch.int32, W.device, stream)
     rc = L.lrbi_w4_quantize(ctypes.byref(lay), w, *factors, group, packed.data_ptr(), meta.data_ptr(), _stream_ptr(stream))
     if rc != OK:
         raise LrbiError(rc, "lrbi_w4_quantize")

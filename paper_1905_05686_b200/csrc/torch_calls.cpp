@@ -6,6 +6,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -101,14 +102,13 @@ Matrix matrix_like(PyObject *o, const char *what, const Matrix &like)
 
 // The stream of a call: the current one, or the torch.cuda.Stream that was given.
 struct Call {
-    c10::cuda::CUDAStream stream;
-    bool other;
+    c10::cuda::CUDAStream current, stream;
     at::Device device;
 
-    Call(const at::Device &d, PyObject *s) : stream(c10::cuda::getCurrentCUDAStream(d.index())), other(s != Py_None), device(d)
+    Call(const at::Device &d, PyObject *s) : current(c10::cuda::getCurrentCUDAStream(d.index())), stream(current), device(d)
     {
         if (d.index() != c10::cuda::current_device()) throw BadValue("the call's tensors must be on the current CUDA device");
-        if (!other) return;
+        if (s == Py_None) return;
         int64_t v[3];
         const char *names[3] = {"stream_id", "device_index", "device_type"};
         for (int i = 0; i < 3; ++i) {
@@ -118,13 +118,22 @@ struct Call {
             Py_DECREF(a);
             if (v[i] == -1 && PyErr_Occurred()) throw Raised();
         }
+        if (v[2] != (int64_t)c10::DeviceType::CUDA || v[1] != d.index()) throw BadValue("stream must be a stream of the tensors' device");
         stream = c10::cuda::CUDAStream::unpack3(v[0], (c10::DeviceIndex)v[1], (c10::DeviceType)v[2]);
     }
-    // A new tensor.  On a stream that is not the current one it is kept until that stream is through with it.
+    // Memory that this call alone uses, out of the pool of the call's stream: what was freed there is through with before the
+    // call's kernels begin.  (The current stream may still be reading what was freed to its own pool.)
+    at::Tensor scratch(at::IntArrayRef sizes, at::ScalarType type) const
+    {
+        if (stream == current) return at::detail::empty_cuda(sizes, type, device, std::nullopt);
+        const c10::cuda::CUDAStreamGuard guard(stream);
+        return at::detail::empty_cuda(sizes, type, device, std::nullopt);
+    }
+    // A new tensor for the caller, whose own stream will use it too: its memory is kept until that stream is through with it.
     at::Tensor make(at::IntArrayRef sizes, at::ScalarType type) const
     {
-        at::Tensor t = at::detail::empty_cuda(sizes, type, device, std::nullopt);
-        if (other) t.record_stream(stream.unwrap());
+        at::Tensor t = scratch(sizes, type);
+        if (stream != current) t.record_stream(current.unwrap());
         return t;
     }
     // Two new arrays out of one allocation, the second on a 16-byte boundary (allocations cost more than the checks of a call).
@@ -292,7 +301,7 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         auto [dgamma, dbeta] = c.make_two({dy.cols}, at::kFloat, {dy.cols}, at::kFloat);
         if (restore) y = c.make({dy.rows, dy.cols}, dy.type);
         const size_t need = lrbi_layer_norm_backward_workspace(dy.rows, dy.cols);
-        const at::Tensor work = c.make({(int64_t)need}, at::kByte);
+        const at::Tensor work = c.scratch({(int64_t)need}, at::kByte);
         check(lrbi_layer_norm_backward(dy.data, dy.dtype, dy.stride, x.data, x.dtype, x.stride, k.bytes(), k.scales(), dy.rows, dy.cols, p.gamma, p.beta,
                                        p.dtype, mean, rstd, dres.data, dres.stride, dx.data_ptr(), type_code(type), dy.cols,
                                        restore ? y.data_ptr() : nullptr, dy.cols, static_cast<float *>(dgamma.data_ptr()),
