@@ -238,7 +238,7 @@ def lrbi_decode_mask(layer, ip: torch.Tensor, iz: torch.Tensor, mask_out: torch.
     if ip.numel() != L.lrbi_packed_ip_words(ctypes.byref(lay)) or iz.numel() != L.lrbi_packed_iz_words(ctypes.byref(lay)):
         raise ValueError("packed factor sizes do not match the layout")
     if mask_out is None:
-        mask_out = torch.empty((lay.rows, (lay.cols + 31) // 32), dtype=torch.int32, device=ip.device)
+        mask_out = _empty((lay.rows, (lay.cols + 31) // 32), torch.int32, ip.device, stream)
     elif mask_out.numel() != L.lrbi_mask_words(ctypes.byref(lay)):
         raise ValueError("mask_out has the wrong size")
     rc = L.lrbi_decode_mask(ctypes.byref(lay), _dev(ip, torch.int32, "ip"), _dev(iz, torch.int32, "iz"),
@@ -261,7 +261,7 @@ def lrbi_decode_mask_ranked(layer, ranks, ip_off, iz_off, ip, iz, mask_out=None,
     lay = Layout.of(layer)
     tr = _tile_ranks(lay, ranks, ip_off, iz_off)
     if mask_out is None:
-        mask_out = torch.empty((lay.rows, (lay.cols + 31) // 32), dtype=torch.int32, device=ip.device)
+        mask_out = _empty((lay.rows, (lay.cols + 31) // 32), torch.int32, ip.device, stream)
     rc = lib().lrbi_decode_mask_ranked(ctypes.byref(lay), ctypes.byref(tr), _dev(ip, torch.int32, "ip"), _dev(iz, torch.int32, "iz"),
                                        _dev(mask_out, torch.int32, "mask_out"), _stream_ptr(stream))
     if rc != OK:
@@ -278,7 +278,7 @@ def lrbi_masked_gemm_ranked(layer, ranks, ip_off, iz_off, W, ip, iz, X, Y=None, 
         raise ValueError("W / X shapes do not match the layout")
     batch = X.shape[0]
     if Y is None:
-        Y = torch.empty((batch, lay.rows), dtype=y_dtype, device=X.device)
+        Y = _empty((batch, lay.rows), y_dtype, X.device, stream)
     elif tuple(Y.shape) != (batch, lay.rows) or Y.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("Y has the wrong shape or dtype")
     rc = lib().lrbi_masked_gemm_ranked(ctypes.byref(lay), ctypes.byref(tr), _dev(W, torch.bfloat16, "W"), _dev(ip, torch.int32, "ip"),
@@ -293,7 +293,7 @@ def lrbi_decode_mask_batch(layers, ips, izs, stream=None):
     """Decode the indices of several layers with one launch per 32 layers; returns the list of masks."""
     n = len(layers)
     lays = (Layout * n)(*[Layout.of(l) for l in layers])
-    masks = [torch.empty((l.rows, (l.cols + 31) // 32), dtype=torch.int32, device=ips[0].device) for l in lays]
+    masks = [_empty((l.rows, (l.cols + 31) // 32), torch.int32, ips[0].device, stream) for l in lays]
     arr = lambda ts, what: (ctypes.c_void_p * n)(*[_dev(t, torch.int32, what).value for t in ts])
     rc = lib().lrbi_decode_mask_batch(n, lays, arr(ips, "ip"), arr(izs, "iz"), arr(masks, "mask_out"), _stream_ptr(stream))
     if rc != OK:
@@ -305,7 +305,7 @@ def lrbi_transpose_bf16(src: torch.Tensor, dst: torch.Tensor | None = None, stre
     """dst [cols, rows] = src [rows, cols] transposed (bf16)."""
     rows, cols = src.shape
     if dst is None:
-        dst = torch.empty((cols, rows), dtype=torch.bfloat16, device=src.device)
+        dst = _empty((cols, rows), torch.bfloat16, src.device, stream)
     rc = lib().lrbi_transpose_bf16(_dev(src, torch.bfloat16, "src"), rows, cols, _dev(dst, torch.bfloat16, "dst"), _stream_ptr(stream))
     if rc != OK:
         raise LrbiError(rc, "lrbi_transpose_bf16")
@@ -319,7 +319,7 @@ def lrbi_masked_gemm_dx(layer, Wt, ip, iz, dY, dX=None, dtype=torch.bfloat16, al
         raise ValueError("Wt / dY shapes do not match the layout")
     batch = dY.shape[0]
     if dX is None:
-        dX = torch.empty((batch, lay.cols), dtype=dtype, device=dY.device)
+        dX = _empty((batch, lay.cols), dtype, dY.device, stream)
     rc = lib().lrbi_masked_gemm_dx(ctypes.byref(lay), _dev(Wt, torch.bfloat16, "Wt"), _dev(ip, torch.int32, "ip"), _dev(iz, torch.int32, "iz"),
                                    _dev(dY, torch.bfloat16, "dY"), batch, _dev(dX, dX.dtype, "dX"),
                                    Y_F32 if dX.dtype == torch.float32 else Y_BF16, algo, _stream_ptr(stream))
@@ -336,10 +336,10 @@ def lrbi_masked_gemm_dw(layer, dY, X, ip, iz, dW=None, dtype=torch.bfloat16, wor
     if tuple(dY.shape) != (batch, lay.rows) or tuple(X.shape) != (batch, lay.cols):
         raise ValueError("dY / X shapes do not match the layout")
     if dW is None:
-        dW = torch.empty((lay.rows, lay.cols), dtype=dtype, device=dY.device)
+        dW = _empty((lay.rows, lay.cols), dtype, dY.device, stream)
     need = lib().lrbi_masked_gemm_dw_workspace(ctypes.byref(lay), batch)
     if isinstance(workspace, str):
-        workspace = torch.empty(need, dtype=torch.uint8, device=dY.device)
+        workspace = _empty(need, torch.uint8, dY.device, stream)
     wptr, wbytes = (ctypes.c_void_p(workspace.data_ptr()), workspace.numel()) if workspace is not None else (ctypes.c_void_p(0), 0)
     rc = lib().lrbi_masked_gemm_dw(ctypes.byref(lay), _dev(dY, torch.bfloat16, "dY"), _dev(X, torch.bfloat16, "X"), batch,
                                    _dev(ip, torch.int32, "ip"), _dev(iz, torch.int32, "iz"), _dev(dW, dW.dtype, "dW"),
@@ -354,7 +354,7 @@ def lrbi_nmf_update(layer, W, mp, mz, iterations, eps=1e-9, workspace=None, stre
     lay = Layout.of(layer)
     need = lib().lrbi_nmf_workspace(ctypes.byref(lay))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=W.device)
+        workspace = _empty(need, torch.uint8, W.device, stream)
     rc = lib().lrbi_nmf_update(ctypes.byref(lay), _dev(W, torch.bfloat16, "W"), _dev(mp, torch.float32, "mp"), _dev(mz, torch.float32, "mz"),
                                iterations, ctypes.c_float(eps), ctypes.c_void_p(workspace.data_ptr()), workspace.numel(), _stream_ptr(stream))
     if rc != OK:
@@ -373,8 +373,8 @@ def lrbi_threshold_pack(layer, mp: torch.Tensor, mz: torch.Tensor, tp: torch.Ten
         raise ValueError("factor sizes do not match the layout")
     if tp.numel() != tiles or tz.numel() != tiles:
         raise ValueError("one threshold pair per tile")
-    ip = torch.empty(L.lrbi_packed_ip_words(ctypes.byref(lay)), dtype=torch.int32, device=mp.device)
-    iz = torch.empty(L.lrbi_packed_iz_words(ctypes.byref(lay)), dtype=torch.int32, device=mp.device)
+    ip = _empty(L.lrbi_packed_ip_words(ctypes.byref(lay)), torch.int32, mp.device, stream)
+    iz = _empty(L.lrbi_packed_iz_words(ctypes.byref(lay)), torch.int32, mp.device, stream)
     rc = L.lrbi_threshold_pack(ctypes.byref(lay), _dev(mp, torch.float32, "mp"), _dev(mz, torch.float32, "mz"),
                                _dev(tp, torch.float32, "tp"), _dev(tz, torch.float32, "tz"),
                                _dev(ip, torch.int32, "ip"), _dev(iz, torch.int32, "iz"), _stream_ptr(stream))
@@ -395,7 +395,7 @@ def lrbi_index_cost(layer, W: torch.Tensor, theta: float, ip: torch.Tensor, iz: 
         raise ValueError("packed factor sizes do not match the layout")
     tiles = (-(-lay.rows // lay.tile_rows)) * (-(-lay.cols // lay.tile_cols))
     if out is None:
-        out = torch.empty((tiles, 4), dtype=torch.int64, device=W.device)
+        out = _empty((tiles, 4), torch.int64, W.device, stream)
     elif out.numel() != tiles * 4:
         raise ValueError("out has the wrong size")
     rc = L.lrbi_index_cost(ctypes.byref(lay), _dev(W, torch.bfloat16, "W"), ctypes.c_float(theta), _dev(ip, torch.int32, "ip"),
@@ -423,7 +423,7 @@ def lrbi_masked_gemm(layer, W: torch.Tensor, ip: torch.Tensor, iz: torch.Tensor,
         raise ValueError("packed factor sizes do not match the layout")
     batch = X.shape[0]
     if Y is None:
-        Y = torch.empty((batch, lay.rows), dtype=y_dtype, device=X.device)
+        Y = _empty((batch, lay.rows), y_dtype, X.device, stream)
     if tuple(Y.shape) != (batch, lay.rows) or Y.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("Y must be [batch, rows] bf16 or fp32")
     code = Y_BF16 if Y.dtype == torch.bfloat16 else Y_F32
