@@ -376,6 +376,8 @@ LRBI_API lrbi_status lrbi_layer_norm_backward(const void *dy, int32_t dy_dtype, 
  *       LRBI_ACT_RELU max(h, 0)      LRBI_ACT_GELU h * Phi(h), Phi the normal distribution      LRBI_ACT_SILU h / (1 + exp(-h))
  * lrbi_activation_backward: dh = da * act'(h), from h, or (h NULL) from its 8-bit copy; `a`, in da's type, or NULL,
  * receives act(h) again, for the weight gradient of the layer that it went into.  At h = 0 relu has slope 0.
+ * An infinite h gives what the formula gives: +inf for +inf; for -inf 0 (relu) or NaN (gelu, silu: infinity times zero); the
+ * slopes of gelu and silu are NaN there.
  */
 enum { LRBI_ACT_RELU = 0, LRBI_ACT_GELU = 1, LRBI_ACT_SILU = 2 };
 LRBI_API lrbi_status lrbi_activation(const void *h, int32_t h_dtype, int64_t h_stride, int32_t rows, int32_t cols,

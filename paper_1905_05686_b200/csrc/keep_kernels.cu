@@ -59,7 +59,8 @@ __device__ __forceinline__ void activate(F2 h, F2 &value, F2 &slope)
         const F2 tail = t * p * e;
         float x, y;
         split(tail, x, y);
-        value = fma2(f2(-fabsf(a), -fabsf(b)), tail, f2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+        // The tail of 64 is zero already: +inf would give infinity times zero.  (A NaN comes through the tail.)
+        value = fma2(f2(-fabsf(fminf(a, 64.f)), -fabsf(fminf(b, 64.f))), tail, f2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
         if (SLOPE) slope = fma2(h * f2(0.39894228f), e, f2((a >= 0.f ? 1.f : 0.f) - copysignf(x, a), (b >= 0.f ? 1.f : 0.f) - copysignf(y, b)));
     }
 }
