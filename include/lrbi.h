@@ -376,6 +376,9 @@ LRBI_API lrbi_status lrbi_layer_norm_backward(const void *dy, int32_t dy_dtype, 
  *       LRBI_ACT_RELU max(h, 0)      LRBI_ACT_GELU h * Phi(h), Phi the normal distribution      LRBI_ACT_SILU h / (1 + exp(-h))
  * lrbi_activation_backward: dh = da * act'(h), from h, or (h NULL) from its 8-bit copy; `a`, in da's type, or NULL,
  * receives act(h) again, for the weight gradient of the layer that it went into.  At h = 0 relu has slope 0.
+ * Before it is rounded to its output's type a result is off by at most 2^-20 (1 + h^2 / 8) of itself for gelu (2^-13 for
+ * an output in bf16) and 2^-20 (1 + |h|) for silu (below 2^-100 it may come as 0), a slope by as much of the larger of its
+ * two terms.
  * An infinite h gives what the formula gives: +inf for +inf; for -inf 0 (relu) or NaN (gelu, silu: infinity times zero); the
  * slopes of gelu and silu are NaN there.
  */

@@ -39,3 +39,41 @@ def test_activation_of_infinities(act, dtype, rows, cols, pad):
         assert torch.equal(got[rest], plain.float().cpu()[rest])
     stands = b.lrbi_checkpoint_load(kept, F32)
     assert all(torch.isnan(stands[place]) for place in at)          # a group with either restores as NaN
+
+
+def test_gelu_against_64_bits_in_its_tails():
+    """Relative to the result, where gelu is small too: lrbi.h's bound 2^-20 (1 + h^2 / 8).  Its parts: the tail's fit 2^-23, its
+    evaluation in fp32 with the hardware's reciprocal 3 * 2^-23, exp2 2^-22, and 2^-23 h^2 for the argument of exp2 (three
+    roundings of h^2 / 2 each).  Slopes: the same of both terms, and their sum's rounding."""
+    from scipy.special import erfcx
+    b = _b()
+    h = np.concatenate([np.linspace(-13, 13, 400001), -np.logspace(-30, 1, 20000), np.logspace(-30, 1, 20000)]).astype(np.float32)
+    h = h[None, : h.size // 8 * 8]
+    x = h.astype(np.float64)
+    m = np.abs(x)
+    phi = np.exp(-x * x / 2) / np.sqrt(2 * np.pi)
+    tail = erfcx(m / np.sqrt(2)) * np.exp(-x * x / 2) / 2            # Phi(-|h|), no cancellation
+    value, slope = np.where(x > 0, x * (1 - tail), x * tail), np.where(x >= 0, 1 - tail, tail) + x * phi
+    rel = 2.0 ** -20 * (1 + x * x / 8)
+    t = torch.from_numpy(h).cuda()
+    for cols in (h.shape[1], h.shape[1] - 3):                        # whole and ragged rows
+        got, again = b.lrbi_activation_backward(torch.ones_like(t[:, :cols]), t[:, :cols], "gelu", restore=True)
+        a = b.lrbi_activation(t[:, :cols], "gelu")
+        at = np.s_[:, :cols]
+        assert torch.equal(a, again)
+        off = np.abs(a.cpu().numpy().astype(np.float64) - value[at])
+        assert (off <= (m * tail * rel + 2.0 ** -23 * np.where(x > 0, x, 0) + 1e-44)[at]).all()
+        off = np.abs(got.cpu().numpy().astype(np.float64) - slope[at])
+        assert (off <= (rel * (tail + m * phi) + 2.0 ** -22 * np.where(x >= 0, 1.0, 0.0) + 1e-44)[at]).all()
+
+
+def test_gelu_in_bf16_is_rounded_once_in_its_tails():
+    """lrbi.h: off by 2^-13 of itself before it is rounded, 2^-5 of a step at most; exp2 and its argument 2^-8 of one down to -10."""
+    from scipy.special import erfcx
+    b = _b()
+    h = torch.linspace(-10, -1, 4096, device="cuda").to(BF16)[None]
+    x = h.float().cpu().numpy().astype(np.float64)
+    value = x * erfcx(-x / np.sqrt(2)) * np.exp(-x * x / 2) / 2
+    a = b.lrbi_activation(h, "gelu").float().cpu().numpy().astype(np.float64)
+    step = 2.0 ** (np.floor(np.log2(np.abs(value))) - 7)
+    assert (np.abs(a - value) <= step * (0.5 + 2.0 ** -5 + 2.0 ** -8)).all()
