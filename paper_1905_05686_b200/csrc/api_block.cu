@@ -1,6 +1,7 @@
 // C ABI of the operators around the masked layers: argument checks and calls of the launchers.
 #include <unordered_map>
 
+#include "occupancy_cache.cuh"
 #include "row_ops.cuh"
 
 namespace lrbi {
@@ -21,6 +22,18 @@ cudaError_t allow_shared(const void *kernel, size_t smem)
         e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     }
     return e;
+}
+
+int blocks_per_sm(const void *kernel, int threads, size_t smem)
+{
+    static OccupancyCache cache;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+    return cache.get(kernel, dev, threads, smem, [&] {
+        int n = 0;
+        if ((smem > 32 * 1024 && allow_shared(kernel, smem) != cudaSuccess) || cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) return 0;
+        return n;
+    });
 }
 
 }  // namespace lrbi

@@ -16,7 +16,6 @@
 // 4097 bf16, an access a value, 47.6 (20.5).  row: 2.3 us for one token of 4096, which is the launch, two waits for memory and
 // two sums over a block.
 #include <algorithm>
-#include <atomic>
 
 #include "norm_common.cuh"
 
@@ -346,19 +345,6 @@ __global__ void __launch_bounds__(1024) norm_forward_wide_kernel(NormForward a)
 }
 
 namespace {
-
-// Blocks of a kernel that an SM takes at once; asked once for each amount of shared memory that comes up.
-template <class Kernel>
-int blocks_per_sm(Kernel kernel, int threads, size_t smem)
-{
-    static std::atomic<uint64_t> known{0};     // threads, shared memory and the answer of the last question
-    const uint64_t key = (uint64_t)threads << 48 | (uint64_t)smem << 8, k = known.load(std::memory_order_relaxed);
-    if ((k & ~255ull) == key && k) return (int)(k & 255);
-    int n = 1;
-    if ((smem > 32 * 1024 && allow_shared(kernel, smem) != cudaSuccess) || cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
-    known.store(key | (uint64_t)n, std::memory_order_relaxed);
-    return n;
-}
 
 template <int SRC, int OUT, bool STRIDED, bool COPY, int K>
 lrbi_status tall_kernel_launch(const NormForward &a, cudaStream_t s)

@@ -388,6 +388,11 @@ cudaError_t allow_shared(const void *kernel, size_t smem);
 template <class... A>
 cudaError_t allow_shared(void (*kernel)(A...), size_t smem) { return allow_shared(reinterpret_cast<const void *>(kernel), smem); }
 
+// Host side: blocks of a kernel that an SM of the current device takes at once, 1 where it does not say.
+int blocks_per_sm(const void *kernel, int threads, size_t smem);
+template <class... A>
+int blocks_per_sm(void (*kernel)(A...), int threads, size_t smem) { return blocks_per_sm(reinterpret_cast<const void *>(kernel), threads, smem); }
+
 // Host side: launches a kernel that calls begin(), with `smem` bytes of dynamic shared memory and clusters of `cluster` blocks.
 template <class K, class... A>
 lrbi_status launch_kernel(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t s, unsigned cluster, const A &...a)
