@@ -406,9 +406,10 @@ LRBI_API lrbi_status lrbi_activation_backward(const void *da, int32_t da_dtype, 
  *           and z in the lowest four bits of word (tile, g, r).
  * lrbi_w4_quantize  W [rows][cols] bf16 -> packed, meta.  Over the kept weights of a group: lo = min(0, W), hi = max(0, W),
  *           s = bf16((hi - lo) / 15), z = clamp(round(-lo / s)), q = clamp(round(W / s) + z), each step one fp32 operation,
- *           rounding to nearest even, clamped to 0 .. 15.  A group without a non-zero kept weight has s = 0, z = 8; a kept
- *           weight that is not finite gives s = NaN.  What the array holds at pruned places is not looked at.  ip, iz: the
- *           layer's packed factors, or both NULL (nothing is pruned; only rows and cols of the layout are looked at).
+ *           rounding to nearest even, clamped to 0 .. 15.  A group without a non-zero kept weight (or with a range below
+ *           2^-130, whose s is rounded to 0) has s = 0, z = 8; a kept weight that is not finite, or a range beyond fp32, gives
+ *           s = NaN.  What the array holds at pruned places is not looked at.  ip, iz: the layer's packed factors, or both
+ *           NULL (nothing is pruned; only rows and cols of the layout are looked at).
  * lrbi_w4_gemv  Y [batch][rows] (bf16 or fp32) = X W^T for X [batch][cols] bf16, contiguous, sums in fp32.  Made for a few
  *           rows of X (up to 16 go through the weights together); batch may be 0.
  */

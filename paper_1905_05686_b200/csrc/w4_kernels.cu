@@ -7,6 +7,7 @@
 // (w >> 4j) & 0x000F000F with the exponent of 128 set gives the pair (128 + q, 128 + q') in bf16 with a shift and one
 // logic operation, and subtracting (128 + z) gives q - z exactly: weights and activations enter the product unrounded,
 // sums and scales are fp32.
+#include <cfloat>
 #include <type_traits>
 
 #include "row_ops.cuh"
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(Geo geo, const uint16_
         bool bad = false;
         for (int j = lane; j < group; j += 32) {
             const float v = value[r][p * group + j];
-            bad |= !(fabsf(v) <= 3.4e38f);
+            bad |= !(fabsf(v) <= FLT_MAX);
             lo = fminf(lo, v);
             hi = fmaxf(hi, v);
         }
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(256) w4_quantize_kernel(Geo geo, const uint16_
         bad = __any_sync(0xFFFFFFFFu, bad);
         const float range = __fsub_rn(hi, lo);
         uint32_t bits = f32_to_bf16_rne(__fdiv_rn(range, 15.f));
-        if (bad || !(range <= 3.4e38f)) bits = 0x7FC0u;      // a weight that is not finite, or a range beyond fp32
+        if (bad || !(range <= FLT_MAX)) bits = 0x7FC0u;      // a weight that is not finite, or a range beyond fp32
         const float s = __uint_as_float(bits << 16);
         const bool fine = bits != 0x7FC0u && s > 0.f;
         const int z = fine ? (int)fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f) : 8;

@@ -77,3 +77,23 @@ def test_gelu_in_bf16_is_rounded_once_in_its_tails():
     a = b.lrbi_activation(h, "gelu").float().cpu().numpy().astype(np.float64)
     step = 2.0 ** (np.floor(np.log2(np.abs(value))) - 7)
     assert (np.abs(a - value) <= step * (0.5 + 2.0 ** -5 + 2.0 ** -8)).all()
+
+
+def test_quantize_ranges_up_to_the_end_of_fp32():
+    """A group's range is finite in fp32 up to its largest number; beyond that the scale is NaN."""
+    import test_gpu_w4 as w4
+    b = _b()
+    top = float(w4.f32([0x7F7F])[0])                                  # the largest bf16
+    W = np.zeros((16, 128), np.float32)
+    for row, low in enumerate((0.0, -1e36, -1.2e36, -1.3e36, -2e36, -1e38)):
+        W[row, 3], W[row, 5], W[row, 70] = top, low, 1.0
+    bits = w4.bf16_bits(W)
+    W = w4.f32(bits)
+    q, scale, zero = w4.quantize(W, np.ones_like(W, bool), 64)
+    over = np.isinf(W[:, :64].max(1) - W[:, :64].min(1))
+    assert 0 < over[:6].sum() < 5
+    scale[over, 0], zero[over, 0], q[over, :64] = 0x7FC0, 8, 8
+    got = b.lrbi_w4_quantize((16, 128, 16, 128, 1), b.to_device_bf16(bits.astype(np.uint16)), 64)
+    packed, meta = w4.lay_out(q, scale, zero, 64)
+    assert (got.meta.cpu().numpy().view(np.uint32).reshape(meta.shape) == meta).all()
+    assert (got.packed.cpu().numpy().view(np.uint32).reshape(packed.shape) == packed).all()
