@@ -60,10 +60,12 @@ __device__ __forceinline__ void cut(F2 (&v)[PAIRS], int c, int cols)
     }
 }
 
-__device__ __forceinline__ float inverse_root(float a)   // one Newton step on the hardware's estimate
+// 1 / sqrt(a): one Newton step on the hardware's estimate r, where r and a r are normal numbers (a may be a denormal one, whose
+// half need not be representable).  0 gives infinity, infinity 0.
+__device__ __forceinline__ float inverse_root(float a)
 {
     const float r = rsqrtf(a);
-    return a < 3e38f ? r * fmaf(-0.5f * a * r, r, 1.5f) : r;
+    return a > 0.f && a < 3e38f ? r * fmaf(-0.5f * (a * r), r, 1.5f) : r;
 }
 
 // Waits for the warps that share a row: `threads` of the block, barrier `id` (1 .. 15).

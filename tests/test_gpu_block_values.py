@@ -97,3 +97,22 @@ def test_quantize_ranges_up_to_the_end_of_fp32():
     packed, meta = w4.lay_out(q, scale, zero, 64)
     assert (got.meta.cpu().numpy().view(np.uint32).reshape(meta.shape) == meta).all()
     assert (got.packed.cpu().numpy().view(np.uint32).reshape(packed.shape) == packed).all()
+
+
+@pytest.mark.parametrize("rows", [3, 1500])              # a block has a row; a warp has one
+@pytest.mark.parametrize("cols", [256, 20480])
+def test_rstd_of_variances_that_are_zero_or_tiny(rows, cols):
+    """1 / sqrt(var + eps) for eps = 0: infinite for equal values, and right where the variance is below fp32's normal range."""
+    b = _b()
+    rows = min(rows, 3 if cols > 16384 else rows)
+    gamma = torch.ones(cols, device="cuda")
+    x = torch.full((rows, cols), 0.75, device="cuda")
+    y, mean, rstd = b.lrbi_layer_norm(x, gamma, eps=0.0)
+    assert (mean == 0.75).all() and torch.isinf(rstd).all() and (rstd > 0).all() and torch.isnan(y).all()
+    # pairs (v, -v), squares of two units of 2^-149 and (rounded) of four in turn: the mean is 0, the variance three units
+    v = torch.tensor([1.0, -1.0, 1.41, -1.41], device="cuda") * 2.0 ** -74
+    x = v.repeat(rows, cols // 4)
+    _, mean, rstd = b.lrbi_layer_norm(x, gamma, eps=0.0)
+    assert (mean == 0).all()
+    want = (3 * 2.0 ** -149) ** -0.5
+    assert ((rstd.double() / want - 1).abs() <= 2.0 ** -20).all()
