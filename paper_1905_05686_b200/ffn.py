@@ -89,7 +89,8 @@ class PrunedFFN:
         self.beta -= rate * grads["beta"]
 
     def tokens(self, group: int = 128) -> "TokenFFN":
-        return TokenFFN(self.up.quantize(group), self.down.quantize(group), self.gamma, self.beta, self.act, self.eps)
+        """The block as it is now, in 4 bits; later steps do not change it."""
+        return TokenFFN(self.up.quantize(group), self.down.quantize(group), self.gamma.clone(), self.beta.clone(), self.act, self.eps)
 
 
 class TokenFFN:

@@ -117,3 +117,16 @@ def test_tokens(group, tokens):
 def test_example_runs():
     from paper_1905_05686_b200 import ffn
     ffn.main()
+
+
+def test_tokens_are_served_from_what_was_taken():
+    """Training that goes on after tokens() does not reach the served block."""
+    from paper_1905_05686_b200 import ffn
+    block = ffn.synthetic_block(256, 512, 128)
+    served = block.tokens(64)
+    x = torch.randn((3, 256), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    before = served(x)
+    out, kept = block.forward(x)
+    _, grads = block.backward(torch.ones_like(out), kept)
+    block.step(grads, 0.5)
+    assert grads["gamma"].abs().max() > 0 and torch.equal(served(x), before)
