@@ -183,7 +183,7 @@ const float *statistics(PyObject *o, const char *what, const Matrix &x)
     return static_cast<const float *>(t.data_ptr());
 }
 
-// An 8-bit copy: made for a call, or read by one (its tensors were checked when the Checkpoint was made).
+// An 8-bit copy: made for a call, or read by one.
 struct Copy {
     at::Tensor q, scale;
     int8_t *bytes() const { return q.defined() ? static_cast<int8_t *>(q.data_ptr()) : nullptr; }
@@ -196,11 +196,23 @@ Copy make_copy(const Call &c, int rows, int cols)
     return {std::move(both.first), std::move(both.second)};
 }
 
-Copy read_copy(PyObject *q, PyObject *scale, const at::Device &device)
+// The copy of a [rows, cols] matrix that a call reads.
+Copy read_copy(PyObject *q, PyObject *scale, int64_t rows, int64_t cols, const at::Device &device)
 {
     Copy k = {tensor(q, "q"), tensor(scale, "scale")};
-    if (k.q.device() != device) throw BadValue("the 8-bit copy must be on the call's device");
+    if (!k.q.is_cuda() || k.q.device() != device || k.scale.device() != device) throw BadValue("the 8-bit copy must be on the call's device");
+    if (k.q.scalar_type() != at::kChar || k.scale.scalar_type() != at::kFloat || !k.q.is_contiguous() || !k.scale.is_contiguous())
+        throw BadType("an 8-bit copy is contiguous int8 and its scales contiguous float32");
+    if (rows < 0 || rows > INT_MAX || cols < 1 || cols > LRBI_MAX_ROW_COLS || k.q.numel() != rows * lrbi_checkpoint_pitch((int)cols) || k.scale.numel() != rows * lrbi_checkpoint_groups((int)cols))
+        throw BadValue("the 8-bit copy does not have the size of its matrix");
     return k;
+}
+
+int64_t whole_number(PyObject *o)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised();
+    return v;
 }
 
 void check(int rc, const char *what)
@@ -243,12 +255,12 @@ PyObject *checkpoint_load(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     CALL("checkpoint_load", 6) {
         const at::Device device = tensor(a[0], "q").device();
-        const Copy k = read_copy(a[0], a[1], device);
-        const int rows = (int)PyLong_AsLong(a[2]), cols = (int)PyLong_AsLong(a[3]);
+        const int64_t rows = whole_number(a[2]), cols = whole_number(a[3]);
+        const Copy k = read_copy(a[0], a[1], rows, cols, device);
         const at::ScalarType type = dtype_of(a[4], at::kBFloat16, "dtype");
         const Call c(device, a[5]);
         at::Tensor x = c.make({rows, cols}, type);
-        check(lrbi_checkpoint_load(k.bytes(), k.scales(), rows, cols, x.data_ptr(), type_code(type), cols, c.handle()), "lrbi_checkpoint_load");
+        check(lrbi_checkpoint_load(k.bytes(), k.scales(), (int)rows, (int)cols, x.data_ptr(), type_code(type), cols, c.handle()), "lrbi_checkpoint_load");
         return THPVariable_Wrap(std::move(x));
     });
 }
@@ -285,7 +297,7 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         Matrix x = {nullptr, LRBI_Y_BF16, dy.rows, dy.cols, dy.cols, dy.device, dy.type};
         Copy k;
         if (a[1] != Py_None) x = matrix_like(a[1], "x", dy);
-        else k = read_copy(a[2], a[3], dy.device);
+        else k = read_copy(a[2], a[3], dy.rows, dy.cols, dy.device);
         const Params p = params(a[4], a[7], dy);
         const float *mean = statistics(a[5], "mean", dy), *rstd = statistics(a[6], "rstd", dy);
         const at::ScalarType type = dtype_of(a[10], x.type, "dx_dtype");
@@ -340,7 +352,7 @@ PyObject *activation_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         Matrix h = {nullptr, LRBI_Y_BF16, da.rows, da.cols, da.cols, da.device, da.type};
         Copy k;
         if (a[1] != Py_None) h = matrix_like(a[1], "h", da);
-        else k = read_copy(a[2], a[3], da.device);
+        else k = read_copy(a[2], a[3], da.rows, da.cols, da.device);
         const int act = (int)PyLong_AsLong(a[4]);
         const int restore = PyObject_IsTrue(a[5]);
         if (restore < 0) throw Raised();
@@ -361,14 +373,19 @@ PyObject *w4_gemv(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     CALL("w4_gemv", 8) {
         const at::Tensor &packed = tensor(a[0], "packed"), &meta = tensor(a[1], "meta"), &X = tensor(a[5], "X");
-        const int rows = (int)PyLong_AsLong(a[2]), cols = (int)PyLong_AsLong(a[3]), group = (int)PyLong_AsLong(a[4]);
+        const int64_t rows = whole_number(a[2]), cols = whole_number(a[3]), group = whole_number(a[4]);
+        if (packed.scalar_type() != at::kInt || meta.scalar_type() != at::kInt || !packed.is_cuda() || !packed.is_contiguous() || !meta.is_contiguous())
+            throw BadType("4-bit weights are contiguous CUDA tensors of int32");
+        if (rows < 1 || rows > INT_MAX || cols < 1 || cols > LRBI_MAX_ROW_COLS || group < 1 || group > INT_MAX || meta.device() != packed.device() ||
+            (size_t)packed.numel() != lrbi_w4_packed_words((int)rows, (int)cols) || (size_t)meta.numel() != lrbi_w4_meta_words((int)rows, (int)cols, (int)group))
+            throw BadValue("the 4-bit weights do not have the size of their layer");
         if (!X.is_cuda() || X.scalar_type() != at::kBFloat16 || !X.is_contiguous()) throw BadType("X must be a contiguous CUDA tensor of dtype torch.bfloat16");
         if (X.dim() != 2 || X.size(1) != cols || X.device() != packed.device() || X.size(0) > INT_MAX) throw BadValue("X must be [batch, cols] on the weights' device");
         const at::ScalarType type = dtype_of(a[6], at::kBFloat16, "y_dtype");
         const int batch = (int)X.size(0);
         const Call c(X.device(), a[7]);
         at::Tensor Y = c.make({batch, rows}, type);
-        check(lrbi_w4_gemv(static_cast<const uint32_t *>(packed.data_ptr()), static_cast<const uint32_t *>(meta.data_ptr()), rows, cols, group,
+        check(lrbi_w4_gemv(static_cast<const uint32_t *>(packed.data_ptr()), static_cast<const uint32_t *>(meta.data_ptr()), (int)rows, (int)cols, (int)group,
                            static_cast<const uint16_t *>(X.data_ptr()), batch, Y.data_ptr(), type_code(type), c.handle()),
               "lrbi_w4_gemv");
         return THPVariable_Wrap(std::move(Y));

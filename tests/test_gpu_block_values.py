@@ -116,3 +116,50 @@ def test_rstd_of_variances_that_are_zero_or_tiny(rows, cols):
     assert (mean == 0).all()
     want = (3 * 2.0 ** -149) ** -0.5
     assert ((rstd.double() / want - 1).abs() <= 2.0 ** -20).all()
+
+
+def test_sizes_of_copies_and_weights_are_checked_by_the_calls():
+    """A Checkpoint's or W4Weights' fields may have changed since it was made: calls look at the arrays that they are given."""
+    b = _b()
+    x = torch.randn((6, 300), device="cuda")
+    gamma = torch.ones(300, device="cuda")
+    _, mean, rstd = b.lrbi_layer_norm(x, gamma)
+
+    def copies():
+        yield {"cols": 305}                       # (301 has the same arrays)
+        yield {"rows": 7}
+        yield {"cols": 4096}
+        yield {"rows": -1}
+        yield {"cols": 1 << 40}
+        good = b.lrbi_checkpoint_store(x)
+        yield {"q": good.q[:5]}
+        yield {"q": good.q.view(torch.uint8)}
+        yield {"q": good.q.t()}
+        yield {"q": good.q.cpu()}
+        yield {"scale": good.scale[:, :2].contiguous()}
+        yield {"scale": good.scale.double()}
+        yield {"scale": good.scale.cpu()}
+
+    before = None
+    for change in copies():
+        kept = b.lrbi_checkpoint_store(x)
+        for name, v in change.items():
+            setattr(kept, name, v)
+        before = b.launch_count()
+        with pytest.raises((ValueError, TypeError, OverflowError)):
+            b.lrbi_checkpoint_load(kept)
+        with pytest.raises((ValueError, TypeError, OverflowError)):
+            b.lrbi_layer_norm_backward(torch.ones((kept.rows if 0 < kept.rows < 9 else 6, min(kept.cols, 5000)), device="cuda"), kept, gamma, mean, rstd)
+        with pytest.raises((ValueError, TypeError, OverflowError)):
+            b.lrbi_activation_backward(torch.ones((kept.rows if 0 < kept.rows < 9 else 6, min(kept.cols, 5000)), device="cuda"), kept, "relu")
+        assert b.launch_count() == before, change
+
+    W = b.lrbi_w4_quantize((20, 64, 20, 64, 1), torch.randn((20, 64), device="cuda").bfloat16(), 64)
+    for name, v in (("rows", 33), ("cols", 65), ("group", 32), ("rows", 0), ("packed", W.packed[:-4]), ("meta", W.meta[:-4]), ("meta", W.meta.cpu()),
+                    ("packed", W.packed.float())):
+        changed = b.W4Weights(W.packed, W.meta, 20, 64, 64)
+        setattr(changed, name, v)
+        before = b.launch_count()
+        with pytest.raises((ValueError, TypeError)):
+            b.lrbi_w4_gemv(changed, torch.zeros((2, changed.cols), device="cuda").bfloat16())
+        assert b.launch_count() == before, name
