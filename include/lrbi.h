@@ -315,11 +315,11 @@ LRBI_API lrbi_status lrbi_masked_gemm_dw(const lrbi_layout *layout, const uint16
  * these calls: it retrains and serves whole networks, and they are what stands between two masked layers.)
  *
  * Matrices of these calls are [rows][cols] with unit column stride; element (r, c) is at data[r * stride + c], stride in
- * elements and at least cols, so a slice of a wider array is passed as it is.  Each has its own element type (LRBI_Y_BF16
- * or LRBI_Y_F32) and needs that type's alignment only; rows that start on 16-byte boundaries and a multiple of 8 columns
- * are read and written in vectors.  rows may be 0 (nothing is read; gradients of parameters are written as zeros), cols
- * is 1 .. LRBI_MAX_ROW_COLS.  All sums and statistics are fp32, each output is rounded once.  Outputs must not overlap
- * inputs or one another.
+ * elements, at least cols and less than 2^32 bytes, so a slice of a wider array is passed as it is.  Each has its own element
+ * type (LRBI_Y_BF16 or LRBI_Y_F32) and needs that type's alignment only; rows that start on 16-byte boundaries (32-byte ones
+ * in fp32) and a multiple of 8 columns are read and written in vectors.  rows may be 0 (nothing is read; gradients of
+ * parameters are written as zeros), cols is 1 .. LRBI_MAX_ROW_COLS.  All sums and statistics are fp32, each output is rounded
+ * once.  Outputs must not overlap inputs or one another.
  * Results of a call have the same bits every time it is made on the same GPU model.
  */
 #define LRBI_MAX_ROW_COLS (1 << 24)

@@ -46,11 +46,13 @@ bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 bool dtype_ok(int t) { return t == LRBI_Y_BF16 || t == LRBI_Y_F32; }
 bool cols_ok(int cols) { return cols >= 1 && cols <= LRBI_MAX_ROW_COLS; }
 
-// A matrix of a call: present where rows > 0, its element's alignment, rows that do not overlap.
+// A matrix of a call: present where rows > 0, its element's alignment, rows that do not overlap and whose distance in bytes is a
+// 32-bit number (kernels take a row's place as one multiply-add of 32-bit factors).
 bool matrix_ok(const void *p, int dtype, int64_t stride, int rows, int cols)
 {
-    if (!dtype_ok(dtype) || stride < cols || stride > (INT64_MAX >> 36)) return false;
-    return rows == 0 || (p && aligned(p, dtype == LRBI_Y_F32 ? 4 : 2));
+    const int size = dtype == LRBI_Y_F32 ? 4 : 2;
+    if (!dtype_ok(dtype) || stride < cols || stride > UINT32_MAX / size) return false;
+    return rows == 0 || (p && aligned(p, size));
 }
 bool floats_ok(const void *p, int n) { return n == 0 || (p && aligned(p, 4)); }
 bool copy_ok(const void *q, const void *scale, int rows) { return rows == 0 || (q && scale && aligned(q, 16) && aligned(scale, 4)); }

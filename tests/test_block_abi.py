@@ -98,3 +98,22 @@ def test_w4_meta_alignment(lib):
         off = ctypes.c_void_p(at)
         refused(lib, L.lrbi_w4_gemv, [P, P, 64, 64, 64, P, 0, P, 0, NULL], [(1, off)])        # no rows of X: nothing could be launched
         refused(lib, L.lrbi_w4_quantize, [ctypes.byref(lay), P, P, P, 64, P, P, NULL], [(6, off)])
+
+
+def test_rows_far_apart(lib):
+    """Rows may be up to 2^32 bytes apart, not more."""
+    L = lib.lib()
+    for code, size in ((0, 2), (1, 4)):
+        most = (1 << 32) // size - 1
+        store = [P, code, most, 0, 64, P, P, NULL]
+        assert L.lrbi_checkpoint_store(*store) == lib.OK
+        refused(lib, L.lrbi_checkpoint_store, store, [(2, most + 1), (2, 1 << 40), (2, (1 << 63) - 1)])
+        act = [P, code, most, 0, 64, 1, P, code, most, P, P, NULL]
+        assert L.lrbi_activation(*act) == lib.OK
+        refused(lib, L.lrbi_activation, act, [(2, most + 1), (8, most + 1)])
+        back = [P, code, most, P, code, most, NULL, NULL, 0, 64, 2, P, code, most, P, most, NULL]
+        assert L.lrbi_activation_backward(*back) == lib.OK
+        refused(lib, L.lrbi_activation_backward, back, [(2, most + 1), (5, most + 1), (13, most + 1), (15, most + 1)])
+        norm = [P, code, most, 0, 64, P, P, 1, 1e-5, P, code, most, P, P, P, P, NULL]
+        assert L.lrbi_layer_norm(*norm) == lib.OK
+        refused(lib, L.lrbi_layer_norm, norm, [(2, most + 1), (11, most + 1)])

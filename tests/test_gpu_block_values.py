@@ -163,3 +163,26 @@ def test_sizes_of_copies_and_weights_are_checked_by_the_calls():
         with pytest.raises((ValueError, TypeError)):
             b.lrbi_w4_gemv(changed, torch.zeros((2, changed.cols), device="cuda").bfloat16())
         assert b.launch_count() == before, name
+
+
+@pytest.mark.parametrize("dtype,stride", [(BF16, (1 << 30) + 8), (BF16, (1 << 30) + 5), (F32, (1 << 29) + 8), (F32, (1 << 28) + 1)])
+@pytest.mark.parametrize("cols", [264, 9000])
+def test_rows_more_than_two_gigabytes_apart(cols, dtype, stride):
+    """The same bits as side by side."""
+    b = _b()
+    base = torch.empty(stride + cols, dtype=dtype, device="cuda")
+    x = torch.as_strided(base, (2, cols), (stride, 1))
+    own = torch.randn((2, cols), device="cuda").to(dtype)
+    x.copy_(own)
+    gamma = torch.ones(cols, device="cuda")
+    got = []
+    for t in (x, own):
+        y, mean, rstd, kept = b.lrbi_layer_norm(t, gamma, checkpoint=True)
+        a, _ = b.lrbi_activation(t, "gelu", checkpoint=True)
+        got.append((y, mean, rstd, kept.q, a, b.lrbi_activation_backward(t, t, "silu"), *b.lrbi_layer_norm_backward(t, t, gamma, mean, rstd, dres=t),
+                    b.lrbi_checkpoint_store(t).q))
+    if stride % 8 == 0:                 # both are whole vectors: sums in the same order
+        assert all(torch.equal(p, q) for p, q in zip(*got))
+    else:
+        assert all(torch.equal(got[0][i], got[1][i]) for i in (3, 4, 5, -1))
+        assert all((p.float() - q.float()).abs().max() <= 2.0 ** -7 * q.float().abs().max() for p, q in zip(*got))
