@@ -238,10 +238,9 @@ __device__ __forceinline__ int kept_lane() { return __shfl_sync(0xFFFFFFFFu, thr
 __device__ __forceinline__ int kept(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }      // what is the same in all lanes
 
 // Asynchronous copies into shared memory: later rows are under way without registers to wait for them.
-__device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)   // bytes: 4, 8 or 16
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, int bytes)   // bytes: 4 or 16
 {
     if (bytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-    else if (bytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy_async_if(bool on, uint32_t to, const void *from)      // 16 bytes; a predicate, not a branch
