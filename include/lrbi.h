@@ -376,9 +376,9 @@ LRBI_API lrbi_status lrbi_layer_norm_backward(const void *dy, int32_t dy_dtype, 
  *       LRBI_ACT_RELU max(h, 0)      LRBI_ACT_GELU h * Phi(h), Phi the normal distribution      LRBI_ACT_SILU h / (1 + exp(-h))
  * lrbi_activation_backward: dh = da * act'(h), from h, or (h NULL) from its 8-bit copy; `a`, in da's type, or NULL,
  * receives act(h) again, for the weight gradient of the layer that it went into.  At h = 0 relu has slope 0.
- * Before it is rounded to its output's type a result is off by at most 2^-20 (1 + h^2 / 8) of itself for gelu (2^-13 for
- * an output in bf16) and 2^-20 (1 + |h|) for silu (below 2^-100 it may come as 0), a slope by as much of the larger of its
- * two terms.
+ * Before it is rounded to its output's type a result is off by at most 2^-20 (1 + h^2 / 8) of itself for gelu (2^-13 more
+ * for an output in bf16) and 2^-20 (1 + |h|) for silu (below 2^-100 it may come as 0), a slope by as much of the larger of
+ * its two terms.
  * An infinite h gives what the formula gives: +inf for +inf; for -inf 0 (relu) or NaN (gelu, silu: infinity times zero); the
  * slopes of gelu and silu are NaN there.
  */
@@ -410,8 +410,10 @@ LRBI_API lrbi_status lrbi_activation_backward(const void *da, int32_t da_dtype, 
  *           2^-130, whose s is rounded to 0) has s = 0, z = 8; a kept weight that is not finite, or a range beyond fp32, gives
  *           s = NaN.  What the array holds at pruned places is not looked at.  ip, iz: the layer's packed factors, or both
  *           NULL (nothing is pruned; only rows and cols of the layout are looked at).
+ *           Columns up to 65535 * 128; LRBI_ERR_UNSUPPORTED beyond.
  * lrbi_w4_gemv  Y [batch][rows] (bf16 or fp32) = X W^T for X [batch][cols] bf16, contiguous, sums in fp32.  Made for a few
- *           rows of X (up to 16 go through the weights together); batch may be 0.
+ *           rows of X: up to 16 go through the weights together, and each further 16 read them again.  batch may be 0, and up
+ *           to 16 * 65535; LRBI_ERR_UNSUPPORTED beyond.
  */
 LRBI_API size_t lrbi_w4_packed_words(int32_t rows, int32_t cols);             /* RT*U*128; 0 if a size is out of range */
 LRBI_API size_t lrbi_w4_meta_words(int32_t rows, int32_t cols, int32_t group); /* RT*G*16; 0 also for other groups      */

@@ -492,7 +492,8 @@ def _native():
 
 
 class Checkpoint:
-    """A matrix kept in 8 bits: q [rows, pitch] int8, scale [rows, groups] float32 (one per CHECKPOINT_GROUP columns of a row)."""
+    """A matrix kept in 8 bits: q [rows, pitch] int8, scale [rows, groups] float32 (one per CHECKPOINT_GROUP columns of a row).
+    Where a call made it, both lie in one allocation: holding either, or saving it with torch.save, keeps both."""
 
     __slots__ = ("q", "scale", "rows", "cols")
 
@@ -548,7 +549,8 @@ def lrbi_checkpoint_load(kept: Checkpoint, dtype=torch.bfloat16, stream=None) ->
 
 def lrbi_layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor | None = None, eps: float = 1e-5, y_dtype=None,
                     checkpoint: bool = False, stream=None):
-    """Layer norm over the columns of x [rows, cols].  Returns (y, mean, rstd), and the 8-bit copy of x with checkpoint=True."""
+    """Layer norm over the columns of x [rows, cols].  Returns (y, mean, rstd), and the 8-bit copy of x with checkpoint=True.
+    mean and rstd lie in one allocation (clone one to keep or save it by itself)."""
     out = _native().layer_norm(x, gamma, beta, eps, y_dtype, checkpoint, stream)
     return (*out[:3], Checkpoint._of(out[3], out[4], *x.shape)) if checkpoint else out
 
@@ -558,7 +560,7 @@ def lrbi_layer_norm_backward(dy: torch.Tensor, x, gamma: torch.Tensor, mean: tor
                              stream=None):
     """Gradients of the layer norm: x is the forward input or its Checkpoint.  Returns (dx, dgamma, dbeta), dgamma and dbeta in
     fp32, and the forward result again with restore=True (in dy's type; pass the beta of the forward pass).  dres is added to dx,
-    which has x's type, or dy's where x is a Checkpoint, unless dx_dtype says otherwise."""
+    which has x's type, or dy's where x is a Checkpoint, unless dx_dtype says otherwise.  dgamma and dbeta lie in one allocation."""
     return _native().layer_norm_backward(dy, *_kept_or_rows(x, dy, "x"), gamma, mean, rstd, beta, dres, restore, dx_dtype, stream)
 
 

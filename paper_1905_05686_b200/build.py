@@ -30,7 +30,8 @@ def torch_version() -> str | None:
     if where is None:
         return None
     with open(os.path.join(where, "version.py")) as f:
-        return re.search(r"^__version__ = ['\"](.+)['\"]", f.read(), re.M).group(1)
+        found = re.search(r"^__version__ = ['\"](.+)['\"]", f.read(), re.M)
+    return found.group(1) if found else "unknown"
 
 
 def calls_path() -> str | None:

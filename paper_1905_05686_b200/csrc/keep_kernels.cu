@@ -6,9 +6,9 @@
 //
 // One pass, and memory bounds it: 4096 x 16384 bf16, gelu forward with the copy and backward from it, 137 us of 124 at the
 // rate of a plain copy; 16384 x 4096 bf16: stored in 34.4 us (31.1), loaded in 33.4 (31.1), gelu 43.7 (41.0), with the copy
-// 60 (51.6); fp32 within 4% throughout.  The arithmetic of gelu and of the copy takes nearly as long as memory in bf16, which
+// 60 (51.6); fp32: stored in 51.2 us (51.5), loaded in 53.6, gelu 82.3 (82.0), with the copy 93.9 (92.6).  The arithmetic of gelu and of the copy takes nearly as long as memory in bf16, which
 // is why values go in pairs and four groups share one division (a chunk at a time the copy was stored in 46 us).  Rows that
-// are not whole vectors are bound by their accesses, one a value: 4096 x 8191 bf16, gelu step, 110 us (62).
+// are not whole vectors are bound by their accesses, one a value: 4096 x 8191 bf16, gelu step, 108 us (62).
 #include "row_ops.cuh"
 
 namespace lrbi {

@@ -535,7 +535,8 @@ __global__ void __launch_bounds__(HELD_THREADS<NV>, 1) norm_backward_held_kernel
     }
 }
 
-// Rows beyond the registers of a block: sums over rows in memory, a thread's own columns; dy and x are read twice.
+// Rows beyond the registers of a block: sums over rows in memory, a thread's own columns, read and written for every row; dy
+// and x are read twice.  2000 x 20001 bf16 235 us (floor 37), 2000 x 32768 690 (60): the sums' traffic, 16 bytes a value.
 template <int DY, int SRC, bool STRIDED>
 __global__ void __launch_bounds__(1024) norm_backward_wide_kernel(NormBackward a)
 {

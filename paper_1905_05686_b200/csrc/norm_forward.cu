@@ -9,9 +9,9 @@
 //         sums' shuffles are paid once per row, gamma and beta come from shared memory without bank conflicts, and warps
 //         run apart from one another, so that loads, arithmetic and stores of different rows overlap.
 //   row   few rows: latency counts, a block has a row, a lane one or two chunks.
-//   wide  rows beyond the registers of a block: read three times, mostly from L2.
+//   wide  rows beyond the registers of a block: read three times, mostly from L2.  2000 x 32768 bf16 111 us (floor 40).
 //
-// Bound, tall: memory and issue about alike (10 instructions a value in bf16).  16384 x 4096 bf16 47.5 us (floor 41), with the
+// Bound, tall: memory and issue about alike (12 instructions a value in bf16).  16384 x 4096 bf16 47.5 us (floor 41), with the
 // copy 61 (51.6); 4096 x 4096 14.9 (10.3): three rounds of rows and 4 us to begin and to drain; 8192 x 4096 fp32 51 (41); 8192 x
 // 4097 bf16, an access a value, 47.6 (20.5).  row: 2.3 us for one token of 4096, which is the launch, two waits for memory and
 // two sums over a block.
@@ -383,7 +383,7 @@ lrbi_status forward_launch(NormForward a, cudaStream_t s)
     a.warps = (spans + most - 1) / most;
     // Few rows leave most of the GPU idle with a warp each, and the parameters' way into shared memory is a good part of the
     // time: then a block takes a row.  Rows of two warps: 300 x 4096 3.9 us (two warps: 7.2), 700 6.5, 900 8.1 (6.7), 1300
-    // 9.7 (7.3); of one: 590 x 1024 2.5 (2.8), 1200 3.7 (4.0), 1500 x 1157 6.6 (5.5), 2000 x 1024 5.4 (4.0).
+    // 9.7 (7.3); of one: 590 x 1024 2.5 (2.8); at the change, 1183 and 1184 rows: x 1024 3.33 (3.01), x 1157 4.35 (4.22).
     const bool few = (long long)a.rows * a.warps < (a.warps > 1 ? 10 : 8) * NORM_SMS;
     if (spans > 64) return norm_launch(norm_forward_wide_kernel<SRC, STRIDED>, a.rows, dim3(1024), 0, s, a);
     if (few) {

@@ -5,8 +5,9 @@
 //   vector    a lane has 8 neighbouring columns: one access of 16 bytes in bf16, of 32 in fp32.  For rows that start on
 //             boundaries of that many bytes and hold a multiple of 8 columns.
 //   strided   a lane has columns lane, lane + 32, ..: any alignment and any width; an access of the warp is 64 or 128
-//             neighbouring bytes.  (Aligned vectors moved into place by shuffles and funnel shifts were built too: 35
-//             instructions a value in the layer norm against 9.)
+//             neighbouring bytes.  (Aligned vectors moved into place by shuffles and funnel shifts a value were built too: 35
+//             instructions a value in the layer norm against 9.  A leaner form, which settles the shift once for a whole row,
+//             was not built.)
 // Either way a group of 128 columns (what shares a scale in 8 bits) lies within a span.
 #pragma once
 #include <type_traits>

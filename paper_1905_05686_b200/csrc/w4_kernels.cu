@@ -130,10 +130,14 @@ template <int GROUP, int NT, int TILES, bool VEC> constexpr int W4_SLOT = TILES 
 // add up in shared memory, block by block and then over the cluster, in a fixed order that depends on the layer alone.  A step's
 // weights come through a ring of asynchronous copies, the activations too or a step ahead in registers.  NT: tiles of 8 batch rows.
 //
-// Bound: on paper the weights' bytes (16384 x 16384, one row: 21.5 us).  Measured 33.7 us, and 30.0 with every load taken out:
-// turning four bits into bf16 takes a shift, a logic operation and a subtraction for two weights, and the logic pipe issues
-// every second cycle.  (Leaving the 128 + z in and taking it out of the sums would save the subtraction, and pruned weights
-// would no longer be exact zeros.)  The smaller layers add about 2 us of launch and first latency.
+// Bound: on paper the weights' bytes (16384 x 16384, one row: 21.5 us).  Measured 33.7 us, and 30.0 with every load taken out.
+// No one unit is full: the kernel issues in half of the slots and waits for memory longest.  What is known to cost time:
+// turning four bits into bf16 (a shift, a logic operation and a subtraction for two weights; leaving the 128 + z in and taking
+// it out of the sums would save the subtraction, and pruned weights would no longer be exact zeros), and the cut in whole
+// tiles: 256 blocks, as the common sizes have, give 108 SMs two and 40 one, so that the busiest has 1 / 0.865 of the mean, in
+// the 30.0 us too.  The smaller layers add about 2 us of launch and first latency.  Activations that are not whole vectors
+// (columns not a multiple of 8, or X not on a 16-byte boundary) are loaded a value at a time: 4096 x 9216, one row, 16.3 us
+// (7.4), 16384 x 4096, eight rows, 26.6 (12.1).
 template <int GROUP, int NT, int TILES, bool VEC>
 __global__ void __launch_bounds__(32 * W4_WARPS, NT > 1 || TILES > 1 ? 2 : VEC ? 3 : 4) w4_gemv_kernel(W4 w, const uint16_t *__restrict__ X, int batch, void *__restrict__ Y, int y_dtype, int sharing)
 {

@@ -29,6 +29,7 @@ class PrunedLayer:
     Wt: torch.Tensor | None = None      # transposed, for the gradient of the layer's input
 
     def refresh(self):
+        """To be called whenever W has changed: dx reads the transposed weights."""
         self.Wt = B.lrbi_transpose_bf16(self.W, self.Wt)
 
     def __call__(self, X):
