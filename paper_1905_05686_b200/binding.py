@@ -208,6 +208,8 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     current = torch.cuda.current_stream(device)
+    if not isinstance(stream, torch.cuda.Stream):        # another library's, with the handle in cuda_stream
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     t.record_stream(current)

@@ -152,6 +152,18 @@ def test_the_current_stream_given_by_name():
     assert torch.equal(a, b.lrbi_activation(x, "silu"))
 
 
+def test_streams_that_torch_did_not_make():
+    """Calls that take a stream by its handle go on taking any object that has one."""
+    b = _b()
+    W = torch.randn((64, 96), device="cuda").bfloat16()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for handle in (side.cuda_stream, torch.cuda.current_stream().cuda_stream):
+        got = b.lrbi_transpose_bf16(W, stream=types.SimpleNamespace(cuda_stream=handle))
+        torch.cuda.synchronize()
+        assert torch.equal(got, W.t())
+
+
 def test_streams_of_another_device_are_refused():
     b = _b()
     x = torch.zeros((4, 40), device="cuda")
