@@ -422,6 +422,77 @@ LRBI_API lrbi_status lrbi_w4_quantize(const lrbi_layout *layout, const uint16_t 
 LRBI_API lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, int32_t rows, int32_t cols, int32_t group,
                                   const uint16_t *X, int32_t batch, void *Y, int32_t y_dtype, void *stream);
 
+/*
+ * Rows in 8-bit integers with a scale each, and their product: a layer's channels and a batch's tokens, of any number.
+ *       top = max |v|,   scale = top / 127,   q = round_to_even(v * (127 / top))             (each step one fp32 operation)
+ *       Y[b][o] = (float(sum_i q_X[b][i] * q_W[o][i]) * scale_X[b]) * scale_W[o],            rounded once to Y's type
+ * The sum is a whole number and exact.  A row whose top is below 2^-118 is kept as zeros (scale 0); one that holds a NaN or an
+ * infinity has scale NaN and q = 0, so that what it is multiplied into is NaN.
+ *   q      device, int8 (-127 .. 127), [rows][lrbi_i8_pitch(cols)], 16-byte aligned; bytes past the last column are 0 (the calls
+ *          that make q write them, the product relies on them)
+ *   scale  device, fp32, [rows]
+ * cols is 1 .. LRBI_I8_MAX_COLS, up to which no sum leaves 32 bits.
+ * lrbi_i8_quantize  W [rows][cols] bf16, contiguous -> q, scale of its rows.  ip, iz: the layer's packed factors, or both NULL
+ *           (nothing is pruned; only rows and cols of the layout are looked at).  The range is that of the kept weights, pruned
+ *           ones are exactly zero, and what the array holds at their places is not looked at.
+ * lrbi_i8_tokens    x [rows][cols] (bf16 or fp32, rows x_stride elements apart) -> q, scale of the rows of act(x); act: LRBI_ACT_*,
+ *           or LRBI_ACT_NONE for x itself.  act(x) is taken in fp32 (as far off as
+ *           lrbi_activation states, for x in bf16 as for outputs in bf16) and not rounded.
+ * lrbi_i8_gemm      Y [batch][rows], contiguous.  batch may be 0.
+ */
+#define LRBI_I8_MAX_COLS (1 << 17)
+enum { LRBI_ACT_NONE = -1 };
+LRBI_API int32_t lrbi_i8_pitch(int32_t cols);          /* cols rounded up to 16; 0 for cols out of range */
+LRBI_API lrbi_status lrbi_i8_quantize(const lrbi_layout *layout, const uint16_t *W, const uint32_t *ip, const uint32_t *iz,
+                                      int8_t *q, float *scale, void *stream);
+LRBI_API lrbi_status lrbi_i8_tokens(const void *x, int32_t x_dtype, int64_t x_stride, int32_t rows, int32_t cols, int32_t act,
+                                    int8_t *q, float *scale, void *stream);
+LRBI_API lrbi_status lrbi_i8_gemm(const int8_t *w_q, const float *w_scale, int32_t rows, int32_t cols, const int8_t *x_q,
+                                  const float *x_scale, int32_t batch, void *Y, int32_t y_dtype, void *stream);
+
+/*
+ * Between two blocks: the norm behind a block, its gate, the residual scale and the norm before the next block, in one pass.
+ *       z   = norm(f) * post_gamma + post_beta
+ *       out = residual_scale * x + gate * z
+ *       u   = norm(out) * gamma + beta                  of out as it is stored
+ *   x, out        the residual stream, x_dtype;  f (what the block gave) and u: f_dtype.  A bf16 stream goes with a bf16 f.
+ *   norm          kind LRBI_NORM_LAYER: (v - mean) / sqrt(mean of (v - mean)^2 + eps);  LRBI_NORM_RMS: v / sqrt(mean of v^2 + eps)
+ *   vectors       device, [cols], param_dtype each.  post_gamma NULL: z = f.  gate NULL: 1.  gamma NULL: no second norm, u and
+ *                 u_q are NULL.  post_beta, beta: with their gamma only, or NULL
+ *   u             or, for the next layer's 8-bit product, u_q and u_scale (as lrbi_i8_tokens makes them, of u before it is
+ *                 rounded); one of the two where gamma is given
+ *   stats         device, fp32, [4][rows], for the backward pass, or NULL: mean and 1 / root of out, mean and 1 / root of f (0 and 1
+ *                 where there is no norm, means 0 for LRBI_NORM_RMS)
+ *
+ * lrbi_residual_norm_backward: du and dout, the gradients of u and of out (the residual stream's), give
+ *       g  = du * gamma,  n = (out - mean) / root,  ds = dout + (g - mean_c(g) - n * mean_c(g * n)) / root
+ *       dx = residual_scale * ds,   df = the gradient of f,   sums over rows for the vectors            (RMS: no mean_c(g) term)
+ *   dout          x_dtype, or NULL: nothing else reads out.  du: f_dtype; NULL where gamma is
+ *   out, stats    as the forward pass left them; out is not read where gamma is NULL
+ *   dgamma .. dgate  device, fp32, [cols]; any may be NULL, and those of vectors that the call does not have are
+ *   workspace     device, lrbi_residual_norm_backward_workspace(rows, cols) bytes, 16-byte aligned, scratch for the call
+ * cols is 1 .. LRBI_MAX_RESIDUAL_COLS.  Matrices, alignment, rows of 0 and repeatability are as for lrbi_layer_norm.
+ */
+#define LRBI_MAX_RESIDUAL_COLS 32768
+enum { LRBI_NORM_LAYER = 0, LRBI_NORM_RMS = 1 };
+typedef struct {
+    int32_t rows, cols;
+    int32_t kind;
+    int32_t x_dtype, f_dtype, param_dtype;
+    float residual_scale, eps;                 /* eps of both norms; the backward pass does not look at it */
+    const void *gamma, *beta, *post_gamma, *post_beta, *gate;
+} lrbi_residual;
+LRBI_API lrbi_status lrbi_residual_norm(const lrbi_residual *how, const void *x, int64_t x_stride, const void *f, int64_t f_stride,
+                                        void *out, int64_t out_stride, void *u, int64_t u_stride, int8_t *u_q, float *u_scale,
+                                        float *stats, void *stream);
+LRBI_API size_t lrbi_residual_norm_backward_workspace(int32_t rows, int32_t cols);
+LRBI_API lrbi_status lrbi_residual_norm_backward(const lrbi_residual *how, const void *du, int64_t du_stride, const void *dout,
+                                                 int64_t dout_stride, const void *out, int64_t out_stride, const void *f,
+                                                 int64_t f_stride, const float *stats, void *dx, int64_t dx_stride, void *df,
+                                                 int64_t df_stride, float *dgamma, float *dbeta, float *dpost_gamma,
+                                                 float *dpost_beta, float *dgate, void *workspace, size_t workspace_bytes,
+                                                 void *stream);
+
 /* Which kernel LRBI_ALGO_AUTO would run for this layout and batch (an LRBI_ALGO_* value). */
 LRBI_API int32_t lrbi_masked_gemm_choice(const lrbi_layout *layout, int32_t batch);
 

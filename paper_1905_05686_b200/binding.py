@@ -51,6 +51,12 @@ class TileRanks(ctypes.Structure):
     _fields_ = [("ranks", ctypes.c_void_p), ("ip_offset", ctypes.c_void_p), ("iz_offset", ctypes.c_void_p)]
 
 
+class Residual(ctypes.Structure):
+    """lrbi_residual: sizes, types, numbers and vectors of a call between two blocks."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "kind", "x_dtype", "f_dtype", "param_dtype")] + [
+        (n, ctypes.c_float) for n in ("residual_scale", "eps")] + [(n, ctypes.c_void_p) for n in ("gamma", "beta", "post_gamma", "post_beta", "gate")]
+
+
 class Layout(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("tile_rows", ctypes.c_int32),
                 ("tile_cols", ctypes.c_int32), ("rank", ctypes.c_int32)]
@@ -151,6 +157,21 @@ def lib():
         L.lrbi_w4_quantize.restype = i32
         L.lrbi_w4_gemv.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, i32, vp]
         L.lrbi_w4_gemv.restype = i32
+        L.lrbi_i8_pitch.argtypes = [i32]
+        L.lrbi_i8_pitch.restype = i32
+        L.lrbi_i8_quantize.argtypes = [lp, vp, vp, vp, vp, vp, vp]
+        L.lrbi_i8_quantize.restype = i32
+        L.lrbi_i8_tokens.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp, vp]
+        L.lrbi_i8_tokens.restype = i32
+        L.lrbi_i8_gemm.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, vp]
+        L.lrbi_i8_gemm.restype = i32
+        rp = ctypes.POINTER(Residual)
+        L.lrbi_residual_norm.argtypes = [rp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
+        L.lrbi_residual_norm.restype = i32
+        L.lrbi_residual_norm_backward_workspace.argtypes = [i32, i32]
+        L.lrbi_residual_norm_backward_workspace.restype = sz
+        L.lrbi_residual_norm_backward.argtypes = [rp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.lrbi_residual_norm_backward.restype = i32
         L.lrbi_launch_count.argtypes = []
         L.lrbi_launch_count.restype = ctypes.c_uint64
         L.lrbi_device_status.argtypes = [i32]
@@ -471,7 +492,7 @@ def lrbi_masked_gemm_static(layer, W: torch.Tensor, ip: torch.Tensor, iz: torch.
 
 
 # ---------------------------------------------------------------------------------------------
-# Around the layers: layer norm, 8-bit copies, the nonlinearity, 4-bit weights
+# Around the layers: layer norm, 8-bit copies, the nonlinearity, 4-bit weights, 8-bit products, what stands between two blocks
 # ---------------------------------------------------------------------------------------------
 CHECKPOINT_GROUP = 128
 ACTIVATIONS = {"relu": 0, "gelu": 1, "silu": 2}
@@ -631,6 +652,116 @@ def lrbi_w4_quantize(layer, W: torch.Tensor, group: int = 128, ip: torch.Tensor 
 def lrbi_w4_gemv(weights: W4Weights, X: torch.Tensor, y_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
     """Y [batch, rows] = X W^T for X [batch, cols] bf16 and 4-bit weights; made for a few rows of X."""
     return _native().w4_gemv(weights.packed, weights.meta, weights.rows, weights.cols, weights.group, X, y_dtype, stream)
+
+
+I8_MAX_COLS = 1 << 17
+
+
+class I8Rows:
+    """Rows in 8-bit integers with a scale each (lrbi.h): q [rows, pitch] int8, its rows' bytes past the last column 0, and
+    scale [rows] float32.  A layer's channels (I8Weights) and a batch's tokens (I8Tokens) are kept alike.
+    Where lrbi_i8_tokens made them, both lie in one allocation."""
+
+    __slots__ = ("q", "scale", "rows", "cols")
+
+    def __init__(self, q: torch.Tensor, scale: torch.Tensor, rows: int, cols: int):
+        if not 1 <= cols <= I8_MAX_COLS or rows < 0:
+            raise ValueError("rows in 8 bits have 1 to %d columns" % I8_MAX_COLS)
+        pitch = (cols + 15) // 16 * 16
+        _dev(q, torch.int8, "q")
+        _dev(scale, torch.float32, "scale")
+        if q.shape != (rows, pitch) or scale.shape != (rows,) or q.device != scale.device:
+            raise ValueError("q must be [rows, %d] and scale [rows] on one CUDA device" % pitch)
+        self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
+
+    @classmethod
+    def _of(cls, q, scale, rows, cols):
+        rows8 = object.__new__(cls)
+        rows8.q, rows8.scale, rows8.rows, rows8.cols = q, scale, rows, cols
+        return rows8
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    @property
+    def nbytes(self):
+        return self.q.numel() + 4 * self.scale.numel()
+
+
+I8Weights = I8Tokens = I8Rows
+
+
+def lrbi_i8_quantize(layer, W: torch.Tensor, ip: torch.Tensor | None = None, iz: torch.Tensor | None = None, stream=None) -> I8Weights:
+    """W [rows, cols] bf16 in 8 bits, a scale for each row; with the layer's packed factors, pruned weights are exactly zero."""
+    lay = Layout.of(layer)
+    L = lib()
+    if tuple(W.shape) != (lay.rows, lay.cols):
+        raise ValueError("W shape does not match the layout")
+    if not 1 <= lay.cols <= I8_MAX_COLS:
+        raise ValueError("rows in 8 bits have 1 to %d columns" % I8_MAX_COLS)
+    if (ip is None) != (iz is None):
+        raise ValueError("ip and iz come together")
+    if ip is not None and (ip.numel() != L.lrbi_packed_ip_words(ctypes.byref(lay)) or iz.numel() != L.lrbi_packed_iz_words(ctypes.byref(lay))):
+        raise ValueError("packed factor sizes do not match the layout")
+    w = _dev(W, torch.bfloat16, "W")
+    factors = [None if t is None else _dev(t, torch.int32, what) for t, what in ((ip, "ip"), (iz, "iz"))]
+    q = _empty((lay.rows, L.lrbi_i8_pitch(lay.cols)), torch.int8, W.device, stream)
+    scale = _empty((lay.rows,), torch.float32, W.device, stream)
+    rc = L.lrbi_i8_quantize(ctypes.byref(lay), w, *factors, q.data_ptr(), scale.data_ptr(), _stream_ptr(stream))
+    if rc != OK:
+        raise LrbiError(rc, "lrbi_i8_quantize")
+    return I8Weights(q, scale, lay.rows, lay.cols)
+
+
+def lrbi_i8_tokens(x: torch.Tensor, act: str | None = None, stream=None) -> I8Tokens:
+    """The rows of x [rows, cols] (bf16 or fp32), or of act(x), in 8 bits."""
+    q, scale = _native().i8_tokens(x, -1 if act is None else _act(act), stream)
+    return I8Tokens._of(q, scale, *x.shape)
+
+
+def lrbi_i8_gemm(weights: I8Weights, tokens: I8Tokens, y_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """Y [tokens, rows] = tokens W^T, both in 8 bits: sums of whole numbers, exact, times a scale of each token and channel."""
+    if not isinstance(weights, I8Rows) or not isinstance(tokens, I8Rows):
+        raise TypeError("weights and tokens must be I8Weights and I8Tokens")
+    if weights.cols != tokens.cols:
+        raise ValueError("the tokens must have as many columns as the weights")
+    return _native().i8_gemm(weights.q, weights.scale, weights.rows, weights.cols, tokens.q, tokens.scale, tokens.rows, y_dtype, stream)
+
+
+NORMS = {"layer": 0, "rms": 1}
+
+
+def _kind(kind):
+    code = NORMS.get(kind)
+    if code is None:
+        raise ValueError("kind must be one of %s" % ", ".join(sorted(NORMS)))
+    return code
+
+
+def lrbi_residual_norm(x: torch.Tensor, f: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tensor | None = None, *,
+                       post_gamma: torch.Tensor | None = None, post_beta: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                       residual_scale: float = 1.0, eps: float = 1e-5, kind: str = "layer", tokens: bool = False, stream=None):
+    """What stands between two blocks, in one pass, for the residual stream x and the block's result f, [rows, cols]:
+
+        out = residual_scale * x + gate * z,   z = norm(f) * post_gamma + post_beta, or f without post_gamma
+        u = norm(out) * gamma + beta           (norm: kind "layer" or "rms")
+
+    Returns (out, u, stats): out in x's type, u in f's (None without gamma), stats float32 [4, rows] for the backward pass.  With
+    tokens=True u comes as I8Tokens for the next layer's 8-bit product, and stats is None."""
+    out, u, stats, q, scale = _native().residual_norm(x, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, eps, _kind(kind), tokens, stream)
+    return out, (I8Tokens._of(q, scale, *x.shape) if tokens else u), stats
+
+
+def lrbi_residual_norm_backward(du: torch.Tensor | None, dout: torch.Tensor | None, out: torch.Tensor | None, f: torch.Tensor,
+                                gamma: torch.Tensor | None, beta: torch.Tensor | None = None, *, post_gamma: torch.Tensor | None = None,
+                                post_beta: torch.Tensor | None = None, gate: torch.Tensor | None = None, residual_scale: float = 1.0,
+                                stats: torch.Tensor | None = None, kind: str = "layer", stream=None):
+    """Gradients of lrbi_residual_norm from those of u (None without gamma) and of out (None: nothing else reads it), with the out
+    and stats that it returned and the arguments that it was given.  Returns (dx, df, grads): dx in out's type, df in f's, and
+    fp32 gradients of the vectors that were given, by name ("gamma", "beta", "post_gamma", "post_beta", "gate"; one allocation)."""
+    dx, df, *vectors = _native().residual_norm_backward(du, dout, out, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, stats, _kind(kind), stream)
+    return dx, df, {name: g for name, g in zip(("gamma", "beta", "post_gamma", "post_beta", "gate"), vectors) if g is not None}
 
 
 class HostLayer:

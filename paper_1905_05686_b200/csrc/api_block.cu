@@ -56,6 +56,29 @@ bool matrix_ok(const void *p, int dtype, int64_t stride, int rows, int cols)
 }
 bool floats_ok(const void *p, int n) { return n == 0 || (p && aligned(p, 4)); }
 bool copy_ok(const void *q, const void *scale, int rows) { return rows == 0 || (q && scale && aligned(q, 16) && aligned(scale, 4)); }
+bool i8_cols_ok(int cols) { return cols >= 1 && cols <= LRBI_I8_MAX_COLS; }
+bool rows8_ok(const void *q, const void *scale) { return q && scale && aligned(q, 16) && aligned(scale, 4); }
+
+// What both passes between two blocks ask of a call.
+bool residual_ok(const lrbi_residual *h)
+{
+    if (!h || h->rows < 0 || h->cols < 1 || h->cols > LRBI_MAX_RESIDUAL_COLS || (h->kind != LRBI_NORM_LAYER && h->kind != LRBI_NORM_RMS)) return false;
+    if (!dtype_ok(h->x_dtype) || !dtype_ok(h->f_dtype) || !dtype_ok(h->param_dtype) || (h->x_dtype == LRBI_Y_BF16 && h->f_dtype != LRBI_Y_BF16)) return false;
+    if ((h->beta && !h->gamma) || (h->post_beta && !h->post_gamma) || !(h->eps >= 0.f)) return false;
+    for (const void *v : {h->gamma, h->beta, h->post_gamma, h->post_beta, h->gate})
+        if (v && !aligned(v, h->param_dtype == LRBI_Y_F32 ? 4 : 2)) return false;
+    return true;
+}
+JoinArgs join_args(const lrbi_residual *h)
+{
+    JoinArgs n = {};
+    n.rows = h->rows; n.cols = h->cols;
+    n.rms = h->kind == LRBI_NORM_RMS;
+    n.x_dtype = h->x_dtype; n.f_dtype = h->f_dtype; n.param_dtype = h->param_dtype;
+    n.residual_scale = h->residual_scale; n.eps = h->eps;
+    n.gamma = h->gamma; n.beta = h->beta; n.post_gamma = h->post_gamma; n.post_beta = h->post_beta; n.gate = h->gate;
+    return n;
+}
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
 
 }  // namespace
@@ -209,6 +232,90 @@ lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, int32_t r
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     if (batch == 0) return LRBI_OK;
     return launch_w4_gemv(packed, meta, rows, cols, group, X, batch, Y, y_dtype, static_cast<cudaStream_t>(stream));
+}
+
+int32_t lrbi_i8_pitch(int32_t cols) { return i8_cols_ok(cols) ? i8_pitch(cols) : 0; }
+
+lrbi_status lrbi_i8_quantize(const lrbi_layout *layout, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int8_t *q, float *scale, void *stream)
+{
+    if (!layout || layout->rows < 1 || !i8_cols_ok(layout->cols) || !W || !aligned(W, 2) || !rows8_ok(q, scale) || !ip != !iz) return LRBI_ERR_INVALID_ARG;
+    if (ip && (!aligned(ip, 4) || !aligned(iz, 4) || layout->tile_rows < 1 || layout->tile_cols < 1 || layout->rank < 1)) return LRBI_ERR_INVALID_ARG;
+    if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
+    lrbi_layout l = *layout;
+    if (!ip) { l.tile_rows = l.rows; l.tile_cols = l.cols; l.rank = 1; }
+    return launch_i8_quantize(make_geo(l), W, ip, iz, q, scale, static_cast<cudaStream_t>(stream));
+}
+
+lrbi_status lrbi_i8_tokens(const void *x, int32_t x_dtype, int64_t x_stride, int32_t rows, int32_t cols, int32_t act, int8_t *q, float *scale, void *stream)
+{
+    if (rows < 0 || !i8_cols_ok(cols) || !matrix_ok(x, x_dtype, x_stride, rows, cols) || act < LRBI_ACT_NONE || act > LRBI_ACT_SILU) return LRBI_ERR_INVALID_ARG;
+    if (rows > 0 && !rows8_ok(q, scale)) return LRBI_ERR_INVALID_ARG;
+    if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
+    if (rows == 0) return LRBI_OK;
+    return launch_i8_tokens(x, x_dtype, x_stride, rows, cols, act, q, scale, static_cast<cudaStream_t>(stream));
+}
+
+lrbi_status lrbi_i8_gemm(const int8_t *w_q, const float *w_scale, int32_t rows, int32_t cols, const int8_t *x_q, const float *x_scale, int32_t batch,
+                         void *Y, int32_t y_dtype, void *stream)
+{
+    if (rows < 1 || !i8_cols_ok(cols) || batch < 0 || !dtype_ok(y_dtype) || !rows8_ok(w_q, w_scale)) return LRBI_ERR_INVALID_ARG;
+    if (batch > 0 && (!rows8_ok(x_q, x_scale) || !Y || !aligned(Y, y_dtype == LRBI_Y_F32 ? 4 : 2))) return LRBI_ERR_INVALID_ARG;
+    if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
+    if (batch == 0) return LRBI_OK;
+    return launch_i8_gemm({w_q, w_scale, x_q, x_scale, Y, y_dtype, rows, cols, i8_pitch(cols), batch}, static_cast<cudaStream_t>(stream));
+}
+
+lrbi_status lrbi_residual_norm(const lrbi_residual *how, const void *x, int64_t x_stride, const void *f, int64_t f_stride, void *out, int64_t out_stride,
+                               void *u, int64_t u_stride, int8_t *u_q, float *u_scale, float *stats, void *stream)
+{
+    if (!residual_ok(how)) return LRBI_ERR_INVALID_ARG;
+    const int rows = how->rows, cols = how->cols;
+    if (!matrix_ok(x, how->x_dtype, x_stride, rows, cols) || !matrix_ok(f, how->f_dtype, f_stride, rows, cols) || !matrix_ok(out, how->x_dtype, out_stride, rows, cols)) return LRBI_ERR_INVALID_ARG;
+    if (!u_q != !u_scale || (u && u_q) || ((u || u_q) && !how->gamma)) return LRBI_ERR_INVALID_ARG;
+    if (rows > 0 && how->gamma && !u && !u_q) return LRBI_ERR_INVALID_ARG;
+    if ((u && !matrix_ok(u, how->f_dtype, u_stride, rows, cols)) || (u_q && !rows8_ok(u_q, u_scale)) || (stats && !aligned(stats, 4))) return LRBI_ERR_INVALID_ARG;
+    if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
+    if (rows == 0) return LRBI_OK;
+    JoinArgs n = join_args(how);
+    n.x = x; n.x_stride = x_stride;
+    n.f = f; n.f_stride = f_stride;
+    n.out = out; n.out_stride = out_stride;
+    n.u = u; n.u_stride = u_stride;
+    n.q = u_q; n.q_scale = u_scale;
+    n.stats = stats;
+    return launch_join(n, static_cast<cudaStream_t>(stream));
+}
+
+size_t lrbi_residual_norm_backward_workspace(int32_t rows, int32_t cols)
+{
+    return rows >= 0 && cols >= 1 && cols <= LRBI_MAX_RESIDUAL_COLS ? join_backward_workspace(rows, cols) : 0;
+}
+
+lrbi_status lrbi_residual_norm_backward(const lrbi_residual *how, const void *du, int64_t du_stride, const void *dout, int64_t dout_stride,
+                                        const void *out, int64_t out_stride, const void *f, int64_t f_stride, const float *stats, void *dx,
+                                        int64_t dx_stride, void *df, int64_t df_stride, float *dgamma, float *dbeta, float *dpost_gamma,
+                                        float *dpost_beta, float *dgate, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!residual_ok(how)) return LRBI_ERR_INVALID_ARG;
+    const int rows = how->rows, cols = how->cols;
+    if (!matrix_ok(f, how->f_dtype, f_stride, rows, cols) || !matrix_ok(dx, how->x_dtype, dx_stride, rows, cols) || !matrix_ok(df, how->f_dtype, df_stride, rows, cols)) return LRBI_ERR_INVALID_ARG;
+    if (how->gamma ? !matrix_ok(du, how->f_dtype, du_stride, rows, cols) || !matrix_ok(out, how->x_dtype, out_stride, rows, cols) : du != nullptr) return LRBI_ERR_INVALID_ARG;
+    if (dout && !matrix_ok(dout, how->x_dtype, dout_stride, rows, cols)) return LRBI_ERR_INVALID_ARG;
+    if (rows > 0 && (how->gamma || how->post_gamma) && (!stats || !aligned(stats, 4))) return LRBI_ERR_INVALID_ARG;
+    if ((dgamma && !how->gamma) || (dbeta && !how->beta) || (dpost_gamma && !how->post_gamma) || (dpost_beta && !how->post_beta) || (dgate && !how->gate)) return LRBI_ERR_INVALID_ARG;
+    for (const float *v : {dgamma, dbeta, dpost_gamma, dpost_beta, dgate}) if (v && !aligned(v, 4)) return LRBI_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < join_backward_workspace(rows, cols)) return LRBI_ERR_INVALID_ARG;
+    if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
+    JoinArgs n = join_args(how);
+    n.du = du; n.du_stride = du_stride;
+    n.dout = dout; n.dout_stride = dout_stride;
+    if (how->gamma) { n.out = const_cast<void *>(out); n.out_stride = out_stride; }
+    n.f = f; n.f_stride = f_stride;
+    n.stats = const_cast<float *>(stats);
+    n.dx = dx; n.dx_stride = dx_stride;
+    n.df = df; n.df_stride = df_stride;
+    n.dgamma = dgamma; n.dbeta = dbeta; n.dpost_gamma = dpost_gamma; n.dpost_beta = dpost_beta; n.dgate = dgate;
+    return launch_join_backward(n, static_cast<float *>(workspace), static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

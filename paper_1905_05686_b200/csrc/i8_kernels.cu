@@ -1,0 +1,244 @@
+// Rows in 8-bit integers with a scale each -- a layer's channels, a batch's tokens -- and their product for a few tokens.
+//
+//   a row v:   top = max |v|,   scale = top / 127,   q = rint(v * (127 / top))             (each step one fp32 operation)
+//   product:   Y[b][o] = (sum over i of q_X[b][i] * q_W[o][i]) * scale_X[b] * scale_W[o]   (the sum is a whole number, exact)
+//
+// Rows of q start on 16-byte boundaries and hold zeros past the last column, so that a product takes them 16 bytes at a time.
+#include "activation.cuh"
+
+namespace lrbi {
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Tokens
+// ---------------------------------------------------------------------------------------------------------------------
+struct TokenArgs {
+    RowsIn x;
+    int8_t *q;
+    float *scale;
+    int rows, cols, pitch;
+};
+
+// blockDim = (threads of a row, rows of a block).  A thread has up to K chunks of its row in registers, as results of the
+// nonlinearity in fp32, between the maximum and the bytes; rows of more chunks than that are read, and activated, twice.
+template <int SRC, int ACT, bool STRIDED, int K>
+__global__ void __launch_bounds__(512) i8_tokens_kernel(TokenArgs a)
+{
+    begin();
+    constexpr int SIZE = SRC == SRC_F32 ? 4 : 2;
+    __shared__ uint32_t part[16];
+    const int lane = kept_lane(), warp = threadIdx.x >> 5, warps = blockDim.x >> 5, team = threadIdx.y;
+    const long long row = (long long)blockIdx.x * blockDim.y + team;
+    const bool there = row < a.rows;
+    const int rounds = (a.cols + warps * SPAN * K - 1) / (warps * SPAN * K);
+    const char *x = static_cast<const char *>(a.x.data) + row * a.x.stride * SIZE;
+    F2 v[K][PAIRS];
+    uint32_t top = 0;
+    auto load = [&](int round) {
+        Raw<SRC, STRIDED> raw[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = lane_column<STRIDED>(((round * K + k) * warps + warp) * SPAN, lane);
+            raw[k].clear();
+            if (there && c < a.cols) raw[k].load_at(x + (long long)c * SIZE, a.cols - c);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw[k].get(v[k]);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                F2 slope;
+                if constexpr (ACT != ACT_NONE) activate<ACT, false, SRC == SRC_F32, false>(v[k][i], v[k][i], slope);      // 0 stays 0 in all of them
+            }
+        }
+    };
+    for (int r = 0; r < rounds; ++r) {
+        load(r);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                float lo, hi;
+                split(v[k][i], lo, hi);
+                top = max(top, max(__float_as_uint(lo) & 0x7FFFFFFFu, __float_as_uint(hi) & 0x7FFFFFFFu));      // a NaN is above infinity
+            }
+    }
+    let_next();
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (warps > 1) {
+        if (lane == 0) part[team * warps + warp] = top;
+        __syncthreads();
+        top = __reduce_max_sync(0xFFFFFFFFu, part[team * warps + (lane < warps ? lane : 0)]);
+    }
+    if (!there) return;
+    const TokenScale s(top);
+    if (threadIdx.x == 0) a.scale[row] = s.scale();
+    int8_t *q = a.q + row * a.pitch;
+    for (int r = 0; r < rounds; ++r) {
+        if (rounds > 1) load(r);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = lane_column<STRIDED>(((r * K + k) * warps + warp) * SPAN, lane);
+            store_i8<STRIDED>(q + c, a.pitch - c, v[k], s.factor, s.fine);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Weights
+// ---------------------------------------------------------------------------------------------------------------------
+// A block has a row.  The range is that of the kept weights; pruned ones are stored as zeros whatever the array holds there.
+// The index of a weight is decoded on its own, twice: a layer is quantised once.
+__global__ void __launch_bounds__(256) i8_quantize_kernel(Geo geo, const uint16_t *__restrict__ W, const uint32_t *__restrict__ ip,
+                                                          const uint32_t *__restrict__ iz, int8_t *__restrict__ q, float *__restrict__ scale, int pitch)
+{
+    __shared__ uint32_t part[8];
+    const int o = blockIdx.x, tr = o / geo.tm;
+    const uint16_t *w = W + (long long)o * geo.cols;
+    auto weight = [&](int c) {
+        if (ip) {
+            const int tc = c / geo.tn;
+            const long long t = (long long)tr * geo.gc + tc;
+            const uint32_t *a = ip + (t * geo.tm + (o - tr * geo.tm)) * geo.kw, *b = iz + (t * geo.tn + (c - tc * geo.tn)) * geo.kw;
+            uint32_t any = 0;
+            for (int i = 0; i < geo.kw; ++i) any |= __ldg(a + i) & __ldg(b + i) & (i == geo.kw - 1 ? tail_mask(geo.k) : 0xFFFFFFFFu);
+            if (!any) return 0.f;
+        }
+        return __uint_as_float((uint32_t)__ldg(w + c) << 16);
+    };
+    uint32_t top = 0;
+    for (int c = threadIdx.x; c < geo.cols; c += 256) top = max(top, __float_as_uint(weight(c)) & 0x7FFFFFFFu);
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+    __syncthreads();
+    top = __reduce_max_sync(0xFFFFFFFFu, part[threadIdx.x & 7]);
+    const TokenScale s(top);
+    if (threadIdx.x == 0) scale[o] = s.scale();
+    for (int c = threadIdx.x; c < pitch; c += 256) q[(long long)o * pitch + c] = s.fine && c < geo.cols ? (int8_t)(int)rintf(__fmul_rn(weight(c), s.factor)) : (int8_t)0;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Products of a few tokens
+// ---------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mma_i8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// A block has 16 rows of weights and 8 * NT tokens; its warps take 64 columns each in turn and add their sums up at the end.
+// The column is a summation index: lane (g, t) takes 16 neighbouring bytes of rows g and g + 8, and of token g, as the four
+// words that two steps of 32 columns want, both operands in the same order.
+constexpr int I8_WARPS = 8;
+template <int NT>
+__global__ void __launch_bounds__(32 * I8_WARPS) i8_few_kernel(I8Product p)
+{
+    begin();
+    constexpr int U = 4;       // steps of a warp whose loads are under way together
+    __shared__ int sums[I8_WARPS][8 * NT][16];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int o0 = blockIdx.x * 16, b0 = blockIdx.y * 8 * NT;
+    const int8_t *w0 = p.w + (long long)min(o0 + g, p.rows - 1) * p.pitch, *w1 = p.w + (long long)min(o0 + g + 8, p.rows - 1) * p.pitch;
+    const int8_t *x[NT];
+    bool on[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        on[n] = b0 + 8 * n + g < p.batch;
+        x[n] = p.x + (long long)(on[n] ? b0 + 8 * n + g : 0) * p.pitch;
+    }
+    int d[NT][4] = {};
+    for (int c0 = warp * 64; c0 < p.pitch; c0 += I8_WARPS * 64 * U) {
+        uint4 a[U][2], b[U][NT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + u * I8_WARPS * 64 + 16 * t;
+            const bool in = c < p.pitch;
+            a[u][0] = a[u][1] = make_uint4(0, 0, 0, 0);
+            if (in) { a[u][0] = ld_once16(w0 + c); a[u][1] = ld_once16(w1 + c); }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) b[u][n] = in && on[n] ? __ldg(reinterpret_cast<const uint4 *>(x[n] + c)) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma_i8(d[n], a[u][0].x, a[u][1].x, a[u][0].y, a[u][1].y, b[u][n].x, b[u][n].y);
+                mma_i8(d[n], a[u][0].z, a[u][1].z, a[u][0].w, a[u][1].w, b[u][n].z, b[u][n].w);
+            }
+    }
+    let_next();
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[warp][8 * n + 2 * t + (i & 1)][g + 8 * (i >> 1)] = d[n][i];
+    __syncthreads();
+    for (int k = threadIdx.x; k < 8 * NT * 16; k += 32 * I8_WARPS) {
+        const int b = b0 + k / 16, o = o0 + k % 16;
+        if (b >= p.batch || o >= p.rows) continue;
+        int v = 0;
+#pragma unroll
+        for (int w = 0; w < I8_WARPS; ++w) v += sums[w][k / 16][k % 16];
+        const float y = ((float)v * __ldg(p.x_scale + b)) * __ldg(p.w_scale + o);
+        const long long to = (long long)b * p.rows + o;
+        if (p.y_dtype == LRBI_Y_F32) static_cast<float *>(p.y)[to] = y;
+        else static_cast<uint16_t *>(p.y)[to] = (uint16_t)pack_bf16(y, 0.f);
+    }
+}
+
+namespace {
+
+template <int SRC, int ACT, bool STRIDED, int K>
+lrbi_status tokens_launch(const TokenArgs &a, int threads, cudaStream_t s)
+{
+    const int teams = threads < 256 ? 256 / threads : 1;
+    return launch_kernel(i8_tokens_kernel<SRC, ACT, STRIDED, K>, dim3((a.rows + teams - 1) / teams), dim3(threads, teams), 0, s, 1, a);
+}
+
+template <int SRC, int ACT, bool STRIDED>
+lrbi_status tokens_chunks(const TokenArgs &a, cudaStream_t s)
+{
+    const int spans = (a.cols + SPAN - 1) / SPAN;
+    if (spans <= 16) return tokens_launch<SRC, ACT, STRIDED, 1>(a, 32 * (spans <= 1 ? 1 : spans <= 2 ? 2 : spans <= 4 ? 4 : spans <= 8 ? 8 : 16), s);
+    if (spans <= 32) return tokens_launch<SRC, ACT, STRIDED, 2>(a, 512, s);
+    return tokens_launch<SRC, ACT, STRIDED, 4>(a, 512, s);
+}
+
+template <int SRC, int ACT>
+lrbi_status tokens_rows(const TokenArgs &a, cudaStream_t s)
+{
+    return a.cols % CHUNK == 0 && vector_rows(a.x.data, a.x.stride, SRC) ? tokens_chunks<SRC, ACT, false>(a, s) : tokens_chunks<SRC, ACT, true>(a, s);
+}
+
+template <int SRC>
+lrbi_status tokens_act(const TokenArgs &a, int act, cudaStream_t s)
+{
+    if (act == LRBI_ACT_RELU) return tokens_rows<SRC, LRBI_ACT_RELU>(a, s);
+    if (act == LRBI_ACT_GELU) return tokens_rows<SRC, LRBI_ACT_GELU>(a, s);
+    if (act == LRBI_ACT_SILU) return tokens_rows<SRC, LRBI_ACT_SILU>(a, s);
+    return tokens_rows<SRC, ACT_NONE>(a, s);
+}
+
+}  // namespace
+
+lrbi_status launch_i8_tokens(const void *x, int dtype, long long stride, int rows, int cols, int act, int8_t *q, float *scale, cudaStream_t s)
+{
+    const TokenArgs a = {{x, stride}, q, scale, rows, cols, i8_pitch(cols)};
+    return dtype == LRBI_Y_F32 ? tokens_act<SRC_F32>(a, act, s) : tokens_act<SRC_BF16>(a, act, s);
+}
+
+lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int8_t *q, float *scale, cudaStream_t s)
+{
+    i8_quantize_kernel<<<g.rows, 256, 0, s>>>(g, W, ip, iz, q, scale, i8_pitch(g.cols));
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) { note_cuda_error((int)e); return LRBI_ERR_CUDA; }
+    count_launch();
+    return LRBI_OK;
+}
+
+lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
+{
+    const int tiles = (p.rows + 15) / 16;
+    if (p.batch <= 8) return launch_kernel(i8_few_kernel<1>, dim3(tiles, 1), dim3(32 * I8_WARPS), 0, s, 1, p);
+    return launch_kernel(i8_few_kernel<2>, dim3(tiles, (p.batch + 15) / 16), dim3(32 * I8_WARPS), 0, s, 1, p);
+}
+
+}  // namespace lrbi

@@ -225,4 +225,40 @@ lrbi_status launch_w4_gemv(const uint32_t *packed, const uint32_t *meta, int row
 lrbi_status launch_w4_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int group, uint32_t *packed, uint32_t *meta,
                                cudaStream_t s);
 
+// Rows in 8-bit integers with a scale each.
+inline int i8_pitch(int cols) { return (cols + 15) / 16 * 16; }
+struct I8Product {
+    const int8_t *w; const float *w_scale;     // [rows][pitch], [rows]
+    const int8_t *x; const float *x_scale;     // [batch][pitch], [batch]
+    void *y; int y_dtype;                      // [batch][rows]
+    int rows, cols, pitch, batch;
+};
+lrbi_status launch_i8_tokens(const void *x, int dtype, long long stride, int rows, int cols, int act, int8_t *q, float *scale, cudaStream_t s);
+lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int8_t *q, float *scale, cudaStream_t s);
+lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s);
+
+// Between two blocks: out = scale * x + gate * norm(f), u = norm(out), and the backward pass; null pointers for what a call
+// does not have.
+struct JoinArgs {
+    int rows, cols;
+    bool rms;
+    int x_dtype, f_dtype, param_dtype;      // x, out, dout, dx; f, u, du, df; the vectors
+    float residual_scale, eps;
+    const void *gamma, *beta, *post_gamma, *post_beta, *gate;
+    const void *x; long long x_stride;
+    const void *f; long long f_stride;
+    void *out; long long out_stride;        // read by the backward pass
+    void *u; long long u_stride;
+    int8_t *q; float *q_scale;              // u as 8-bit tokens
+    float *stats;                           // [4][rows]: mean and 1 / root of out, of f
+    const void *du; long long du_stride;
+    const void *dout; long long dout_stride;
+    void *dx; long long dx_stride;
+    void *df; long long df_stride;
+    float *dgamma, *dbeta, *dpost_gamma, *dpost_beta, *dgate;
+};
+size_t join_backward_workspace(int rows, int cols);
+lrbi_status launch_join(const JoinArgs &a, cudaStream_t s);
+lrbi_status launch_join_backward(const JoinArgs &a, float *workspace, cudaStream_t s);
+
 }  // namespace lrbi

@@ -375,6 +375,46 @@ __device__ __forceinline__ void keep_chunk(const KeptOut &k, long long row, int 
     if (Keep<STRIDED>::stores(lane) && Keep<STRIDED>::chunk(lane) == 0 && group < k.groups) k.scale[row * k.groups + group] = keep.quotient;
 }
 
+// What a row of 8-bit integers is scaled by, from the bits of its largest magnitude (a NaN is above infinity): q = rint(v * factor)
+// stands for q * scale().  A row that holds a NaN or an infinity gets the scale NaN, one below KEEP_TINY the scale 0, and zeros.
+struct TokenScale {
+    uint32_t top;
+    bool fine;
+    float factor;
+    __device__ __forceinline__ explicit TokenScale(uint32_t bits)
+    {
+        top = bits;
+        fine = bits < 0x7F800000u && __uint_as_float(bits) >= KEEP_TINY;
+        factor = fine ? __fdiv_rn(127.f, __uint_as_float(bits)) : 0.f;
+    }
+    __device__ __forceinline__ float scale() const
+    {
+        return fine ? __fdiv_rn(__uint_as_float(top), 127.f) : top < 0x7F800000u ? 0.f : __uint_as_float(0x7FC00000u);
+    }
+};
+
+// The bytes of a lane's chunk as rint(v * factor), at `to`, the place of its first column; `left` bytes are there from that one
+// on.  (Adding 1.5 * 2^23 as in Keep::bytes.)  fine: false for a row that is kept as zeros.
+template <bool STRIDED>
+__device__ __forceinline__ void store_i8(int8_t *to, int left, const F2 (&v)[PAIRS], float factor, bool fine)
+{
+    uint32_t b[CHUNK];
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) {
+        float lo, hi;
+        split(v[i] * f2(factor), lo, hi);
+        b[2 * i] = fine ? __float_as_uint(__fadd_rn(lo, 12582912.f)) : 0;
+        b[2 * i + 1] = fine ? __float_as_uint(__fadd_rn(hi, 12582912.f)) : 0;
+    }
+    if constexpr (STRIDED) {
+#pragma unroll
+        for (int e = 0; e < CHUNK; ++e) if (32 * e < left) to[32 * e] = (int8_t)b[e];
+    } else if (left > 0) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                                                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+    }
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll

@@ -1,4 +1,5 @@
-// Python calls of the operators around the masked layers (layer norm, 8-bit copies, the nonlinearity, 4-bit products):
+// Python calls of the operators around the masked layers (layer norm, 8-bit copies, the nonlinearity, 4-bit and 8-bit products,
+// what stands between two blocks):
 // checks of torch tensors, allocation of the outputs, the C ABI call.  No computation here.
 //
 // These calls are made per layer and per token on arrays of a few microseconds' work, so their cost on the host counts:
@@ -14,6 +15,7 @@
 #include <climits>
 #include <stdexcept>
 #include <string>
+#include <tuple>
 #include <utility>
 
 #include "lrbi.h"
@@ -392,6 +394,177 @@ PyObject *w4_gemv(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// Rows in 8-bit integers that a call reads: [rows, pitch] int8 and a scale each.
+struct Rows8 { const int8_t *q; const float *scale; };
+Rows8 rows8(PyObject *q, PyObject *scale, int64_t rows, int64_t cols, const at::Device &device, const char *what)
+{
+    const at::Tensor &t = tensor(q, what), &s = tensor(scale, what);
+    if (!t.is_cuda() || t.device() != device || s.device() != device) throw BadValue(std::string(what) + " must be on the call's device");
+    if (t.scalar_type() != at::kChar || s.scalar_type() != at::kFloat || !t.is_contiguous() || !s.is_contiguous())
+        throw BadType(std::string(what) + ": 8-bit rows are contiguous int8 and their scales contiguous float32");
+    if (rows < 0 || rows > INT_MAX || cols < 1 || cols > LRBI_I8_MAX_COLS || t.numel() != rows * lrbi_i8_pitch((int)cols) || s.numel() != rows)
+        throw BadValue(std::string(what) + " does not have the size of its rows");
+    return {static_cast<const int8_t *>(t.data_ptr()), static_cast<const float *>(s.data_ptr())};
+}
+
+std::pair<at::Tensor, at::Tensor> make_rows8(const Call &c, int rows, int cols)
+{
+    if (cols > LRBI_I8_MAX_COLS) throw BadValue("rows in 8 bits have at most 131072 columns");
+    return c.make_two({rows, lrbi_i8_pitch(cols)}, at::kChar, {rows}, at::kFloat);
+}
+
+// i8_tokens(x, act, stream) -> (q, scale)
+PyObject *i8_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    CALL("i8_tokens", 3) {
+        const Matrix x = matrix(tensor(a[0], "x"), "x");
+        const int act = (int)whole_number(a[1]);
+        const Call c(x.device, a[2]);
+        auto [q, scale] = make_rows8(c, x.rows, x.cols);
+        check(lrbi_i8_tokens(x.data, x.dtype, x.stride, x.rows, x.cols, act, static_cast<int8_t *>(q.data_ptr()), static_cast<float *>(scale.data_ptr()), c.handle()),
+              "lrbi_i8_tokens");
+        return tuple(std::move(q), std::move(scale));
+    });
+}
+
+// i8_gemm(w_q, w_scale, rows, cols, x_q, x_scale, batch, y_dtype, stream) -> Y
+PyObject *i8_gemm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    CALL("i8_gemm", 9) {
+        const at::Device device = tensor(a[0], "weights").device();
+        const int64_t rows = whole_number(a[2]), cols = whole_number(a[3]), batch = whole_number(a[6]);
+        const Rows8 w = rows8(a[0], a[1], rows, cols, device, "weights"), x = rows8(a[4], a[5], batch, cols, device, "tokens");
+        const at::ScalarType type = dtype_of(a[7], at::kBFloat16, "y_dtype");
+        const Call c(device, a[8]);
+        at::Tensor Y = c.make({batch, rows}, type);
+        check(lrbi_i8_gemm(w.q, w.scale, (int)rows, (int)cols, x.q, x.scale, (int)batch, Y.data_ptr(), type_code(type), c.handle()), "lrbi_i8_gemm");
+        return THPVariable_Wrap(std::move(Y));
+    });
+}
+
+// The vectors and numbers of a call between two blocks: a[0 ..] = gamma, beta, post_gamma, post_beta, gate.
+lrbi_residual residual(PyObject *const *a, const Matrix &x, const Matrix &f, double scale, double eps, int kind)
+{
+    lrbi_residual h = {x.rows, x.cols, kind, x.dtype, f.dtype, LRBI_Y_F32, (float)scale, (float)eps, nullptr, nullptr, nullptr, nullptr, nullptr};
+    if (x.cols > LRBI_MAX_RESIDUAL_COLS) throw BadValue("the residual stream has at most 32768 columns");
+    if (x.dtype == LRBI_Y_BF16 && f.dtype != LRBI_Y_BF16) throw BadType("f must be bfloat16 where x is");
+    const char *names[5] = {"gamma", "beta", "post_gamma", "post_beta", "gate"};
+    const void **at[5] = {&h.gamma, &h.beta, &h.post_gamma, &h.post_beta, &h.gate};
+    int type = -1;
+    for (int i = 0; i < 5; ++i) {
+        if (a[i] == Py_None) continue;
+        const at::Tensor &t = param(a[i], names[i], x);
+        const int code = type_code(t.scalar_type());
+        if (type >= 0 && code != type) throw BadValue(std::string(names[i]) + " must have the type of the other vectors");
+        h.param_dtype = type = code;
+        *at[i] = t.data_ptr();
+    }
+    if (h.beta && !h.gamma) throw BadValue("beta comes with gamma");
+    if (h.post_beta && !h.post_gamma) throw BadValue("post_beta comes with post_gamma");
+    return h;
+}
+
+double number(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised();
+    return v;
+}
+
+PyObject *or_none(at::Tensor t)
+{
+    if (t.defined()) return THPVariable_Wrap(std::move(t));
+    Py_RETURN_NONE;
+}
+
+template <int N>
+PyObject *tuple_of(at::Tensor (&t)[N])
+{
+    PyObject *r = PyTuple_New(N);
+    for (int i = 0; r && i < N; ++i) {
+        PyObject *item = or_none(std::move(t[i]));
+        if (!item) { Py_DECREF(r); return nullptr; }
+        PyTuple_SET_ITEM(r, i, item);
+    }
+    return r;
+}
+
+// residual_norm(x, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, eps, kind, tokens, stream) -> (out, u, stats, q, scale): None for what the call does not make
+PyObject *residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    CALL("residual_norm", 12) {
+        const Matrix x = matrix(tensor(a[0], "x"), "x"), f = matrix_like(a[1], "f", x);
+        const lrbi_residual how = residual(a + 2, x, f, number(a[7]), number(a[8]), (int)whole_number(a[9]));
+        const int tokens = PyObject_IsTrue(a[10]);
+        if (tokens < 0) throw Raised();
+        if (tokens && !how.gamma) throw BadValue("tokens come from the second norm: give gamma");
+        const Call c(x.device, a[11]);
+        at::Tensor t[5];      // out, u, stats, q, scale
+        t[0] = c.make({x.rows, x.cols}, x.type);
+        if (tokens) std::tie(t[3], t[4]) = make_rows8(c, x.rows, x.cols);
+        else {
+            if (how.gamma) t[1] = c.make({x.rows, x.cols}, f.type);
+            t[2] = c.make({4, x.rows}, at::kFloat);
+        }
+        auto at = [](const at::Tensor &v) { return v.defined() ? v.data_ptr() : nullptr; };
+        check(lrbi_residual_norm(&how, x.data, x.stride, f.data, f.stride, at(t[0]), x.cols, at(t[1]), x.cols, static_cast<int8_t *>(at(t[3])),
+                                 static_cast<float *>(at(t[4])), static_cast<float *>(at(t[2])), c.handle()),
+              "lrbi_residual_norm");
+        return tuple_of(t);
+    });
+}
+
+// residual_norm_backward(du, dout, out, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, stats, kind, stream)
+//     -> (dx, df, dgamma, dbeta, dpost_gamma, dpost_beta, dgate): None for vectors that the call does not have
+PyObject *residual_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    CALL("residual_norm_backward", 13) {
+        const Matrix f = matrix(tensor(a[3], "f"), "f");
+        Matrix x = f, du = {nullptr, f.dtype, f.rows, f.cols, f.cols, f.device, f.type}, dout = du;
+        if (a[2] != Py_None) x = matrix_like(a[2], "out", f);
+        if (a[1] != Py_None) dout = matrix_like(a[1], "dout", f);
+        if (a[2] == Py_None) { if (a[1] == Py_None) throw BadValue("out or dout must be given"); x = dout; }
+        if (a[1] != Py_None && dout.type != x.type) throw BadValue("dout must have out's type");
+        const lrbi_residual how = residual(a + 4, x, f, number(a[9]), 0., (int)whole_number(a[11]));
+        if (how.gamma) {
+            if (a[2] == Py_None) throw BadValue("out must be given where gamma is");
+            du = matrix_like(a[0], "du", f);
+            if (du.type != f.type) throw BadValue("du must have f's type");
+        } else if (a[0] != Py_None) throw BadValue("du comes with gamma");
+        const float *stats = nullptr;
+        if (how.gamma || how.post_gamma) {
+            const at::Tensor &t = tensor(a[10], "stats");
+            if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.device() != f.device || t.numel() != 4 * (int64_t)f.rows)
+                throw BadType("stats must be the contiguous float32 tensor [4, rows] of the forward pass");
+            stats = static_cast<const float *>(t.data_ptr());
+        }
+        const Call c(f.device, a[12]);
+        at::Tensor t[7];      // dx, df, and the vectors' gradients out of one allocation
+        t[0] = c.make({f.rows, f.cols}, x.type);
+        t[1] = c.make({f.rows, f.cols}, f.type);
+        const void *vectors[5] = {how.gamma, how.beta, how.post_gamma, how.post_beta, how.gate};
+        float *to[5] = {};
+        int count = 0;
+        for (const void *v : vectors) count += v != nullptr;
+        if (count) {
+            const int64_t pitch = (f.cols + 3) / 4 * 4;
+            const at::Tensor all = c.make({count * pitch}, at::kFloat);
+            for (int i = 0, k = 0; i < 5; ++i) {
+                if (!vectors[i]) continue;
+                t[2 + i] = Call::part(all, k++ * pitch, {f.cols}, at::kFloat);
+                to[i] = static_cast<float *>(t[2 + i].data_ptr());
+            }
+        }
+        const size_t need = lrbi_residual_norm_backward_workspace(f.rows, f.cols);
+        const at::Tensor work = c.scratch({(int64_t)need}, at::kByte);
+        check(lrbi_residual_norm_backward(&how, du.data, du.stride, a[1] != Py_None ? dout.data : nullptr, dout.stride, how.gamma ? x.data : nullptr, x.stride,
+                                          f.data, f.stride, stats, t[0].data_ptr(), f.cols, t[1].data_ptr(), f.cols, to[0], to[1], to[2], to[3], to[4],
+                                          work.data_ptr(), need, c.handle()),
+              "lrbi_residual_norm_backward");
+        return tuple_of(t);
+    });
+}
+
 PyObject *set_error(PyObject *, PyObject *error)
 {
     Py_INCREF(error);
@@ -402,7 +575,7 @@ PyObject *set_error(PyObject *, PyObject *error)
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(checkpoint_store), FAST(checkpoint_load), FAST(layer_norm), FAST(layer_norm_backward), FAST(activation),
-                         FAST(activation_backward), FAST(w4_gemv), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FAST(activation_backward), FAST(w4_gemv), FAST(i8_tokens), FAST(i8_gemm), FAST(residual_norm), FAST(residual_norm_backward), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lrbi_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
