@@ -1,0 +1,457 @@
+// Products of 8-bit rows on the tensor cores:  Y[b][o] = (sum over i of q_X[b][i] * q_W[o][i]) * scale_X[b] * scale_W[o].
+//
+// tcgen05.mma kind::i8, K-major operands with the 128-byte swizzle (a stage is 128 columns of both), sums in tensor memory as
+// 32-bit whole numbers: exact, in any order.  Two kernels:
+//
+//   long   many tokens.  CTA pairs (cta_group::2) of 256 tokens x 256 channels walk the output tiles; two accumulators, so that
+//          four warps scale and store one tile while the next one is computed.
+//   split  fewer.  128 channels x up to 256 tokens a CTA; the CTAs of a cluster share the columns and add their sums up through
+//          distributed shared memory (whole numbers: the same bits however they are cut), so that all SMs stream the weights.
+//
+// Every wait is bounded; a wait that runs out leaves a code in the device status word, and the CTA ends early.
+#include "norm_common.cuh"
+#include "tcgen05_ptx.cuh"
+
+namespace lrbi {
+
+constexpr int I8_KB = 128;                               // columns (and bytes of a row) of a stage
+constexpr int I8_A_BYTES = 128 * I8_KB;                  // 128 rows of the M operand
+constexpr int I8_THREADS = 192;                          // warp 0 copies, warp 1 multiplies, warps 2-5 scale and store
+constexpr int I8_EPI_WARPS = 4;
+constexpr size_t I8_SHARED = 226 * 1024;                 // dynamic shared memory of a CTA that has an SM to itself
+
+struct I8Ctl {
+    uint64_t full[8], empty[8];      // of the stages
+    uint64_t accum[2], drained[2];   // of the accumulators
+    uint32_t tmem;
+    int abort_flag;
+};
+
+struct I8Tc {
+    const float *x_scale, *w_scale;
+    void *y;
+    int y_dtype;
+    int rows, batch;                 // channels, tokens
+    int blocks;                      // of columns: stages of a tile
+    int stages;
+    int tokens;                      // split: of a tile
+    int split;
+    bool vector;                     // rows of Y are whole 16-byte vectors
+    int *status;
+};
+
+__device__ __forceinline__ void umma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma2_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Signed 8-bit operands, 32-bit sums.
+__host__ __device__ constexpr uint32_t i8_idesc(int m, int n) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+
+// A copy of a CTA of a pair into its own shared memory that signals a barrier of the pair's first CTA (`bar`: its address there).
+__device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *map, uint32_t bar, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ uint32_t in_cta(const void *mine, uint32_t rank)      // the same place in the shared memory of another CTA of the cluster
+{
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(mine)), "r"(rank));
+    return there;
+}
+__device__ __forceinline__ int cluster_int(uint32_t at)
+{
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t at, int (&v)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+                   "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+                   "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                 : "r"(at) : "memory");
+}
+
+// Copies that are under way must land before shared memory is given up: about 2 ms, far beyond any of them.
+__device__ __forceinline__ void let_copies_land()
+{
+    const long long t0 = clock64();
+    while (clock64() - t0 < 4000000ll) { }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Many tokens
+// ---------------------------------------------------------------------------------------------------------------------
+// The tile's M is the token (a lane of tensor memory), its N the channel: a thread has neighbouring outputs of one row of Y.
+// They go through 4 KB a warp, 32 rows x 128 bytes in the swizzled order, and out as whole lines.
+constexpr int I8_LONG_STAGE = 2 * I8_A_BYTES, I8_EPI_BYTES = 32 * 128 + 256 * 4;
+__global__ void __launch_bounds__(I8_THREADS, 1) i8_long_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t *epi = smem + (size_t)p.stages * I8_LONG_STAGE;
+    I8Ctl *ctl = reinterpret_cast<I8Ctl *>(epi + I8_EPI_WARPS * I8_EPI_BYTES);
+    volatile int *abort_flag = &ctl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    if ((smem_u32(smem) & 1023u) != 0) {         // never expected; refuse rather than compute garbage
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, DEV_BAD_SMEM_ALIGN);
+        return;
+    }
+    if (warp == 0) {
+        if (lane < p.stages) {
+            mbar_init(&ctl->full[lane], 1);
+            mbar_init(&ctl->empty[lane], 1);
+        } else if (lane == 8 || lane == 9) {
+            mbar_init(&ctl->accum[lane - 8], 1);
+            mbar_init(&ctl->drained[lane - 8], 2 * I8_EPI_WARPS);
+        } else if (lane == 10) ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc2(&ctl->tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    __syncwarp();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem;
+    begin();
+
+    // Tiles run fastest along the smaller operand: the pairs at work at any time share all of it, and the larger one streams
+    // from memory once.
+    const int token_tiles = (p.batch + 255) / 256, channel_tiles = (p.rows + 255) / 256, tiles = token_tiles * channel_tiles;
+    const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    const bool tokens_fast = p.batch <= p.rows;
+    auto tile_at = [&](int t, int &b0, int &o0) {
+        b0 = (tokens_fast ? t % token_tiles : t / channel_tiles) * 256;
+        o0 = (tokens_fast ? t / token_tiles : t % channel_tiles) * 256;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t parity = 1;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step) {
+                int b0, o0;
+                tile_at(t, b0, o0);
+                for (int k = 0; k < p.blocks; ++k) {
+                    ok = mbar_wait(&ctl->empty[s], parity, abort_flag, p.status, DEV_TIMEOUT_EMPTY);
+                    if (!ok) break;
+                    if (rank == 0) mbar_arrive_expect_tx(&ctl->full[s], 2 * I8_LONG_STAGE);       // of both CTAs
+                    const uint32_t bar = in_cta(&ctl->full[s], 0);
+                    uint8_t *a = smem + (size_t)s * I8_LONG_STAGE;
+                    tma_load_2d_pair(a, &x_map, bar, k * I8_KB, b0 + (int)rank * 128);
+                    tma_load_2d_pair(a + I8_A_BYTES, &w_map, bar, k * I8_KB, o0 + (int)rank * 128);
+                    if (++s == p.stages) { s = 0; parity ^= 1; }
+                }
+            }
+            if (!ok) let_copies_land();
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = i8_idesc(256, 256);
+            int s = 0, n = 0;
+            uint32_t parity = 0;
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += step, ++n) {
+                ok = mbar_wait(&ctl->drained[n & 1], (n >> 1 & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d = tmem + (n & 1) * 256;
+                for (int k = 0; k < p.blocks; ++k) {
+                    ok = mbar_wait(&ctl->full[s], parity, abort_flag, p.status, DEV_TIMEOUT_FULL);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t a = make_sw128_desc(smem_u32(smem + (size_t)s * I8_LONG_STAGE)), b = make_sw128_desc(smem_u32(smem + (size_t)s * I8_LONG_STAGE + I8_A_BYTES));
+#pragma unroll
+                    for (int q = 0; q < I8_KB / 32; ++q) umma2_i8(d, a + (uint64_t)(2 * q), b + (uint64_t)(2 * q), idesc, (k | q) ? 1u : 0u);
+                    umma2_commit_both(&ctl->empty[s]);
+                    if (++s == p.stages) { s = 0; parity ^= 1; }
+                }
+                if (ok) umma2_commit_both(&ctl->accum[n & 1]);
+            }
+        }
+    } else {
+        const int quad = warp & 3;
+        uint8_t *stage = epi + (warp - 2) * I8_EPI_BYTES;
+        float *scale = reinterpret_cast<float *>(stage + 32 * 128);
+        const bool f32 = p.y_dtype == LRBI_Y_F32;
+        const int each = f32 ? 32 : 64;          // columns of 128 bytes
+        bool ok = true;
+        int n = 0;
+        for (int t = first; t < tiles; t += step, ++n) {
+            int b0, o0;
+            tile_at(t, b0, o0);
+            b0 += (int)rank * 128 + quad * 32;
+            const int left = min(32, p.batch - b0);      // rows of Y that the warp has
+            const float token = lane < left ? __ldg(p.x_scale + b0 + lane) : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) scale[i * 32 + lane] = o0 + i * 32 + lane < p.rows ? __ldg(p.w_scale + o0 + i * 32 + lane) : 0.f;
+            ok = mbar_wait(&ctl->accum[n & 1], n >> 1 & 1, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
+            __syncwarp();                                // the loads below are the whole warp's: one verdict for all lanes
+            if (!ok || *abort_flag) break;
+            tc_fence_after();
+            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (n & 1) * 256;
+            for (int c = 0; c < 256; c += each) {
+                uint4 *own = reinterpret_cast<uint4 *>(stage + lane * 128);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1 && f32) break;
+                    int v[32];
+                    tmem_ld32(from + c + 32 * h, v);
+                    tmem_ld_wait();
+                    const float4 *w = reinterpret_cast<const float4 *>(scale + c + 32 * h);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 s = w[i];
+                        const float y0 = ((float)v[4 * i] * token) * s.x, y1 = ((float)v[4 * i + 1] * token) * s.y, y2 = ((float)v[4 * i + 2] * token) * s.z,
+                                    y3 = ((float)v[4 * i + 3] * token) * s.w;
+                        if (f32) own[i ^ (lane & 7)] = make_uint4(__float_as_uint(y0), __float_as_uint(y1), __float_as_uint(y2), __float_as_uint(y3));
+                        else *(reinterpret_cast<uint2 *>(own + ((4 * h + i / 2) ^ (lane & 7))) + (i & 1)) = make_uint2(pack_bf16(y0, y1), pack_bf16(y2, y3));
+                    }
+                }
+                if (c + each >= 256) {                   // read: the accumulator may be overwritten
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (rank == 0) mbar_arrive(&ctl->drained[n & 1]);
+                        else mbar_arrive_remote(&ctl->drained[n & 1], 0);
+                    }
+                }
+                __syncwarp();
+                if (p.vector) {
+                    const int piece = lane & 7, per = f32 ? 4 : 8, o = o0 + c + piece * per;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = i * 4 + (lane >> 3);
+                        if (r < left && o < p.rows)
+                            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + ((long long)(b0 + r) * p.rows + o) * (f32 ? 4 : 2)) =
+                                *reinterpret_cast<const uint4 *>(stage + r * 128 + ((piece ^ (r & 7)) << 4));
+                    }
+                } else {
+                    for (int r = 0; r < left; ++r)
+                        for (int e = lane; e < each; e += 32) {
+                            const int o = o0 + c + e, at = e * (f32 ? 4 : 2);
+                            const uint8_t *from8 = stage + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15);
+                            if (o < p.rows) {
+                                if (f32) static_cast<float *>(p.y)[(long long)(b0 + r) * p.rows + o] = *reinterpret_cast<const float *>(from8);
+                                else static_cast<uint16_t *>(p.y)[(long long)(b0 + r) * p.rows + o] = *reinterpret_cast<const uint16_t *>(from8);
+                            }
+                        }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    let_next();
+    tc_fence_before();
+    __syncthreads();
+    __syncwarp();
+    cluster_sync_all();              // neither CTA frees tensor memory or leaves while the other may still touch it
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc2(tmem, 512);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Fewer tokens
+// ---------------------------------------------------------------------------------------------------------------------
+// The tile's M is the channel, its N the token (a multiple of 16 up to 256, as many as there are).
+__global__ void __launch_bounds__(I8_THREADS, 1) i8_split_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int stage_bytes = I8_A_BYTES + p.tokens * I8_KB;
+    I8Ctl *ctl = reinterpret_cast<I8Ctl *>(smem + (size_t)p.stages * stage_bytes);
+    volatile int *abort_flag = &ctl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t columns = p.tokens <= 32 ? 32 : p.tokens <= 64 ? 64 : p.tokens <= 128 ? 128 : 256;
+    const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
+    if ((smem_u32(smem) & 1023u) != 0) {         // never expected; refuse rather than compute garbage
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, DEV_BAD_SMEM_ALIGN);
+        return;
+    }
+    if (warp == 0) {
+        if (lane < p.stages) {
+            mbar_init(&ctl->full[lane], 1);
+            mbar_init(&ctl->empty[lane], 1);
+        } else if (lane == 8) mbar_init(&ctl->accum[0], 1);
+        else if (lane == 9) ctl->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(&ctl->tmem, columns);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem;
+    begin();
+
+    const int token_tiles = (p.batch + p.tokens - 1) / p.tokens, tile = blockIdx.x / p.split;
+    const int b0 = (tile % token_tiles) * p.tokens, o0 = (tile / token_tiles) * 128;
+    const int k0 = (int)((long long)p.blocks * rank / p.split), k1 = (int)((long long)p.blocks * (rank + 1) / p.split);      // at least one block: blocks >= split
+    const int used = min(p.tokens, p.batch - b0);
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t parity = 1;
+            bool ok = true;
+            for (int k = k0; k < k1; ++k) {
+                ok = mbar_wait(&ctl->empty[s], parity, abort_flag, p.status, DEV_TIMEOUT_EMPTY);
+                if (!ok) break;
+                mbar_arrive_expect_tx(&ctl->full[s], stage_bytes);
+                tma_load_2d(smem + (size_t)s * stage_bytes, &w_map, &ctl->full[s], k * I8_KB, o0);
+                tma_load_2d(smem + (size_t)s * stage_bytes + I8_A_BYTES, &x_map, &ctl->full[s], k * I8_KB, b0);
+                if (++s == p.stages) { s = 0; parity ^= 1; }
+            }
+            if (!ok) let_copies_land();
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = i8_idesc(128, p.tokens);
+            int s = 0;
+            uint32_t parity = 0;
+            bool ok = true;
+            for (int k = k0; k < k1; ++k) {
+                ok = mbar_wait(&ctl->full[s], parity, abort_flag, p.status, DEV_TIMEOUT_FULL);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t a = make_sw128_desc(smem_u32(smem + (size_t)s * stage_bytes)), b = make_sw128_desc(smem_u32(smem + (size_t)s * stage_bytes + I8_A_BYTES));
+#pragma unroll
+                for (int q = 0; q < I8_KB / 32; ++q) umma_i8(tmem, a + (uint64_t)(2 * q), b + (uint64_t)(2 * q), idesc, (k != k0 || q) ? 1u : 0u);
+                umma_commit(&ctl->empty[s]);
+                if (++s == p.stages) { s = 0; parity ^= 1; }
+            }
+            if (ok) umma_commit(&ctl->accum[0]);
+        }
+    }
+    const int quad = warp & 3, o = o0 + quad * 32 + lane;
+    const bool there = warp >= 2 && o < p.rows;
+    const float channel = there ? __ldg(p.w_scale + o) : 0.f;
+    auto store = [&](int j, int sum) {       // of token j of the tile
+        const float y = ((float)sum * __ldg(p.x_scale + b0 + j)) * channel;
+        const long long to = (long long)(b0 + j) * p.rows + o;
+        if (!there) return;
+        if (p.y_dtype == LRBI_Y_F32) static_cast<float *>(p.y)[to] = y;
+        else static_cast<uint16_t *>(p.y)[to] = (uint16_t)pack_bf16(y, 0.f);
+    };
+    bool ok = true;
+    if (warp >= 2) {
+        ok = mbar_wait(&ctl->accum[0], 0, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
+        __syncwarp();
+        ok = ok && *abort_flag == 0;
+        if (ok) {
+            tc_fence_after();
+            // All products are through, and so are the copies that they waited for: the stages are free for the partial sums.
+            int *part = reinterpret_cast<int *>(smem);
+            for (int c = 0; c < used; c += 16) {
+                uint32_t v[16];
+                tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (p.split > 1) part[(c + j) * 128 + quad * 32 + lane] = (int)v[j];
+                    else if (c + j < used) store(c + j, (int)v[j]);
+                }
+            }
+        }
+    }
+    let_next();
+    __syncwarp();
+    if (p.split > 1) {
+        cluster_sync_all();
+        if (warp >= 2 && ok) {
+            const int j0 = used * rank / p.split, j1 = used * (rank + 1) / p.split;
+            const uint32_t mine = smem_u32(smem) + (quad * 32 + lane) * 4;
+            for (int j = j0; j < j1; ++j) {
+                int sum = 0;
+                for (int r = 0; r < p.split; ++r) {
+                    uint32_t there_;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_) : "r"(mine + j * 512), "r"(r));
+                    sum += cluster_int(there_);
+                }
+                store(j, sum);
+            }
+        }
+        __syncwarp();
+        cluster_sync_all();          // a CTA stays while others read its sums
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, columns);
+    }
+}
+
+namespace {
+
+lrbi_status i8_map(CUtensorMap *map, const int8_t *q, int rows, int cols, int pitch, int box_rows)
+{
+    const EncodeTiledFn encode = get_encode_fn();
+    if (!encode) { note_cuda_error(-1); return LRBI_ERR_CUDA; }
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {I8_KB, (cuuint32_t)box_rows}, each[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(q), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { note_cuda_error((int)r); return LRBI_ERR_CUDA; }
+    return LRBI_OK;
+}
+
+I8Tc i8_args(const I8Product &p)
+{
+    I8Tc t = {};
+    t.x_scale = p.x_scale; t.w_scale = p.w_scale;
+    t.y = p.y; t.y_dtype = p.y_dtype;
+    t.rows = p.rows; t.batch = p.batch;
+    t.blocks = (p.cols + I8_KB - 1) / I8_KB;
+    const int size = p.y_dtype == LRBI_Y_F32 ? 4 : 2;
+    t.vector = reinterpret_cast<uintptr_t>(p.y) % 16 == 0 && (long long)p.rows * size % 16 == 0;
+    t.status = device_status_ptr();
+    return t;
+}
+
+}  // namespace
+
+lrbi_status launch_i8_long(const I8Product &p, cudaStream_t s)
+{
+    I8Tc t = i8_args(p);
+    t.stages = 6;
+    const size_t smem = (size_t)t.stages * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl);
+    static_assert((size_t)6 * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl) <= I8_SHARED, "");
+    CUtensorMap x_map, w_map;
+    lrbi_status rc = i8_map(&x_map, p.x, p.batch, p.cols, p.pitch, 128);
+    if (rc == LRBI_OK) rc = i8_map(&w_map, p.w, p.rows, p.cols, p.pitch, 128);
+    if (rc != LRBI_OK) return rc;
+    const long long tiles = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
+    if (tiles > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
+    const int pairs = (int)(tiles < NORM_SMS / 2 ? tiles : NORM_SMS / 2);
+    return launch_kernel(i8_long_kernel, dim3(2 * pairs), dim3(I8_THREADS), smem, s, 2, x_map, w_map, t);
+}
+
+lrbi_status launch_i8_split(const I8Product &p, int split, cudaStream_t s)
+{
+    I8Tc t = i8_args(p);
+    t.tokens = p.batch >= 256 ? 256 : (p.batch + 15) / 16 * 16;
+    t.split = split;
+    const int stage = I8_A_BYTES + t.tokens * I8_KB;
+    const long long tiles = (long long)((p.batch + t.tokens - 1) / t.tokens) * ((p.rows + 127) / 128);
+    if (tiles * split > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
+    t.stages = (int)((I8_SHARED - sizeof(I8Ctl)) / stage);
+    if (t.stages > 8) t.stages = 8;
+    const size_t smem = (size_t)t.stages * stage + sizeof(I8Ctl);      // at least four stages of 48 KB: room for 256 tokens' sums
+    CUtensorMap x_map, w_map;
+    lrbi_status rc = i8_map(&x_map, p.x, p.batch, p.cols, p.pitch, t.tokens);
+    if (rc == LRBI_OK) rc = i8_map(&w_map, p.w, p.rows, p.cols, p.pitch, 128);
+    if (rc != LRBI_OK) return rc;
+    return launch_kernel(i8_split_kernel, dim3((unsigned)(tiles * split)), dim3(I8_THREADS), smem, s, split, x_map, w_map, t);
+}
+
+}  // namespace lrbi

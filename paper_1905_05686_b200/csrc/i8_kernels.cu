@@ -5,6 +5,7 @@
 //
 // Rows of q start on 16-byte boundaries and hold zeros past the last column, so that a product takes them 16 bytes at a time.
 #include "activation.cuh"
+#include "norm_common.cuh"
 
 namespace lrbi {
 
@@ -236,9 +237,18 @@ lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *
 
 lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
 {
+    if (p.batch > 16) {
+        const long long pairs = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
+        if (pairs >= 32) return launch_i8_long(p, s);
+        const int blocks = (p.cols + 127) / 128;
+        const long long tiles = (long long)((p.batch + 255) / 256) * ((p.rows + 127) / 128);
+        int split = 1;
+        while (split < 8 && tiles * split * 2 <= NORM_SMS && blocks >= 4 * split) split *= 2;
+        return launch_i8_split(p, split, s);
+    }
     const int tiles = (p.rows + 15) / 16;
-    if (p.batch <= 8) return launch_kernel(i8_few_kernel<1>, dim3(tiles, 1), dim3(32 * I8_WARPS), 0, s, 1, p);
-    return launch_kernel(i8_few_kernel<2>, dim3(tiles, (p.batch + 15) / 16), dim3(32 * I8_WARPS), 0, s, 1, p);
+    if (p.batch <= 8) return launch_kernel(i8_few_kernel<1>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
+    return launch_kernel(i8_few_kernel<2>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
 }
 
 }  // namespace lrbi
