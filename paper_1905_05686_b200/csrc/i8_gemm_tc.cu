@@ -9,6 +9,8 @@
 //          distributed shared memory (whole numbers: the same bits however they are cut), so that all SMs stream the weights.
 //
 // Every wait is bounded; a wait that runs out leaves a code in the device status word, and the CTA ends early.
+#include <algorithm>
+
 #include "norm_common.cuh"
 #include "tcgen05_ptx.cuh"
 
@@ -16,8 +18,9 @@ namespace lrbi {
 
 constexpr int I8_KB = 128;                               // columns (and bytes of a row) of a stage
 constexpr int I8_A_BYTES = 128 * I8_KB;                  // 128 rows of the M operand
-constexpr int I8_THREADS = 192;                          // warp 0 copies, warp 1 multiplies, warps 2-5 scale and store
-constexpr int I8_EPI_WARPS = 4;
+constexpr int I8_EPI_WARPS = 8;                          // long: warps 2-9 scale and store (warp 0 copies, warp 1 multiplies)
+constexpr int I8_LONG_THREADS = 32 * (2 + I8_EPI_WARPS);
+constexpr int I8_SPLIT_WARPS = 6;                        // split: warps 2-5 empty tensor memory, all of them add up and store
 constexpr size_t I8_SHARED = 226 * 1024;                 // dynamic shared memory of a CTA that has an SM to itself
 
 struct I8Ctl {
@@ -36,7 +39,7 @@ struct I8Tc {
     int stages;
     int tokens;                      // split: of a tile
     int split;
-    bool vector;                     // rows of Y are whole 16-byte vectors
+    int vector;                      // bytes that an access to Y may have: 16, 8, 4 or 2
     int *status;
 };
 
@@ -59,17 +62,29 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
-__device__ __forceinline__ uint32_t in_cta(const void *mine, uint32_t rank)      // the same place in the shared memory of another CTA of the cluster
+__device__ __forceinline__ uint32_t in_cta(uint32_t mine, uint32_t rank)      // the same place in the shared memory of another CTA of the cluster
 {
     uint32_t there;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(mine)), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(rank));
     return there;
 }
-__device__ __forceinline__ int cluster_int(uint32_t at)
+// Four neighbouring whole numbers of shared memory of the cluster, or four that are 32 apart.
+__device__ __forceinline__ int4 cluster_int4(uint32_t at)
 {
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
+}
+__device__ __forceinline__ int4 cluster_ints(uint32_t at)
+{
+    int4 v;
+    asm volatile("ld.shared::cluster.s32 %0, [%4];\n\tld.shared::cluster.s32 %1, [%4+128];\n\tld.shared::cluster.s32 %2, [%4+256];\n\tld.shared::cluster.s32 %3, [%4+384];"
+                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void l2_prefetch_2d(const CUtensorMap *map, int x, int y)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t at, int (&v)[32])
 {
@@ -78,6 +93,26 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, int (&v)[32])
                    "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
                    "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(at) : "memory");
+}
+
+// Stores `bytes` (2 to 16, whole values) of a 16-byte piece in accesses of `vector` bytes at most.
+__device__ __forceinline__ void store_piece(uint8_t *to, const uint4 &v, int bytes, int vector)
+{
+    if (bytes == 16 && vector == 16) *reinterpret_cast<uint4 *>(to) = v;
+    else if (bytes == 16 && vector == 8) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(v.x, v.y);
+        *reinterpret_cast<uint2 *>(to + 8) = make_uint2(v.z, v.w);
+    } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (4 * i + 4 <= bytes && vector >= 4) *reinterpret_cast<uint32_t *>(to + 4 * i) = w[i];
+            else {
+                if (4 * i < bytes) *reinterpret_cast<uint16_t *>(to + 4 * i) = (uint16_t)w[i];
+                if (4 * i + 2 < bytes) *reinterpret_cast<uint16_t *>(to + 4 * i + 2) = (uint16_t)(w[i] >> 16);
+            }
+        }
+    }
 }
 
 // Copies that are under way must land before shared memory is given up: about 2 ms, far beyond any of them.
@@ -91,9 +126,10 @@ __device__ __forceinline__ void let_copies_land()
 // Many tokens
 // ---------------------------------------------------------------------------------------------------------------------
 // The tile's M is the token (a lane of tensor memory), its N the channel: a thread has neighbouring outputs of one row of Y.
-// They go through 4 KB a warp, 32 rows x 128 bytes in the swizzled order, and out as whole lines.
-constexpr int I8_LONG_STAGE = 2 * I8_A_BYTES, I8_EPI_BYTES = 32 * 128 + 256 * 4;
-__global__ void __launch_bounds__(I8_THREADS, 1) i8_long_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
+// They go through 2 KB a warp, 32 rows x 64 bytes with the pieces of a row in an order that keeps the banks apart, and out as
+// whole sectors.
+constexpr int I8_LONG_STAGE = 2 * I8_A_BYTES, I8_EPI_BYTES = 32 * 64 + 128 * 4;
+__global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t *epi = smem + (size_t)p.stages * I8_LONG_STAGE;
@@ -146,7 +182,7 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_long_kernel(const __grid_con
                     ok = mbar_wait(&ctl->empty[s], parity, abort_flag, p.status, DEV_TIMEOUT_EMPTY);
                     if (!ok) break;
                     if (rank == 0) mbar_arrive_expect_tx(&ctl->full[s], 2 * I8_LONG_STAGE);       // of both CTAs
-                    const uint32_t bar = in_cta(&ctl->full[s], 0);
+                    const uint32_t bar = in_cta(smem_u32(&ctl->full[s]), 0);
                     uint8_t *a = smem + (size_t)s * I8_LONG_STAGE;
                     tma_load_2d_pair(a, &x_map, bar, k * I8_KB, b0 + (int)rank * 128);
                     tma_load_2d_pair(a + I8_A_BYTES, &w_map, bar, k * I8_KB, o0 + (int)rank * 128);
@@ -180,45 +216,35 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_long_kernel(const __grid_con
             }
         }
     } else {
-        const int quad = warp & 3;
+        // a warp has the tokens of its quarter of tensor memory and half of the channels
+        const int quad = warp & 3, half = (warp - 2) >> 2;
         uint8_t *stage = epi + (warp - 2) * I8_EPI_BYTES;
-        float *scale = reinterpret_cast<float *>(stage + 32 * 128);
+        float *scale = reinterpret_cast<float *>(stage + 32 * 64);
         const bool f32 = p.y_dtype == LRBI_Y_F32;
-        const int each = f32 ? 32 : 64;          // columns of 128 bytes
+        const int size = f32 ? 4 : 2;
         bool ok = true;
         int n = 0;
         for (int t = first; t < tiles; t += step, ++n) {
             int b0, o0;
             tile_at(t, b0, o0);
             b0 += (int)rank * 128 + quad * 32;
+            o0 += half * 128;
             const int left = min(32, p.batch - b0);      // rows of Y that the warp has
             const float token = lane < left ? __ldg(p.x_scale + b0 + lane) : 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) scale[i * 32 + lane] = o0 + i * 32 + lane < p.rows ? __ldg(p.w_scale + o0 + i * 32 + lane) : 0.f;
+            for (int i = 0; i < 4; ++i) scale[i * 32 + lane] = o0 + i * 32 + lane < p.rows ? __ldg(p.w_scale + o0 + i * 32 + lane) : 0.f;
             ok = mbar_wait(&ctl->accum[n & 1], n >> 1 & 1, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
             __syncwarp();                                // the loads below are the whole warp's: one verdict for all lanes
             if (!ok || *abort_flag) break;
             tc_fence_after();
-            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (n & 1) * 256;
-            for (int c = 0; c < 256; c += each) {
-                uint4 *own = reinterpret_cast<uint4 *>(stage + lane * 128);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1 && f32) break;
-                    int v[32];
-                    tmem_ld32(from + c + 32 * h, v);
-                    tmem_ld_wait();
-                    const float4 *w = reinterpret_cast<const float4 *>(scale + c + 32 * h);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 s = w[i];
-                        const float y0 = ((float)v[4 * i] * token) * s.x, y1 = ((float)v[4 * i + 1] * token) * s.y, y2 = ((float)v[4 * i + 2] * token) * s.z,
-                                    y3 = ((float)v[4 * i + 3] * token) * s.w;
-                        if (f32) own[i ^ (lane & 7)] = make_uint4(__float_as_uint(y0), __float_as_uint(y1), __float_as_uint(y2), __float_as_uint(y3));
-                        else *(reinterpret_cast<uint2 *>(own + ((4 * h + i / 2) ^ (lane & 7))) + (i & 1)) = make_uint2(pack_bf16(y0, y1), pack_bf16(y2, y3));
-                    }
-                }
-                if (c + each >= 256) {                   // read: the accumulator may be overwritten
+            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (n & 1) * 256 + half * 128;
+            uint4 *own = reinterpret_cast<uint4 *>(stage + lane * 64);
+            const int swap = lane >> 1 & 3;
+            for (int c = 0; c < 128; c += 32) {
+                int v[32];
+                tmem_ld32(from + c, v);
+                tmem_ld_wait();
+                if (c == 96) {                           // read: the accumulator may be overwritten
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
@@ -226,28 +252,39 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_long_kernel(const __grid_con
                         else mbar_arrive_remote(&ctl->drained[n & 1], 0);
                     }
                 }
-                __syncwarp();
-                if (p.vector) {
-                    const int piece = lane & 7, per = f32 ? 4 : 8, o = o0 + c + piece * per;
+                const float4 *w = reinterpret_cast<const float4 *>(scale + c);
+                float y[32];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int r = i * 4 + (lane >> 3);
-                        if (r < left && o < p.rows)
-                            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + ((long long)(b0 + r) * p.rows + o) * (f32 ? 4 : 2)) =
-                                *reinterpret_cast<const uint4 *>(stage + r * 128 + ((piece ^ (r & 7)) << 4));
-                    }
-                } else {
-                    for (int r = 0; r < left; ++r)
-                        for (int e = lane; e < each; e += 32) {
-                            const int o = o0 + c + e, at = e * (f32 ? 4 : 2);
-                            const uint8_t *from8 = stage + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15);
-                            if (o < p.rows) {
-                                if (f32) static_cast<float *>(p.y)[(long long)(b0 + r) * p.rows + o] = *reinterpret_cast<const float *>(from8);
-                                else static_cast<uint16_t *>(p.y)[(long long)(b0 + r) * p.rows + o] = *reinterpret_cast<const uint16_t *>(from8);
-                            }
-                        }
+                for (int i = 0; i < 8; ++i) {
+                    const float4 s = w[i];
+                    y[4 * i] = ((float)v[4 * i] * token) * s.x;
+                    y[4 * i + 1] = ((float)v[4 * i + 1] * token) * s.y;
+                    y[4 * i + 2] = ((float)v[4 * i + 2] * token) * s.z;
+                    y[4 * i + 3] = ((float)v[4 * i + 3] * token) * s.w;
                 }
-                __syncwarp();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {            // fp32: 16 columns at a time
+                    if (h == 1 && !f32) break;
+                    if (f32) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            own[i ^ swap] = make_uint4(__float_as_uint(y[16 * h + 4 * i]), __float_as_uint(y[16 * h + 4 * i + 1]), __float_as_uint(y[16 * h + 4 * i + 2]), __float_as_uint(y[16 * h + 4 * i + 3]));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            own[i ^ swap] = make_uint4(pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]), pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7]));
+                    }
+                    __syncwarp();
+                    const int piece = lane & 3, o = o0 + c + h * 16 + piece * (16 / size), some = min(16 / size, p.rows - o);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i * 8 + (lane >> 2);
+                        if (r < left && some > 0)
+                            store_piece(static_cast<uint8_t *>(p.y) + ((long long)(b0 + r) * p.rows + o) * size, *reinterpret_cast<const uint4 *>(stage + r * 64 + ((piece ^ (r >> 1 & 3)) << 4)),
+                                        some * size, p.vector);
+                    }
+                    __syncwarp();
+                }
             }
         }
     }
@@ -265,8 +302,10 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_long_kernel(const __grid_con
 // ---------------------------------------------------------------------------------------------------------------------
 // Fewer tokens
 // ---------------------------------------------------------------------------------------------------------------------
-// The tile's M is the channel, its N the token (a multiple of 16 up to 256, as many as there are).
-__global__ void __launch_bounds__(I8_THREADS, 1) i8_split_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
+// The tile's M is the channel, its N the token (a multiple of 16 up to 256, as many as there are).  TWO: two CTAs fit an SM, so
+// that one is set up, and asks for its first weights, while another ends.
+template <bool TWO>
+__global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     const int stage_bytes = I8_A_BYTES + p.tokens * I8_KB;
@@ -279,6 +318,10 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_split_kernel(const __grid_co
         if (threadIdx.x == 0) atomicCAS(p.status, 0, DEV_BAD_SMEM_ALIGN);
         return;
     }
+    const int token_tiles = (p.batch + p.tokens - 1) / p.tokens, tile = blockIdx.x / p.split;
+    const int b0 = (tile % token_tiles) * p.tokens, o0 = (tile / token_tiles) * 128;
+    const int k0 = (int)((long long)p.blocks * rank / p.split), k1 = (int)((long long)p.blocks * (rank + 1) / p.split);      // at least one block: blocks >= split
+    const int used = min(p.tokens, p.batch - b0);
     if (warp == 0) {
         if (lane < p.stages) {
             mbar_init(&ctl->full[lane], 1);
@@ -288,16 +331,14 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_split_kernel(const __grid_co
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(&ctl->tmem, columns);
+    // A hint that needs no order: the first weights come to L2 while the kernel before this one (the tokens') ends.
+    if (warp == 2 && lane < p.stages && k0 + lane < k1) l2_prefetch_2d(&w_map, (k0 + lane) * I8_KB, o0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     begin();
 
-    const int token_tiles = (p.batch + p.tokens - 1) / p.tokens, tile = blockIdx.x / p.split;
-    const int b0 = (tile % token_tiles) * p.tokens, o0 = (tile / token_tiles) * 128;
-    const int k0 = (int)((long long)p.blocks * rank / p.split), k1 = (int)((long long)p.blocks * (rank + 1) / p.split);      // at least one block: blocks >= split
-    const int used = min(p.tokens, p.batch - b0);
     if (warp == 0) {
         if (lane == 0) {
             int s = 0;
@@ -331,60 +372,81 @@ __global__ void __launch_bounds__(I8_THREADS, 1) i8_split_kernel(const __grid_co
             }
             if (ok) umma_commit(&ctl->accum[0]);
         }
-    }
-    const int quad = warp & 3, o = o0 + quad * 32 + lane;
-    const bool there = warp >= 2 && o < p.rows;
-    const float channel = there ? __ldg(p.w_scale + o) : 0.f;
-    auto store = [&](int j, int sum) {       // of token j of the tile
-        const float y = ((float)sum * __ldg(p.x_scale + b0 + j)) * channel;
-        const long long to = (long long)(b0 + j) * p.rows + o;
-        if (!there) return;
-        if (p.y_dtype == LRBI_Y_F32) static_cast<float *>(p.y)[to] = y;
-        else static_cast<uint16_t *>(p.y)[to] = (uint16_t)pack_bf16(y, 0.f);
-    };
-    bool ok = true;
-    if (warp >= 2) {
-        ok = mbar_wait(&ctl->accum[0], 0, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
+    } else {
+        const int quad = warp & 3;
+        bool ok = mbar_wait(&ctl->accum[0], 0, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
         __syncwarp();
-        ok = ok && *abort_flag == 0;
-        if (ok) {
+        if (ok && *abort_flag == 0) {
             tc_fence_after();
-            // All products are through, and so are the copies that they waited for: the stages are free for the partial sums.
-            int *part = reinterpret_cast<int *>(smem);
-            for (int c = 0; c < used; c += 16) {
-                uint32_t v[16];
-                tmem_ld16(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+            // All products are through, and so are the copies that they waited for: the sums, [token][channel], take the stages' place.
+            int *to = reinterpret_cast<int *>(smem) + quad * 32 + lane;
+            for (int c = 0; c < p.tokens; c += 32) {     // (the last 16 may be beyond the tile, not beyond what was allocated)
+                int v[32];
+                tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
                 tmem_ld_wait();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (p.split > 1) part[(c + j) * 128 + quad * 32 + lane] = (int)v[j];
-                    else if (c + j < used) store(c + j, (int)v[j]);
-                }
+                for (int j = 0; j < 32; ++j) if (c + j < p.tokens) to[(c + j) * 128] = v[j];
             }
         }
+        tc_fence_before();
     }
     let_next();
     __syncwarp();
-    if (p.split > 1) {
-        cluster_sync_all();
-        if (warp >= 2 && ok) {
-            const int j0 = used * rank / p.split, j1 = used * (rank + 1) / p.split;
-            const uint32_t mine = smem_u32(smem) + (quad * 32 + lane) * 4;
-            for (int j = j0; j < j1; ++j) {
-                int sum = 0;
-                for (int r = 0; r < p.split; ++r) {
-                    uint32_t there_;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there_) : "r"(mine + j * 512), "r"(r));
-                    sum += cluster_int(there_);
+    if (p.split > 1) cluster_sync_all();
+    else __syncthreads();
+    // The CTAs of the cluster take the tokens in equal parts, a warp one at a time: four neighbouring channels a lane where rows of
+    // Y are whole vectors of four, else channels 32 apart.
+    if (*abort_flag == 0) {
+        const bool f32 = p.y_dtype == LRBI_Y_F32, four = p.vector >= (f32 ? 16 : 8);
+        const int j1 = used * (rank + 1) / p.split;
+        const int gap = four ? 1 : 32, o = o0 + lane * (four ? 4 : 1);
+        float channel[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) channel[i] = o + i * gap < p.rows ? __ldg(p.w_scale + o + i * gap) : 0.f;
+        const uint32_t mine = smem_u32(smem) + lane * (four ? 16 : 4);
+        constexpr int T = 4;                     // tokens whose loads are under way together: they take most of a microsecond each
+        for (int j = used * rank / p.split + warp; j < j1; j += I8_SPLIT_WARPS * T) {
+            float token[T];
+            int4 sum[T];
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                token[t] = __ldg(p.x_scale + b0 + min(j + t * I8_SPLIT_WARPS, j1 - 1));
+                sum[t] = make_int4(0, 0, 0, 0);
+            }
+#pragma unroll 4
+            for (int r = 0; r < p.split; ++r) {
+                const uint32_t from = p.split > 1 ? in_cta(mine, r) : mine;      // (a CTA's own addresses are addresses of the cluster, too)
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    if (j + t * I8_SPLIT_WARPS >= j1) break;
+                    const uint32_t at = from + (j + t * I8_SPLIT_WARPS) * 512;
+                    const int4 v = four ? cluster_int4(at) : cluster_ints(at);
+                    sum[t].x += v.x; sum[t].y += v.y; sum[t].z += v.z; sum[t].w += v.w;
                 }
-                store(j, sum);
+            }
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                const int own = j + t * I8_SPLIT_WARPS;
+                if (own >= j1) break;
+                const float y[4] = {((float)sum[t].x * token[t]) * channel[0], ((float)sum[t].y * token[t]) * channel[1], ((float)sum[t].z * token[t]) * channel[2],
+                                    ((float)sum[t].w * token[t]) * channel[3]};
+                const long long to = (long long)(b0 + own) * p.rows + o;
+                if (four && o < p.rows) {        // rows is a multiple of four: all of them are there
+                    if (f32) *reinterpret_cast<float4 *>(static_cast<float *>(p.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
+                    else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.y) + to) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+                } else if (!four) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (o + 32 * i >= p.rows) continue;
+                        if (f32) static_cast<float *>(p.y)[to + 32 * i] = y[i];
+                        else static_cast<uint16_t *>(p.y)[to + 32 * i] = (uint16_t)pack_bf16(y[i], 0.f);
+                    }
+                }
             }
         }
-        __syncwarp();
-        cluster_sync_all();          // a CTA stays while others read its sums
     }
-    tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    if (p.split > 1) cluster_sync_all();         // a CTA stays while others read its sums
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, columns);
@@ -412,8 +474,8 @@ I8Tc i8_args(const I8Product &p)
     t.y = p.y; t.y_dtype = p.y_dtype;
     t.rows = p.rows; t.batch = p.batch;
     t.blocks = (p.cols + I8_KB - 1) / I8_KB;
-    const int size = p.y_dtype == LRBI_Y_F32 ? 4 : 2;
-    t.vector = reinterpret_cast<uintptr_t>(p.y) % 16 == 0 && (long long)p.rows * size % 16 == 0;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p.y) | (uintptr_t)((long long)p.rows * (p.y_dtype == LRBI_Y_F32 ? 4 : 2));
+    t.vector = at % 16 == 0 ? 16 : at % 8 == 0 ? 8 : at % 4 == 0 ? 4 : 2;
     t.status = device_status_ptr();
     return t;
 }
@@ -433,7 +495,7 @@ lrbi_status launch_i8_long(const I8Product &p, cudaStream_t s)
     const long long tiles = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
     if (tiles > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
     const int pairs = (int)(tiles < NORM_SMS / 2 ? tiles : NORM_SMS / 2);
-    return launch_kernel(i8_long_kernel, dim3(2 * pairs), dim3(I8_THREADS), smem, s, 2, x_map, w_map, t);
+    return launch_kernel(i8_long_kernel, dim3(2 * pairs), dim3(I8_LONG_THREADS), smem, s, 2, x_map, w_map, t);
 }
 
 lrbi_status launch_i8_split(const I8Product &p, int split, cudaStream_t s)
@@ -444,14 +506,15 @@ lrbi_status launch_i8_split(const I8Product &p, int split, cudaStream_t s)
     const int stage = I8_A_BYTES + t.tokens * I8_KB;
     const long long tiles = (long long)((p.batch + t.tokens - 1) / t.tokens) * ((p.rows + 127) / 128);
     if (tiles * split > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
-    t.stages = (int)((I8_SHARED - sizeof(I8Ctl)) / stage);
-    if (t.stages > 8) t.stages = 8;
-    const size_t smem = (size_t)t.stages * stage + sizeof(I8Ctl);      // at least four stages of 48 KB: room for 256 tokens' sums
+    const bool two = t.tokens <= 128;            // three stages or more in half of an SM's shared memory
+    t.stages = std::min(8, (int)(((two ? I8_SHARED / 2 : I8_SHARED) - sizeof(I8Ctl)) / stage));
+    const size_t smem = (size_t)t.stages * stage + sizeof(I8Ctl);      // in all cases more than the 512 bytes a token that the sums take
     CUtensorMap x_map, w_map;
     lrbi_status rc = i8_map(&x_map, p.x, p.batch, p.cols, p.pitch, t.tokens);
     if (rc == LRBI_OK) rc = i8_map(&w_map, p.w, p.rows, p.cols, p.pitch, 128);
     if (rc != LRBI_OK) return rc;
-    return launch_kernel(i8_split_kernel, dim3((unsigned)(tiles * split)), dim3(I8_THREADS), smem, s, split, x_map, w_map, t);
+    const dim3 grid((unsigned)(tiles * split)), block(32 * I8_SPLIT_WARPS);
+    return two ? launch_kernel(i8_split_kernel<true>, grid, block, smem, s, split, x_map, w_map, t) : launch_kernel(i8_split_kernel<false>, grid, block, smem, s, split, x_map, w_map, t);
 }
 
 }  // namespace lrbi

@@ -4,6 +4,8 @@
 //   product:   Y[b][o] = (sum over i of q_X[b][i] * q_W[o][i]) * scale_X[b] * scale_W[o]   (the sum is a whole number, exact)
 //
 // Rows of q start on 16-byte boundaries and hold zeros past the last column, so that a product takes them 16 bytes at a time.
+#include <algorithm>
+
 #include "activation.cuh"
 #include "norm_common.cuh"
 
@@ -235,20 +237,27 @@ lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *
     return LRBI_OK;
 }
 
-lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
+lrbi_status launch_i8_few(const I8Product &p, cudaStream_t s)
 {
-    if (p.batch > 16) {
-        const long long pairs = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
-        if (pairs >= 32) return launch_i8_long(p, s);
-        const int blocks = (p.cols + 127) / 128;
-        const long long tiles = (long long)((p.batch + 255) / 256) * ((p.rows + 127) / 128);
-        int split = 1;
-        while (split < 8 && tiles * split * 2 <= NORM_SMS && blocks >= 4 * split) split *= 2;
-        return launch_i8_split(p, split, s);
-    }
     const int tiles = (p.rows + 15) / 16;
     if (p.batch <= 8) return launch_kernel(i8_few_kernel<1>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
     return launch_kernel(i8_few_kernel<2>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
+}
+
+// How long the two tensor-core kernels take, in microseconds, as fitted to their times: what a launch costs, a block of 128 columns of
+// every tile that a CTA (or pair) has in turn, and for a split the sums of a tile's tokens; neither less than memory takes.
+lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
+{
+    if (p.batch <= 8) return launch_i8_few(p, s);
+    const int blocks = (p.cols + 127) / 128, tokens = p.batch >= 256 ? 256 : (p.batch + 15) / 16 * 16;
+    const long long tiles = (long long)((p.batch + tokens - 1) / tokens) * ((p.rows + 127) / 128);
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= NORM_SMS * (tokens <= 128 ? 5 : 4) / 4 && blocks >= 4 * split) split *= 2;
+    const long long pairs = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
+    const double bytes = ((double)p.rows * p.cols + (double)p.batch * p.cols + 2. * p.batch * p.rows) / 5.2e6;
+    const double few = 4. + 0.018 * tokens + std::max((double)((blocks + split - 1) / split) * (0.3 + 0.0009 * tokens) * ((tiles * split + NORM_SMS - 1) / NORM_SMS), bytes);
+    const double many = 4.5 + std::max((double)((pairs + NORM_SMS / 2 - 1) / (NORM_SMS / 2)) * blocks * 0.275, bytes);
+    return many < few ? launch_i8_long(p, s) : launch_i8_split(p, split, s);
 }
 
 }  // namespace lrbi
