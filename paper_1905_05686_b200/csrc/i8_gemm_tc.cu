@@ -26,6 +26,7 @@ constexpr size_t I8_SHARED = 226 * 1024;                 // dynamic shared memor
 struct I8Ctl {
     uint64_t full[8], empty[8];      // of the stages
     uint64_t accum[2], drained[2];   // of the accumulators
+    float token[256];                // split: the tile's scales
     uint32_t tmem;
     int abort_flag;
 };
@@ -68,18 +69,21 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t mine, uint32_t rank)      //
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(rank));
     return there;
 }
-// Four neighbouring whole numbers of shared memory of the cluster, or four that are 32 apart.
-__device__ __forceinline__ int4 cluster_int4(uint32_t at)
+// Four neighbouring whole numbers of shared memory of the cluster, or four that are 32 apart, where `on`; else zeros.  (A predicate,
+// not a branch: the loads of several tokens stay together.)
+__device__ __forceinline__ int4 cluster_int4(bool on, uint32_t at)
 {
     int4 v;
-    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t@p ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "r"(at), "r"((uint32_t)on) : "memory");
     return v;
 }
-__device__ __forceinline__ int4 cluster_ints(uint32_t at)
+__device__ __forceinline__ int4 cluster_ints(bool on, uint32_t at)
 {
     int4 v;
-    asm volatile("ld.shared::cluster.s32 %0, [%4];\n\tld.shared::cluster.s32 %1, [%4+128];\n\tld.shared::cluster.s32 %2, [%4+256];\n\tld.shared::cluster.s32 %3, [%4+384];"
-                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "r"(at) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t@p ld.shared::cluster.s32 %0, [%4];\n\t"
+                 "@p ld.shared::cluster.s32 %1, [%4+128];\n\t@p ld.shared::cluster.s32 %2, [%4+256];\n\t@p ld.shared::cluster.s32 %3, [%4+384];\n\t}"
+                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "r"(at), "r"((uint32_t)on) : "memory");
     return v;
 }
 __device__ __forceinline__ void l2_prefetch_2d(const CUtensorMap *map, int x, int y)
@@ -338,6 +342,13 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
     tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     begin();
+    // In the end the CTAs of the cluster take the tokens in equal parts, a warp one at a time: four neighbouring channels a lane where rows of
+    // Y are whole vectors of four, else channels 32 apart.
+    const bool f32 = p.y_dtype == LRBI_Y_F32, four = p.vector >= (f32 ? 16 : 8);
+    const int gap = four ? 1 : 32, o = o0 + lane * (four ? 4 : 1);
+    float channel[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) channel[i] = o + i * gap < p.rows ? __ldg(p.w_scale + o + i * gap) : 0.f;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -374,6 +385,7 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
         }
     } else {
         const int quad = warp & 3;
+        for (int j = threadIdx.x - 64; j < used; j += 128) ctl->token[j] = __ldg(p.x_scale + b0 + j);
         bool ok = mbar_wait(&ctl->accum[0], 0, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
         __syncwarp();
         if (ok && *abort_flag == 0) {
@@ -394,15 +406,8 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
     __syncwarp();
     if (p.split > 1) cluster_sync_all();
     else __syncthreads();
-    // The CTAs of the cluster take the tokens in equal parts, a warp one at a time: four neighbouring channels a lane where rows of
-    // Y are whole vectors of four, else channels 32 apart.
     if (*abort_flag == 0) {
-        const bool f32 = p.y_dtype == LRBI_Y_F32, four = p.vector >= (f32 ? 16 : 8);
         const int j1 = used * (rank + 1) / p.split;
-        const int gap = four ? 1 : 32, o = o0 + lane * (four ? 4 : 1);
-        float channel[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) channel[i] = o + i * gap < p.rows ? __ldg(p.w_scale + o + i * gap) : 0.f;
         const uint32_t mine = smem_u32(smem) + lane * (four ? 16 : 4);
         constexpr int T = 4;                     // tokens whose loads are under way together: they take most of a microsecond each
         for (int j = used * rank / p.split + warp; j < j1; j += I8_SPLIT_WARPS * T) {
@@ -410,7 +415,7 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
             int4 sum[T];
 #pragma unroll
             for (int t = 0; t < T; ++t) {
-                token[t] = __ldg(p.x_scale + b0 + min(j + t * I8_SPLIT_WARPS, j1 - 1));
+                token[t] = ctl->token[min(j + t * I8_SPLIT_WARPS, j1 - 1)];
                 sum[t] = make_int4(0, 0, 0, 0);
             }
 #pragma unroll 4
@@ -418,9 +423,9 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
                 const uint32_t from = p.split > 1 ? in_cta(mine, r) : mine;      // (a CTA's own addresses are addresses of the cluster, too)
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
-                    if (j + t * I8_SPLIT_WARPS >= j1) break;
+                    const bool on = j + t * I8_SPLIT_WARPS < j1;
                     const uint32_t at = from + (j + t * I8_SPLIT_WARPS) * 512;
-                    const int4 v = four ? cluster_int4(at) : cluster_ints(at);
+                    const int4 v = four ? cluster_int4(on, at) : cluster_ints(on, at);
                     sum[t].x += v.x; sum[t].y += v.y; sum[t].z += v.z; sum[t].w += v.w;
                 }
             }
@@ -498,15 +503,15 @@ lrbi_status launch_i8_long(const I8Product &p, cudaStream_t s)
     return launch_kernel(i8_long_kernel, dim3(2 * pairs), dim3(I8_LONG_THREADS), smem, s, 2, x_map, w_map, t);
 }
 
-lrbi_status launch_i8_split(const I8Product &p, int split, cudaStream_t s)
+lrbi_status launch_i8_split(const I8Product &p, int tokens, int split, cudaStream_t s)      // tokens of a tile: a multiple of 16, up to 256
 {
     I8Tc t = i8_args(p);
-    t.tokens = p.batch >= 256 ? 256 : (p.batch + 15) / 16 * 16;
+    t.tokens = tokens;
     t.split = split;
     const int stage = I8_A_BYTES + t.tokens * I8_KB;
     const long long tiles = (long long)((p.batch + t.tokens - 1) / t.tokens) * ((p.rows + 127) / 128);
     if (tiles * split > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
-    const bool two = t.tokens <= 128;            // three stages or more in half of an SM's shared memory
+    const bool two = t.tokens <= 128 && tiles * split > NORM_SMS;      // three stages or more in half of an SM's shared memory
     t.stages = std::min(8, (int)(((two ? I8_SHARED / 2 : I8_SHARED) - sizeof(I8Ctl)) / stage));
     const size_t smem = (size_t)t.stages * stage + sizeof(I8Ctl);      // in all cases more than the 512 bytes a token that the sums take
     CUtensorMap x_map, w_map;

@@ -24,9 +24,10 @@ struct TokenArgs {
 // blockDim = (threads of a row, rows of a block).  A thread has up to K chunks of its row in registers, as results of the
 // nonlinearity in fp32, between the maximum and the bytes; rows of more chunks than that are read, and activated, twice.
 template <int SRC, int ACT, bool STRIDED, int K>
-__global__ void __launch_bounds__(512) i8_tokens_kernel(TokenArgs a)
+__global__ void __launch_bounds__(512, 2) i8_tokens_kernel(TokenArgs a)
 {
     begin();
+    let_next();         // a product that follows is set up, and asks for its weights, meanwhile
     constexpr int SIZE = SRC == SRC_F32 ? 4 : 2;
     __shared__ uint32_t part[16];
     const int lane = kept_lane(), warp = threadIdx.x >> 5, warps = blockDim.x >> 5, team = threadIdx.y;
@@ -65,7 +66,6 @@ __global__ void __launch_bounds__(512) i8_tokens_kernel(TokenArgs a)
                 top = max(top, max(__float_as_uint(lo) & 0x7FFFFFFFu, __float_as_uint(hi) & 0x7FFFFFFFu));      // a NaN is above infinity
             }
     }
-    let_next();
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     if (warps > 1) {
         if (lane == 0) part[team * warps + warp] = top;
@@ -139,14 +139,14 @@ __global__ void __launch_bounds__(32 * I8_WARPS) i8_few_kernel(I8Product p)
     constexpr int U = 4;       // steps of a warp whose loads are under way together
     __shared__ int sums[I8_WARPS][8 * NT][16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int o0 = blockIdx.x * 16, b0 = blockIdx.y * 8 * NT;
+    const int o0 = blockIdx.x * 16;
     const int8_t *w0 = p.w + (long long)min(o0 + g, p.rows - 1) * p.pitch, *w1 = p.w + (long long)min(o0 + g + 8, p.rows - 1) * p.pitch;
     const int8_t *x[NT];
     bool on[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        on[n] = b0 + 8 * n + g < p.batch;
-        x[n] = p.x + (long long)(on[n] ? b0 + 8 * n + g : 0) * p.pitch;
+        on[n] = 8 * n + g < p.batch;
+        x[n] = p.x + (long long)(on[n] ? 8 * n + g : 0) * p.pitch;
     }
     int d[NT][4] = {};
     for (int c0 = warp * 64; c0 < p.pitch; c0 += I8_WARPS * 64 * U) {
@@ -175,11 +175,11 @@ __global__ void __launch_bounds__(32 * I8_WARPS) i8_few_kernel(I8Product p)
         for (int i = 0; i < 4; ++i) sums[warp][8 * n + 2 * t + (i & 1)][g + 8 * (i >> 1)] = d[n][i];
     __syncthreads();
     for (int k = threadIdx.x; k < 8 * NT * 16; k += 32 * I8_WARPS) {
-        const int b = b0 + k / 16, o = o0 + k % 16;
+        const int b = k / 16, o = o0 + k % 16;
         if (b >= p.batch || o >= p.rows) continue;
         int v = 0;
 #pragma unroll
-        for (int w = 0; w < I8_WARPS; ++w) v += sums[w][k / 16][k % 16];
+        for (int w = 0; w < I8_WARPS; ++w) v += sums[w][b][k % 16];
         const float y = ((float)v * __ldg(p.x_scale + b)) * __ldg(p.w_scale + o);
         const long long to = (long long)b * p.rows + o;
         if (p.y_dtype == LRBI_Y_F32) static_cast<float *>(p.y)[to] = y;
@@ -192,7 +192,7 @@ namespace {
 template <int SRC, int ACT, bool STRIDED, int K>
 lrbi_status tokens_launch(const TokenArgs &a, int threads, cudaStream_t s)
 {
-    const int teams = threads < 256 ? 256 / threads : 1;
+    const int teams = threads < 128 ? 128 / threads : 1;
     return launch_kernel(i8_tokens_kernel<SRC, ACT, STRIDED, K>, dim3((a.rows + teams - 1) / teams), dim3(threads, teams), 0, s, 1, a);
 }
 
@@ -200,6 +200,8 @@ template <int SRC, int ACT, bool STRIDED>
 lrbi_status tokens_chunks(const TokenArgs &a, cudaStream_t s)
 {
     const int spans = (a.cols + SPAN - 1) / SPAN;
+    // Many rows: a thread has four chunks of its row, all of them under way at once, and few others to wait for.
+    if (spans > 2 && (long long)a.rows * spans > 64 * NORM_SMS) return tokens_launch<SRC, ACT, STRIDED, 4>(a, 32 * std::min(16, (spans + 3) / 4), s);
     if (spans <= 16) return tokens_launch<SRC, ACT, STRIDED, 1>(a, 32 * (spans <= 1 ? 1 : spans <= 2 ? 2 : spans <= 4 ? 4 : spans <= 8 ? 8 : 16), s);
     if (spans <= 32) return tokens_launch<SRC, ACT, STRIDED, 2>(a, 512, s);
     return tokens_launch<SRC, ACT, STRIDED, 4>(a, 512, s);
@@ -244,20 +246,27 @@ lrbi_status launch_i8_few(const I8Product &p, cudaStream_t s)
     return launch_kernel(i8_few_kernel<2>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
 }
 
-// How long the two tensor-core kernels take, in microseconds, as fitted to their times: what a launch costs, a block of 128 columns of
-// every tile that a CTA (or pair) has in turn, and for a split the sums of a tile's tokens; neither less than memory takes.
+// Which kernel, by an estimate of the times of all, in microseconds, as fitted to those measured: what a launch costs; for every 128
+// columns that a CTA (or pair) takes in turn, more the more tokens a tile has; the sums and stores of a tile; neither less than
+// memory takes.
 lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
 {
     if (p.batch <= 8) return launch_i8_few(p, s);
-    const int blocks = (p.cols + 127) / 128, tokens = p.batch >= 256 ? 256 : (p.batch + 15) / 16 * 16;
-    const long long tiles = (long long)((p.batch + tokens - 1) / tokens) * ((p.rows + 127) / 128);
-    int split = 1;
-    while (split < 8 && tiles * split * 2 <= NORM_SMS * (tokens <= 128 ? 5 : 4) / 4 && blocks >= 4 * split) split *= 2;
+    const int blocks = (p.cols + 127) / 128;
+    const double memory = ((double)p.rows * p.cols + (double)p.batch * p.cols + (p.y_dtype == LRBI_Y_F32 ? 4. : 2.) * p.batch * p.rows) / 5.2e6;
     const long long pairs = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
-    const double bytes = ((double)p.rows * p.cols + (double)p.batch * p.cols + 2. * p.batch * p.rows) / 5.2e6;
-    const double few = 4. + 0.018 * tokens + std::max((double)((blocks + split - 1) / split) * (0.3 + 0.0009 * tokens) * ((tiles * split + NORM_SMS - 1) / NORM_SMS), bytes);
-    const double many = 4.5 + std::max((double)((pairs + NORM_SMS / 2 - 1) / (NORM_SMS / 2)) * blocks * 0.275, bytes);
-    return many < few ? launch_i8_long(p, s) : launch_i8_split(p, split, s);
+    double best = 4.5 + std::max((double)((pairs + NORM_SMS / 2 - 1) / (NORM_SMS / 2)) * blocks * 0.275, memory);
+    int tokens = 0, split = 0;      // none: the kernel for many tokens
+    for (int n : {16, 32, 64, 128, 256})
+        for (int k = 1; k <= 8 && k <= blocks; k *= 2) {
+            const int each = std::min(n, (p.batch + 15) / 16 * 16);
+            const long long ctas = (long long)((p.batch + each - 1) / each) * ((p.rows + 127) / 128) * k;
+            const double rounds = (double)((ctas + NORM_SMS - 1) / NORM_SMS);
+            const double t = 3.3 + std::max(rounds * (((blocks + k - 1) / k) * (0.2 + 0.0013 * each) + 0.6 + 0.0135 * each + (k == 8 ? 1. : 0.)), memory);
+            if (t < best) { best = t; tokens = each; split = k; }
+        }
+    if (p.batch <= 16 && 1.5 + 0.4 * blocks / 8. + memory * 2. < best) return launch_i8_few(p, s);
+    return split ? launch_i8_split(p, tokens, split, s) : launch_i8_long(p, s);
 }
 
 }  // namespace lrbi

@@ -237,7 +237,7 @@ lrbi_status launch_i8_tokens(const void *x, int dtype, long long stride, int row
 lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int8_t *q, float *scale, cudaStream_t s);
 lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s);
 lrbi_status launch_i8_long(const I8Product &p, cudaStream_t s);
-lrbi_status launch_i8_split(const I8Product &p, int split, cudaStream_t s);
+lrbi_status launch_i8_split(const I8Product &p, int tokens, int split, cudaStream_t s);
 
 // Between two blocks: out = scale * x + gate * norm(f), u = norm(out), and the backward pass; null pointers for what a call
 // does not have.
