@@ -20,13 +20,14 @@ constexpr int I8_KB = 128;                               // columns (and bytes o
 constexpr int I8_A_BYTES = 128 * I8_KB;                  // 128 rows of the M operand
 constexpr int I8_EPI_WARPS = 8;                          // long: warps 2-9 scale and store (warp 0 copies, warp 1 multiplies)
 constexpr int I8_LONG_THREADS = 32 * (2 + I8_EPI_WARPS);
-constexpr int I8_SPLIT_WARPS = 6;                        // split: warps 2-5 empty tensor memory, all of them add up and store
+constexpr int I8_SPLIT_WARPS = 10;                       // split: warps 2-9 empty tensor memory, all of them scale and store
 constexpr size_t I8_SHARED = 226 * 1024;                 // dynamic shared memory of a CTA that has an SM to itself
 
 struct I8Ctl {
     uint64_t full[8], empty[8];      // of the stages
     uint64_t accum[2], drained[2];   // of the accumulators
-    float token[256];                // split: the tile's scales
+    uint64_t added;                  // split: the other CTAs' sums have been added to this one's
+    alignas(16) float token[256];    // split: the tile's scales
     uint32_t tmem;
     int abort_flag;
 };
@@ -69,22 +70,11 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t mine, uint32_t rank)      //
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(rank));
     return there;
 }
-// Four neighbouring whole numbers of shared memory of the cluster, or four that are 32 apart, where `on`; else zeros.  (A predicate,
-// not a branch: the loads of several tokens stay together.)
-__device__ __forceinline__ int4 cluster_int4(bool on, uint32_t at)
+// Adds `bytes` of whole numbers of this CTA's shared memory to those at `to` in another CTA of the cluster, whose barrier `bar` counts them.
+__device__ __forceinline__ void add_to_cta(uint32_t to, uint32_t from, uint32_t bytes, uint32_t bar)
 {
-    int4 v;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t@p ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];\n\t}"
-                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "r"(at), "r"((uint32_t)on) : "memory");
-    return v;
-}
-__device__ __forceinline__ int4 cluster_ints(bool on, uint32_t at)
-{
-    int4 v;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t@p ld.shared::cluster.s32 %0, [%4];\n\t"
-                 "@p ld.shared::cluster.s32 %1, [%4+128];\n\t@p ld.shared::cluster.s32 %2, [%4+256];\n\t@p ld.shared::cluster.s32 %3, [%4+384];\n\t}"
-                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "r"(at), "r"((uint32_t)on) : "memory");
-    return v;
+    asm volatile("cp.reduce.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes.add.s32 [%0], [%1], %2, [%3];"
+                 ::"r"(to), "r"(from), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void l2_prefetch_2d(const CUtensorMap *map, int x, int y)
 {
@@ -331,7 +321,8 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
             mbar_init(&ctl->full[lane], 1);
             mbar_init(&ctl->empty[lane], 1);
         } else if (lane == 8) mbar_init(&ctl->accum[0], 1);
-        else if (lane == 9) ctl->abort_flag = 0;
+        else if (lane == 9) mbar_init(&ctl->added, 1);
+        else if (lane == 10) ctl->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc(&ctl->tmem, columns);
@@ -384,74 +375,106 @@ __global__ void __launch_bounds__(32 * I8_SPLIT_WARPS, TWO ? 2 : 1) i8_split_ker
             if (ok) umma_commit(&ctl->accum[0]);
         }
     } else {
-        const int quad = warp & 3;
-        for (int j = threadIdx.x - 64; j < used; j += 128) ctl->token[j] = __ldg(p.x_scale + b0 + j);
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        for (int j = threadIdx.x - 64; j < used; j += 256) ctl->token[j] = __ldg(p.x_scale + b0 + j);
+        asm volatile("bar.sync 1, 256;" ::: "memory");           // these eight warps
         bool ok = mbar_wait(&ctl->accum[0], 0, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
         __syncwarp();
-        if (ok && *abort_flag == 0) {
+        ok = ok && *abort_flag == 0;
+        if (ok) {
             tc_fence_after();
-            // All products are through, and so are the copies that they waited for: the sums, [token][channel], take the stages' place.
-            int *to = reinterpret_cast<int *>(smem) + quad * 32 + lane;
-            for (int c = 0; c < p.tokens; c += 32) {     // (the last 16 may be beyond the tile, not beyond what was allocated)
+            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16);
+            const int own = o0 + quad * 32 + lane;
+            const float scale = own < p.rows ? __ldg(p.w_scale + own) : 0.f;
+            // Alone, straight from tensor memory: the warp has 32 neighbouring channels of a token.  Else (all products are through,
+            // and so are the copies that they waited for) the sums, [token][channel], take the stages' place.
+            int *part = reinterpret_cast<int *>(smem) + quad * 32 + lane;
+            for (int c = half * 32; c < used; c += 64) {
                 int v[32];
-                tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+                tmem_ld32(from + c, v);
                 tmem_ld_wait();
+                if (p.split > 1) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) if (c + j < p.tokens) to[(c + j) * 128] = v[j];
+                    for (int j = 0; j < 16; ++j) part[(c + j) * 128] = v[j];
+                    if (c + 16 < p.tokens) {         // (else they are beyond the tile, not beyond what was allocated of tensor memory)
+#pragma unroll
+                        for (int j = 16; j < 32; ++j) part[(c + j) * 128] = v[j];
+                    }
+                } else if (own < p.rows) {
+                    char *to = static_cast<char *>(p.y) + ((long long)(b0 + c) * p.rows + own) * (f32 ? 4 : 2);
+                    const long long pitch = (long long)p.rows * (f32 ? 4 : 2);
+                    const int left = used - c;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 token = *reinterpret_cast<const float4 *>(&ctl->token[c + j]);
+                        const float y[4] = {((float)v[j] * token.x) * scale, ((float)v[j + 1] * token.y) * scale, ((float)v[j + 2] * token.z) * scale, ((float)v[j + 3] * token.w) * scale};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (j + i < left) {
+                                if (f32) *reinterpret_cast<float *>(to) = y[i];
+                                else *reinterpret_cast<uint16_t *>(to) = (uint16_t)pack_bf16(y[i], 0.f);
+                            }
+                            to += pitch;
+                        }
+                    }
+                }
             }
+            if (p.split > 1) fence_async_proxy();    // the sums are read by bulk copies
         }
         tc_fence_before();
     }
     let_next();
     __syncwarp();
-    if (p.split > 1) cluster_sync_all();
-    else __syncthreads();
-    if (*abort_flag == 0) {
-        const int j1 = used * (rank + 1) / p.split;
-        const uint32_t mine = smem_u32(smem) + lane * (four ? 16 : 4);
-        constexpr int T = 4;                     // tokens whose loads are under way together: they take most of a microsecond each
-        for (int j = used * rank / p.split + warp; j < j1; j += I8_SPLIT_WARPS * T) {
-            float token[T];
-            int4 sum[T];
-#pragma unroll
-            for (int t = 0; t < T; ++t) {
-                token[t] = ctl->token[min(j + t * I8_SPLIT_WARPS, j1 - 1)];
-                sum[t] = make_int4(0, 0, 0, 0);
+    if (p.split > 1) {
+        // Every CTA takes an equal part of the tokens: the others add theirs to its sums, and it scales and stores them.
+        const int j0 = used * rank / p.split, j1 = used * (rank + 1) / p.split;
+        cluster_sync_all();
+        if (*abort_flag == 0 && threadIdx.x == 0) {
+            mbar_arrive_expect_tx(&ctl->added, (uint32_t)((p.split - 1) * (j1 - j0) * 512));
+            for (int r = 1; r < p.split; ++r) {
+                const int to = (rank + r) % p.split, first = used * to / p.split, bytes = (used * (to + 1) / p.split - first) * 512;
+                const uint32_t at = smem_u32(smem) + first * 512;
+                if (bytes) add_to_cta(in_cta(at, to), at, bytes, in_cta(smem_u32(&ctl->added), to));
             }
-#pragma unroll 4
-            for (int r = 0; r < p.split; ++r) {
-                const uint32_t from = p.split > 1 ? in_cta(mine, r) : mine;      // (a CTA's own addresses are addresses of the cluster, too)
+        }
+        const bool ok = *abort_flag == 0 && mbar_wait(&ctl->added, 0, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
+        if (!ok) let_copies_land();
+        __syncwarp();
+        if (ok && *abort_flag == 0) {
+            constexpr int T = 4;                     // tokens of a warp at a time
+            const uint8_t *mine = smem + lane * (four ? 16 : 4);
+            for (int j = j0 + warp; j < j1; j += I8_SPLIT_WARPS * T) {
+                int4 sum[T];
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
-                    const bool on = j + t * I8_SPLIT_WARPS < j1;
-                    const uint32_t at = from + (j + t * I8_SPLIT_WARPS) * 512;
-                    const int4 v = four ? cluster_int4(on, at) : cluster_ints(on, at);
-                    sum[t].x += v.x; sum[t].y += v.y; sum[t].z += v.z; sum[t].w += v.w;
+                    const int *at = reinterpret_cast<const int *>(mine + min(j + t * I8_SPLIT_WARPS, j1 - 1) * 512);
+                    sum[t] = four ? *reinterpret_cast<const int4 *>(at) : make_int4(at[0], at[32], at[64], at[96]);
                 }
-            }
 #pragma unroll
-            for (int t = 0; t < T; ++t) {
-                const int own = j + t * I8_SPLIT_WARPS;
-                if (own >= j1) break;
-                const float y[4] = {((float)sum[t].x * token[t]) * channel[0], ((float)sum[t].y * token[t]) * channel[1], ((float)sum[t].z * token[t]) * channel[2],
-                                    ((float)sum[t].w * token[t]) * channel[3]};
-                const long long to = (long long)(b0 + own) * p.rows + o;
-                if (four && o < p.rows) {        // rows is a multiple of four: all of them are there
-                    if (f32) *reinterpret_cast<float4 *>(static_cast<float *>(p.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
-                    else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.y) + to) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-                } else if (!four) {
+                for (int t = 0; t < T; ++t) {
+                    const int own = j + t * I8_SPLIT_WARPS;
+                    if (own >= j1) break;
+                    const float token = ctl->token[own];
+                    const float y[4] = {((float)sum[t].x * token) * channel[0], ((float)sum[t].y * token) * channel[1], ((float)sum[t].z * token) * channel[2],
+                                        ((float)sum[t].w * token) * channel[3]};
+                    const long long to = (long long)(b0 + own) * p.rows + o;
+                    if (four && o < p.rows) {        // rows is a multiple of four: all of them are there
+                        if (f32) *reinterpret_cast<float4 *>(static_cast<float *>(p.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
+                        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.y) + to) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+                    } else if (!four) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (o + 32 * i >= p.rows) continue;
-                        if (f32) static_cast<float *>(p.y)[to + 32 * i] = y[i];
-                        else static_cast<uint16_t *>(p.y)[to + 32 * i] = (uint16_t)pack_bf16(y[i], 0.f);
+                        for (int i = 0; i < 4; ++i) {
+                            if (o + 32 * i >= p.rows) continue;
+                            if (f32) static_cast<float *>(p.y)[to + 32 * i] = y[i];
+                            else static_cast<uint16_t *>(p.y)[to + 32 * i] = (uint16_t)pack_bf16(y[i], 0.f);
+                        }
                     }
                 }
             }
         }
-    }
+    } else __syncthreads();
     __syncwarp();
-    if (p.split > 1) cluster_sync_all();         // a CTA stays while others read its sums
+    if (p.split > 1) cluster_sync_all();         // a CTA stays while its sums are under way to others
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, columns);

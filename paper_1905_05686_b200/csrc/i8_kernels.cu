@@ -131,12 +131,10 @@ __device__ __forceinline__ void mma_i8(int (&d)[4], uint32_t a0, uint32_t a1, ui
 // A block has 16 rows of weights and 8 * NT tokens; its warps take 64 columns each in turn and add their sums up at the end.
 // The column is a summation index: lane (g, t) takes 16 neighbouring bytes of rows g and g + 8, and of token g, as the four
 // words that two steps of 32 columns want, both operands in the same order.
-constexpr int I8_WARPS = 8;
-template <int NT>
+template <int NT, int I8_WARPS, int U>
 __global__ void __launch_bounds__(32 * I8_WARPS) i8_few_kernel(I8Product p)
 {
     begin();
-    constexpr int U = 4;       // steps of a warp whose loads are under way together
     __shared__ int sums[I8_WARPS][8 * NT][16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int o0 = blockIdx.x * 16;
@@ -222,6 +220,46 @@ lrbi_status tokens_act(const TokenArgs &a, int act, cudaStream_t s)
     return tokens_rows<SRC, ACT_NONE>(a, s);
 }
 
+template <int NT, int W, int U>
+lrbi_status few_launch(const I8Product &p, cudaStream_t s)
+{
+    return launch_kernel(i8_few_kernel<NT, W, U>, dim3((p.rows + 15) / 16), dim3(32 * W), 0, s, 1, p);
+}
+
+// One token, us: 4096 x 9216 with 8 warps 8.9, 16 11.1; 16384 x 4096 12.6 and 18.1; layers of fewer tiles than SMs: 64 x 16384 5.6 and
+// 4.3, 1000 x 4096 2.9 and 2.5.  Short rows, two steps at a time: 16384 x 500 3.9, four 4.9.
+lrbi_status launch_few(const I8Product &p, cudaStream_t s)
+{
+    if (p.batch > 8) return few_launch<2, 16, 4>(p, s);
+    if (p.rows <= 16 * NORM_SMS) return few_launch<1, 16, 4>(p, s);
+    return p.cols <= 1024 ? few_launch<1, 8, 2>(p, s) : few_launch<1, 8, 4>(p, s);
+}
+
+// Times in microseconds, as fitted to those measured (64 .. 16384 rows, 500 .. 16384 columns, 16 .. 4096 tokens).
+struct Estimate {
+    int rows, batch, blocks;      // blocks: of 128 columns
+    double memory;                // what the arrays take
+
+    explicit Estimate(const I8Product &p) : rows(p.rows), batch(p.batch), blocks((p.cols + 127) / 128)
+    {
+        memory = ((double)rows * p.cols + (double)batch * p.cols + (p.y_dtype == LRBI_Y_F32 ? 4. : 2.) * batch * rows) / 5.7e6;
+    }
+    static double rounds(long long units, int at_once) { return (double)((units + at_once - 1) / at_once); }
+    // 9 to 16 tokens without tensor memory
+    double few(int cols) const { return 1.5 + 0.0006 * cols + rows * (0.0004 + 1e-7 * cols); }
+    // Pairs: a launch and the last tile's stores; 128 columns of a tile.
+    double many() const { return 6. + std::max(rounds((long long)((batch + 255) / 256) * ((rows + 255) / 256), NORM_SMS / 2) * blocks * 0.28, memory); }
+    // Clusters: a launch, the sums and stores of a tile's tokens; 128 columns of a CTA one after the other, or what all of them read of L2.
+    double split(int tokens, int split) const
+    {
+        const long long ctas = (long long)((batch + tokens - 1) / tokens) * ((rows + 127) / 128) * split;
+        const double turns = rounds(ctas, tokens <= 128 ? 2 * NORM_SMS : NORM_SMS) * (split == 8 && tokens > 128 ? 2. : 1.);
+        const double tile = split == 1 ? 0.3 + 0.013 * tokens : 1. + 0.35 * (split > 2) + 0.35 * (split > 4) + 0.0185 * tokens;
+        const double inside = std::max(turns * ((blocks + split - 1) / split) * (tokens <= 192 ? 0.216 : 0.284), (double)ctas * blocks / split * (16384 + 128 * tokens) / 12e6);
+        return 2. + turns * tile + std::max(inside, memory);
+    }
+};
+
 }  // namespace
 
 lrbi_status launch_i8_tokens(const void *x, int dtype, long long stride, int rows, int cols, int act, int8_t *q, float *scale, cudaStream_t s)
@@ -239,33 +277,19 @@ lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *
     return LRBI_OK;
 }
 
-lrbi_status launch_i8_few(const I8Product &p, cudaStream_t s)
-{
-    const int tiles = (p.rows + 15) / 16;
-    if (p.batch <= 8) return launch_kernel(i8_few_kernel<1>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
-    return launch_kernel(i8_few_kernel<2>, dim3(tiles), dim3(32 * I8_WARPS), 0, s, 1, p);
-}
-
-// Which kernel, by an estimate of the times of all, in microseconds, as fitted to those measured: what a launch costs; for every 128
-// columns that a CTA (or pair) takes in turn, more the more tokens a tile has; the sums and stores of a tile; neither less than
-// memory takes.
 lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
 {
-    if (p.batch <= 8) return launch_i8_few(p, s);
-    const int blocks = (p.cols + 127) / 128;
-    const double memory = ((double)p.rows * p.cols + (double)p.batch * p.cols + (p.y_dtype == LRBI_Y_F32 ? 4. : 2.) * p.batch * p.rows) / 5.2e6;
-    const long long pairs = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
-    double best = 4.5 + std::max((double)((pairs + NORM_SMS / 2 - 1) / (NORM_SMS / 2)) * blocks * 0.275, memory);
-    int tokens = 0, split = 0;      // none: the kernel for many tokens
-    for (int n : {16, 32, 64, 128, 256})
-        for (int k = 1; k <= 8 && k <= blocks; k *= 2) {
+    if (p.batch <= 8) return launch_few(p, s);
+    const Estimate e(p);
+    double best = e.many();
+    int tokens = 0, split = 0;
+    for (int n : {16, 32, 64, 128, 192, 256})
+        for (int k = 1; k <= 8 && k <= e.blocks; k *= 2) {
             const int each = std::min(n, (p.batch + 15) / 16 * 16);
-            const long long ctas = (long long)((p.batch + each - 1) / each) * ((p.rows + 127) / 128) * k;
-            const double rounds = (double)((ctas + NORM_SMS - 1) / NORM_SMS);
-            const double t = 3.3 + std::max(rounds * (((blocks + k - 1) / k) * (0.2 + 0.0013 * each) + 0.6 + 0.0135 * each + (k == 8 ? 1. : 0.)), memory);
+            const double t = e.split(each, k);
             if (t < best) { best = t; tokens = each; split = k; }
         }
-    if (p.batch <= 16 && 1.5 + 0.4 * blocks / 8. + memory * 2. < best) return launch_i8_few(p, s);
+    if (p.batch <= 16 && e.few(p.cols) < best) return launch_few(p, s);
     return split ? launch_i8_split(p, tokens, split, s) : launch_i8_long(p, s);
 }
 
