@@ -89,26 +89,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, int (&v)[32])
                  : "r"(at) : "memory");
 }
 
-// Stores `bytes` (2 to 16, whole values) of a 16-byte piece in accesses of `vector` bytes at most.
-__device__ __forceinline__ void store_piece(uint8_t *to, const uint4 &v, int bytes, int vector)
-{
-    if (bytes == 16 && vector == 16) *reinterpret_cast<uint4 *>(to) = v;
-    else if (bytes == 16 && vector == 8) {
-        *reinterpret_cast<uint2 *>(to) = make_uint2(v.x, v.y);
-        *reinterpret_cast<uint2 *>(to + 8) = make_uint2(v.z, v.w);
-    } else {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (4 * i + 4 <= bytes && vector >= 4) *reinterpret_cast<uint32_t *>(to + 4 * i) = w[i];
-            else {
-                if (4 * i < bytes) *reinterpret_cast<uint16_t *>(to + 4 * i) = (uint16_t)w[i];
-                if (4 * i + 2 < bytes) *reinterpret_cast<uint16_t *>(to + 4 * i + 2) = (uint16_t)(w[i] >> 16);
-            }
-        }
-    }
-}
-
 // Copies that are under way must land before shared memory is given up: about 2 ms, far beyond any of them.
 __device__ __forceinline__ void let_copies_land()
 {
@@ -269,13 +249,28 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
                             own[i ^ swap] = make_uint4(pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]), pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7]));
                     }
                     __syncwarp();
-                    const int piece = lane & 3, o = o0 + c + h * 16 + piece * (16 / size), some = min(16 / size, p.rows - o);
+                    const int at = o0 + c + h * 16;      // first channel of the 64 bytes
+                    char *const to = static_cast<char *>(p.y) + ((long long)b0 * p.rows + at) * size;
+                    const long long pitch = (long long)p.rows * size;
+                    const int width = min(64, (p.rows - at) * size);      // bytes that are there
+                    if (p.vector == 16) {                // eight rows at a time
+                        const int piece = lane & 3;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = i * 8 + (lane >> 2);
-                        if (r < left && some > 0)
-                            store_piece(static_cast<uint8_t *>(p.y) + ((long long)(b0 + r) * p.rows + o) * size, *reinterpret_cast<const uint4 *>(stage + r * 64 + ((piece ^ (r >> 1 & 3)) << 4)),
-                                        some * size, p.vector);
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = i * 8 + (lane >> 2);
+                            if (r < left && piece * 16 < width) *reinterpret_cast<uint4 *>(to + r * pitch + piece * 16) = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((piece ^ (r >> 1 & 3)) << 4));
+                        }
+                    } else if (p.vector >= 4) {          // two rows at a time, so that a warp still writes whole stretches
+                        const int word = lane & 15;
+#pragma unroll 8
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = i * 2 + (lane >> 4);
+                            if (r < left && word * 4 < width) *reinterpret_cast<uint32_t *>(to + r * pitch + word * 4) = *reinterpret_cast<const uint32_t *>(stage + r * 64 + (((word >> 2) ^ (r >> 1 & 3)) << 4) + (word & 3) * 4);
+                        }
+                    } else {
+#pragma unroll 8
+                        for (int r = 0; r < 32; ++r)
+                            if (r < left && lane * 2 < width) *reinterpret_cast<uint16_t *>(to + r * pitch + lane * 2) = *reinterpret_cast<const uint16_t *>(stage + r * 64 + (((lane >> 3) ^ (r >> 1 & 3)) << 4) + (lane & 7) * 2);
                     }
                     __syncwarp();
                 }
