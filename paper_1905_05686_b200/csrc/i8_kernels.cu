@@ -134,11 +134,19 @@ __device__ __forceinline__ void mma_i8(int (&d)[4], uint32_t a0, uint32_t a1, ui
 template <int NT, int I8_WARPS, int U>
 __global__ void __launch_bounds__(32 * I8_WARPS) i8_few_kernel(I8Product p)
 {
-    begin();
     __shared__ int sums[I8_WARPS][8 * NT][16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int o0 = blockIdx.x * 16;
     const int8_t *w0 = p.w + (long long)min(o0 + g, p.rows - 1) * p.pitch, *w1 = p.w + (long long)min(o0 + g + 8, p.rows - 1) * p.pitch;
+    // A hint that needs no order: the first weights come to L2 while the kernel before this one (the tokens') ends.  With the tokens,
+    // 4096 x 9216, one of them: 10.3 us, without 11.3; all of the weights at once: 15.
+    if (t < 2)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = (u * I8_WARPS + warp) * 64;
+            if (c < p.pitch) asm volatile("prefetch.global.L2 [%0];" ::"l"((t ? w1 : w0) + c));
+        }
+    begin();
     const int8_t *x[NT];
     bool on[NT];
 #pragma unroll

@@ -212,24 +212,28 @@ struct Team {
 // How rows are dealt out: spans of a warp, threads of a row, rows of a block, blocks that share a row, groups of such blocks.
 struct JoinCut {
     int each, threads, teams, split, groups;
+    bool direct;       // the vectors stay in memory: a row fits a block, they beside it do not
     size_t smem;
     int width() const { return threads / 32 * each * SPAN; }
 };
 
 // row: bytes of a column of a row in shared memory; vectors: of the vectors' columns; meet: of the places to meet, an entry.
-inline JoinCut join_cut(int rows, int cols, int most_each, int row, int vectors, int meet)
+// may_direct: rows of a block may do without the vectors in shared memory (2048 x 16384, root mean square, forward: 118 us as two
+// blocks that share a row).
+inline JoinCut join_cut(int rows, int cols, int most_each, int row, int vectors, int meet, bool may_direct)
 {
     JoinCut k = {};
     const int spans = (cols + SPAN - 1) / SPAN;
     // A warp that has more of a row has fewer others to wait for, and more rows are under way side by side; few rows are better
     // spread over many warps.
-    k.each = spans > 1 && rows > 2 * NORM_SMS ? most_each : 1;
+    k.each = spans > 1 && (rows > 2 * NORM_SMS || spans > JOIN_WARPS) ? most_each : 1;
     for (k.split = 1;; k.split *= 2) {
         const int warps = ((spans + k.split - 1) / k.split + k.each - 1) / k.each;
         k.threads = 32 * warps;
         auto need = [&](int teams) {
-            return (size_t)vectors * k.width() + (size_t)teams * ((size_t)2 * (row * k.width() + warps * 64) + (size_t)2 * warps * k.split * meet);
+            return (size_t)(k.direct ? 0 : vectors) * k.width() + (size_t)teams * ((size_t)2 * (row * k.width() + warps * 64) + (size_t)2 * warps * k.split * meet);
         };
+        k.direct = may_direct && k.split == 1 && warps <= JOIN_WARPS && need(1) > JOIN_SHARED;
         if (k.split < JOIN_SPLIT && (warps > JOIN_WARPS || need(1) > JOIN_SHARED)) continue;
         k.teams = 1;
         while (k.split == 1 && (k.teams + 1) * k.threads <= JOIN_THREADS && need(k.teams + 1) <= JOIN_SHARED) ++k.teams;
@@ -240,8 +244,8 @@ inline JoinCut join_cut(int rows, int cols, int most_each, int row, int vectors,
     return k;
 }
 inline int type_bytes(int dtype) { return dtype == LRBI_Y_F32 ? 4 : 2; }
-inline JoinCut forward_cut(const JoinArgs &a) { return join_cut(a.rows, a.cols, 4, type_bytes(a.x_dtype) + type_bytes(a.f_dtype), 16, 8); }
-inline JoinCut backward_cut(int rows, int cols, int x_dtype, int f_dtype) { return join_cut(rows, cols, 2, 2 * (type_bytes(x_dtype) + type_bytes(f_dtype)), 8, 32); }
+inline JoinCut forward_cut(const JoinArgs &a) { return join_cut(a.rows, a.cols, 4, type_bytes(a.x_dtype) + type_bytes(a.f_dtype), 16, 8, true); }
+inline JoinCut backward_cut(int rows, int cols, int x_dtype, int f_dtype) { return join_cut(rows, cols, 2, 2 * (type_bytes(x_dtype) + type_bytes(f_dtype)), 8, 32, false); }
 
 template <class Kernel>
 lrbi_status join_launch(Kernel kernel, const JoinCut &k, cudaStream_t s, const Join &j)

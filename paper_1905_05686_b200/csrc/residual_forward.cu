@@ -73,8 +73,8 @@ __device__ __forceinline__ void row_statistics(const F2 (&v)[K][PAIRS], int left
 }
 
 // blockDim = (threads of a row, rows of a block); clusters of `split` blocks share a row.  Shared memory: the vectors, the places to
-// meet, and two rows for each team, one of them on its way.
-template <int X, int F, bool STRIDED, int K, bool RMS>
+// meet, and two rows for each team, one of them on its way.  DIRECT: the vectors are read where they are, by every row.
+template <int X, int F, bool STRIDED, int K, bool RMS, bool DIRECT>
 __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
 {
     const JoinArgs &a = j.a;
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
     Team t(j.split);
     const int block0 = t.rank * j.width, w0 = t.warp * K * SPAN, c0 = block0 + w0, left = a.cols - c0;      // first columns of the block, of the warp
     float *vectors = shared;                                 // gate * post_gamma, gate * post_beta, gamma, beta
-    float *part = vectors + 4 * j.width;
+    float *part = vectors + (DIRECT ? 0 : 4 * j.width);
     char *ring = reinterpret_cast<char *>(part + blockDim.y * 2 * t.entries() * 2) + (threadIdx.y * t.warps + t.warp) * 2 * SLOT;
     begin();
     const XS x(a.x, a.x_stride, c0, a.cols);
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
     long long row = (long long)(blockIdx.x / j.split) * blockDim.y + threadIdx.y;
     if (row < a.rows) { f.template ask<false>(ring, row, t.lane); x.template ask<false>(ring + FS::SLOT, row, t.lane); }
     copies_asked();
-    for (int c = (threadIdx.y * blockDim.x + threadIdx.x) * 4; c < j.width; c += blockDim.x * blockDim.y * 4) {
+    for (int c = (threadIdx.y * blockDim.x + threadIdx.x) * 4; !DIRECT && c < j.width; c += blockDim.x * blockDim.y * 4) {
         float4 *to = reinterpret_cast<float4 *>(vectors + vector_place<STRIDED>(c));
         const int from = block0 + c, pitch = j.width / 4;
         const float4 gate = four_of(a.gate, a.param_dtype, j.whole, from, a.cols, 1.f), pg = four_of(a.post_gamma, a.param_dtype, j.whole, from, a.cols, 1.f);
@@ -111,6 +111,21 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
     const int c = lane_column<STRIDED>(c0, t.lane);
     char *const out = static_cast<char *>(a.out) + (long long)c * XSIZE, *const u = static_cast<char *>(a.u) + (long long)c * FSIZE;
     const float *own = vectors + w0;
+    const Params p = {nullptr, nullptr, a.param_dtype, j.whole};
+    // Chunk k of a vector: gate * post_gamma, gate * post_beta, gamma, beta.
+    auto vector = [&](int which, int k, F2 (&w)[PAIRS]) {
+        if constexpr (!DIRECT) get_vector<STRIDED>(own + which * j.width, k, t.lane, w);
+        else {
+            const void *const all[4] = {a.post_gamma, a.post_beta, a.gamma, a.beta};
+            load_param<STRIDED>(all[which], p, c + k * SPAN, a.cols, all[which] ? 0.f : 1.f, w);
+            if (which < 2 && a.gate) {
+                F2 gate[PAIRS];
+                load_param<STRIDED>(a.gate, p, c + k * SPAN, a.cols, 0.f, gate);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) w[i] = w[i] * gate[i];
+            }
+        }
+    };
     auto rows = [&](auto full) {
     constexpr bool FULL = decltype(full)::value;         // the warp has all of its columns
     for (int stage = 0; row < a.rows; row += step, stage ^= 1) {
@@ -134,12 +149,12 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (!FULL && left <= k * SPAN) break;
-            get_vector<STRIDED>(own, k, t.lane, w);
+            vector(0, k, w);
             x.template get<FULL>(slot + FS::SLOT, row, k, left - k * SPAN, t.lane, b);
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) v[k][i] = fma2(b[i], f2(a.residual_scale), fma2(v[k][i], scale, shift) * w[i]);
             if (a.post_beta) {
-                get_vector<STRIDED>(own + j.width, k, t.lane, b);
+                vector(1, k, b);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[k][i] = v[k][i] + b[i];
             }
@@ -167,9 +182,9 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (!FULL && left <= k * SPAN) break;
-            get_vector<STRIDED>(own + 2 * j.width, k, t.lane, w);
+            vector(2, k, w);
             if (a.beta) {
-                get_vector<STRIDED>(own + 3 * j.width, k, t.lane, b);
+                vector(3, k, b);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[k][i] = fma2(fma2(v[k][i], scale, shift), w[i], b[i]);
             } else {
@@ -216,7 +231,8 @@ namespace {
 template <int X, int F, bool STRIDED, bool RMS>
 lrbi_status forward_rows(const JoinCut &k, cudaStream_t s, const Join &j)
 {
-    return k.each == 1 ? join_launch(join_forward_kernel<X, F, STRIDED, 1, RMS>, k, s, j) : join_launch(join_forward_kernel<X, F, STRIDED, 4, RMS>, k, s, j);
+    if (k.each == 1) return join_launch(join_forward_kernel<X, F, STRIDED, 1, RMS, false>, k, s, j);
+    return k.direct ? join_launch(join_forward_kernel<X, F, STRIDED, 4, RMS, true>, k, s, j) : join_launch(join_forward_kernel<X, F, STRIDED, 4, RMS, false>, k, s, j);
 }
 template <int X, int F>
 lrbi_status forward_types(const JoinCut &k, bool vector, cudaStream_t s, const Join &j)
