@@ -674,9 +674,9 @@ class I8Rows:
             raise ValueError("q must be [rows, %d] and scale [rows] on one CUDA device" % pitch)
         self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
 
-    @classmethod
-    def _of(cls, q, scale, rows, cols):
-        rows8 = object.__new__(cls)
+    @staticmethod
+    def _of(q, scale, rows, cols):
+        rows8 = object.__new__(I8Rows)
         rows8.q, rows8.scale, rows8.rows, rows8.cols = q, scale, rows, cols
         return rows8
 
@@ -716,8 +716,9 @@ def lrbi_i8_quantize(layer, W: torch.Tensor, ip: torch.Tensor | None = None, iz:
 
 def lrbi_i8_tokens(x: torch.Tensor, act: str | None = None, stream=None) -> I8Tokens:
     """The rows of x [rows, cols] (bf16 or fp32), or of act(x), in 8 bits."""
-    q, scale = _native().i8_tokens(x, -1 if act is None else _act(act), stream)
-    return I8Tokens._of(q, scale, *x.shape)
+    rows8 = object.__new__(I8Rows)
+    rows8.q, rows8.scale, rows8.rows, rows8.cols = _native().i8_tokens(x, -1 if act is None else _act(act), stream)
+    return rows8
 
 
 def lrbi_i8_gemm(weights: I8Weights, tokens: I8Tokens, y_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
@@ -750,7 +751,7 @@ def lrbi_residual_norm(x: torch.Tensor, f: torch.Tensor, gamma: torch.Tensor | N
     Returns (out, u, stats): out in x's type, u in f's (None without gamma), stats float32 [4, rows] for the backward pass.  With
     tokens=True u comes as I8Tokens for the next layer's 8-bit product, and stats is None."""
     out, u, stats, q, scale = _native().residual_norm(x, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, eps, _kind(kind), tokens, stream)
-    return out, (I8Tokens._of(q, scale, *x.shape) if tokens else u), stats
+    return out, (I8Rows._of(q, scale, *x.shape) if tokens else u), stats
 
 
 def lrbi_residual_norm_backward(du: torch.Tensor | None, dout: torch.Tensor | None, out: torch.Tensor | None, f: torch.Tensor,

@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
             if (t.entry() == 0 && t.lane == 0) a.q_scale[row] = s.scale();
             const int pitch = (a.cols + 15) / 16 * 16;
 #pragma unroll
-            for (int k = 0; k < K; ++k) store_i8<STRIDED>(a.q + row * pitch + c + k * SPAN, pitch - c - k * SPAN, v[k], s.factor, s.fine);
+            for (int k = 0; k < K; ++k) store_i8<STRIDED>(a.q + row * pitch + c + k * SPAN, pitch - c - k * SPAN, v[k], s.factor, s.fine, FULL);
         }
     }
     };

@@ -394,9 +394,9 @@ struct TokenScale {
 };
 
 // The bytes of a lane's chunk as rint(v * factor), at `to`, the place of its first column; `left` bytes are there from that one
-// on.  (Adding 1.5 * 2^23 as in Keep::bytes.)  fine: false for a row that is kept as zeros.
+// on (whole: strided, the warp's whole span is there).  (Adding 1.5 * 2^23 as in Keep::bytes.)  fine: false for a row that is kept as zeros.
 template <bool STRIDED>
-__device__ __forceinline__ void store_i8(int8_t *to, int left, const F2 (&v)[PAIRS], float factor, bool fine)
+__device__ __forceinline__ void store_i8(int8_t *to, int left, const F2 (&v)[PAIRS], float factor, bool fine, bool whole = false)
 {
     uint32_t b[CHUNK];
 #pragma unroll
@@ -407,8 +407,13 @@ __device__ __forceinline__ void store_i8(int8_t *to, int left, const F2 (&v)[PAI
         b[2 * i + 1] = fine ? __float_as_uint(__fadd_rn(hi, 12582912.f)) : 0;
     }
     if constexpr (STRIDED) {
+        if (whole) {
 #pragma unroll
-        for (int e = 0; e < CHUNK; ++e) if (32 * e < left) to[32 * e] = (int8_t)b[e];
+            for (int e = 0; e < CHUNK; ++e) to[32 * e] = (int8_t)b[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < CHUNK; ++e) if (32 * e < left) to[32 * e] = (int8_t)b[e];
+        }
     } else if (left > 0) {
         *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
                                                     __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));

@@ -413,7 +413,7 @@ std::pair<at::Tensor, at::Tensor> make_rows8(const Call &c, int rows, int cols)
     return c.make_two({rows, lrbi_i8_pitch(cols)}, at::kChar, {rows}, at::kFloat);
 }
 
-// i8_tokens(x, act, stream) -> (q, scale)
+// i8_tokens(x, act, stream) -> (q, scale, rows, cols)
 PyObject *i8_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     CALL("i8_tokens", 3) {
@@ -423,7 +423,12 @@ PyObject *i8_tokens(PyObject *, PyObject *const *a, Py_ssize_t n)
         auto [q, scale] = make_rows8(c, x.rows, x.cols);
         check(lrbi_i8_tokens(x.data, x.dtype, x.stride, x.rows, x.cols, act, static_cast<int8_t *>(q.data_ptr()), static_cast<float *>(scale.data_ptr()), c.handle()),
               "lrbi_i8_tokens");
-        return tuple(std::move(q), std::move(scale));
+        PyObject *r = PyTuple_New(4), *items[] = {THPVariable_Wrap(std::move(q)), THPVariable_Wrap(std::move(scale)), PyLong_FromLong(x.rows), PyLong_FromLong(x.cols)};
+        for (int i = 0; i < 4; ++i) {
+            if (r) PyTuple_SET_ITEM(r, i, items[i]);
+            else Py_XDECREF(items[i]);
+        }
+        return r;
     });
 }
 
