@@ -431,7 +431,7 @@ LRBI_API lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, 
  *   q      device, int8 (-127 .. 127), [rows][lrbi_i8_pitch(cols)], 16-byte aligned; bytes past the last column are 0 (the calls
  *          that make q write them, the product relies on them)
  *   scale  device, fp32, [rows]
- * cols is 1 .. LRBI_I8_MAX_COLS, up to which no sum leaves 32 bits.
+ * cols is 1 .. LRBI_I8_MAX_COLS, up to which no sum leaves 32 bits; rows and batch up to 2^31 - 4096 (LRBI_ERR_UNSUPPORTED beyond).
  * lrbi_i8_quantize  W [rows][cols] bf16, contiguous -> q, scale of its rows.  ip, iz: the layer's packed factors, or both NULL
  *           (nothing is pruned; only rows and cols of the layout are looked at).  The range is that of the kept weights, pruned
  *           ones are exactly zero, and what the array holds at their places is not looked at.
@@ -471,7 +471,8 @@ LRBI_API lrbi_status lrbi_i8_gemm(const int8_t *w_q, const float *w_scale, int32
  *   out, stats    as the forward pass left them; out is not read where gamma is NULL
  *   dgamma .. dgate  device, fp32, [cols]; any may be NULL, and those of vectors that the call does not have are
  *   workspace     device, lrbi_residual_norm_backward_workspace(rows, cols) bytes, 16-byte aligned, scratch for the call
- * cols is 1 .. LRBI_MAX_RESIDUAL_COLS.  Matrices, alignment, rows of 0 and repeatability are as for lrbi_layer_norm.
+ * cols is 1 .. LRBI_MAX_RESIDUAL_COLS, rows up to 2^31 - 4096 (LRBI_ERR_UNSUPPORTED beyond).  Matrices, alignment, rows of 0 and
+ * repeatability are as for lrbi_layer_norm.
  */
 #define LRBI_MAX_RESIDUAL_COLS 32768
 enum { LRBI_NORM_LAYER = 0, LRBI_NORM_RMS = 1 };

@@ -57,6 +57,7 @@ bool matrix_ok(const void *p, int dtype, int64_t stride, int rows, int cols)
 bool floats_ok(const void *p, int n) { return n == 0 || (p && aligned(p, 4)); }
 bool copy_ok(const void *q, const void *scale, int rows) { return rows == 0 || (q && scale && aligned(q, 16) && aligned(scale, 4)); }
 bool i8_cols_ok(int cols) { return cols >= 1 && cols <= LRBI_I8_MAX_COLS; }
+constexpr int MOST_ROWS = INT32_MAX - 4095;      // numbers of rows are rounded up to tiles in 32 bits
 bool rows8_ok(const void *q, const void *scale) { return q && scale && aligned(q, 16) && aligned(scale, 4); }
 
 // What both passes between two blocks ask of a call.
@@ -240,6 +241,7 @@ lrbi_status lrbi_i8_quantize(const lrbi_layout *layout, const uint16_t *W, const
 {
     if (!layout || layout->rows < 1 || !i8_cols_ok(layout->cols) || !W || !aligned(W, 2) || !rows8_ok(q, scale) || !ip != !iz) return LRBI_ERR_INVALID_ARG;
     if (ip && (!aligned(ip, 4) || !aligned(iz, 4) || layout->tile_rows < 1 || layout->tile_cols < 1 || layout->rank < 1)) return LRBI_ERR_INVALID_ARG;
+    if (layout->rows > MOST_ROWS) return LRBI_ERR_UNSUPPORTED;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     lrbi_layout l = *layout;
     if (!ip) { l.tile_rows = l.rows; l.tile_cols = l.cols; l.rank = 1; }
@@ -250,6 +252,7 @@ lrbi_status lrbi_i8_tokens(const void *x, int32_t x_dtype, int64_t x_stride, int
 {
     if (rows < 0 || !i8_cols_ok(cols) || !matrix_ok(x, x_dtype, x_stride, rows, cols) || act < LRBI_ACT_NONE || act > LRBI_ACT_SILU) return LRBI_ERR_INVALID_ARG;
     if (rows > 0 && !rows8_ok(q, scale)) return LRBI_ERR_INVALID_ARG;
+    if (rows > MOST_ROWS) return LRBI_ERR_UNSUPPORTED;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     if (rows == 0) return LRBI_OK;
     return launch_i8_tokens(x, x_dtype, x_stride, rows, cols, act, q, scale, static_cast<cudaStream_t>(stream));
@@ -260,6 +263,7 @@ lrbi_status lrbi_i8_gemm(const int8_t *w_q, const float *w_scale, int32_t rows, 
 {
     if (rows < 1 || !i8_cols_ok(cols) || batch < 0 || !dtype_ok(y_dtype) || !rows8_ok(w_q, w_scale)) return LRBI_ERR_INVALID_ARG;
     if (batch > 0 && (!rows8_ok(x_q, x_scale) || !Y || !aligned(Y, y_dtype == LRBI_Y_F32 ? 4 : 2))) return LRBI_ERR_INVALID_ARG;
+    if (rows > MOST_ROWS || batch > MOST_ROWS) return LRBI_ERR_UNSUPPORTED;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     if (batch == 0) return LRBI_OK;
     return launch_i8_gemm({w_q, w_scale, x_q, x_scale, Y, y_dtype, rows, cols, i8_pitch(cols), batch}, static_cast<cudaStream_t>(stream));
@@ -274,6 +278,7 @@ lrbi_status lrbi_residual_norm(const lrbi_residual *how, const void *x, int64_t 
     if (!u_q != !u_scale || (u && u_q) || ((u || u_q) && !how->gamma)) return LRBI_ERR_INVALID_ARG;
     if (rows > 0 && how->gamma && !u && !u_q) return LRBI_ERR_INVALID_ARG;
     if ((u && !matrix_ok(u, how->f_dtype, u_stride, rows, cols)) || (u_q && !rows8_ok(u_q, u_scale)) || (stats && !aligned(stats, 4))) return LRBI_ERR_INVALID_ARG;
+    if (rows > MOST_ROWS) return LRBI_ERR_UNSUPPORTED;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     if (rows == 0) return LRBI_OK;
     JoinArgs n = join_args(how);
@@ -288,7 +293,7 @@ lrbi_status lrbi_residual_norm(const lrbi_residual *how, const void *x, int64_t 
 
 size_t lrbi_residual_norm_backward_workspace(int32_t rows, int32_t cols)
 {
-    return rows >= 0 && cols >= 1 && cols <= LRBI_MAX_RESIDUAL_COLS ? join_backward_workspace(rows, cols) : 0;
+    return rows >= 0 && rows <= MOST_ROWS && cols >= 1 && cols <= LRBI_MAX_RESIDUAL_COLS ? join_backward_workspace(rows, cols) : 0;
 }
 
 lrbi_status lrbi_residual_norm_backward(const lrbi_residual *how, const void *du, int64_t du_stride, const void *dout, int64_t dout_stride,
@@ -304,6 +309,7 @@ lrbi_status lrbi_residual_norm_backward(const lrbi_residual *how, const void *du
     if (rows > 0 && (how->gamma || how->post_gamma) && (!stats || !aligned(stats, 4))) return LRBI_ERR_INVALID_ARG;
     if ((dgamma && !how->gamma) || (dbeta && !how->beta) || (dpost_gamma && !how->post_gamma) || (dpost_beta && !how->post_beta) || (dgate && !how->gate)) return LRBI_ERR_INVALID_ARG;
     for (const float *v : {dgamma, dbeta, dpost_gamma, dpost_beta, dgate}) if (v && !aligned(v, 4)) return LRBI_ERR_INVALID_ARG;
+    if (rows > MOST_ROWS) return LRBI_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < join_backward_workspace(rows, cols)) return LRBI_ERR_INVALID_ARG;
     if (device_timeout_seen()) return LRBI_ERR_TIMEOUT;
     JoinArgs n = join_args(how);

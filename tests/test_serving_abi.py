@@ -26,10 +26,10 @@ def refused(lib, f, good, changes):
 def test_sizes(lib):
     L = lib.lib()
     assert [L.lrbi_i8_pitch(c) for c in (1, 16, 17, 801, 1 << 17, 0, -3, (1 << 17) + 1)] == [16, 16, 32, 816, 1 << 17, 0, 0, 0]
-    for rows, cols in ((0, 1), (1, 4096), (4096, 4096), (10 ** 6, 100), (7, 32768), (2 ** 31 - 1, 32768)):
+    for rows, cols in ((0, 1), (1, 4096), (4096, 4096), (10 ** 6, 100), (7, 32768), (2 ** 31 - 4096, 32768)):
         n = L.lrbi_residual_norm_backward_workspace(rows, cols)
         assert n >= 16 and n % 16 == 0
-    assert [L.lrbi_residual_norm_backward_workspace(*v) for v in ((-1, 4), (4, 0), (4, 32769))] == [0, 0, 0]
+    assert [L.lrbi_residual_norm_backward_workspace(*v) for v in ((-1, 4), (4, 0), (4, 32769), (2 ** 31 - 4095, 4))] == [0] * 4
 
 
 def test_i8_arguments(lib):
@@ -78,6 +78,17 @@ def test_residual_arguments(lib):
     for change, at in ((dict(beta=0), 15), (dict(post_gamma=0, post_beta=0), 16), (dict(post_beta=0), 17), (dict(gate=0), 18)):
         refused(lib, L.lrbi_residual_norm_backward, back, [(0, residual(lib, **change))])      # a gradient of what is not there
     refused(lib, L.lrbi_residual_norm_backward, back, [(0, residual(lib, gamma=0, beta=0))])    # du without gamma
+
+
+def test_too_many_rows(lib):
+    L, before, most = lib.lib(), lib.launch_count(), 2 ** 31 - 1
+    assert L.lrbi_i8_tokens(P, 0, 64, most, 64, -1, P, P, NULL) == lib.ERR_UNSUPPORTED
+    assert L.lrbi_i8_gemm(P, P, most, 96, P, P, 4, P, 0, NULL) == lib.ERR_UNSUPPORTED
+    assert L.lrbi_i8_gemm(P, P, 64, 96, P, P, most, P, 0, NULL) == lib.ERR_UNSUPPORTED
+    assert L.lrbi_i8_quantize(ctypes.byref(lib.Layout(most, 96, 16, 32, 4)), P, NULL, NULL, P, P, NULL) == lib.ERR_UNSUPPORTED
+    assert L.lrbi_residual_norm(residual(lib, rows=most), P, 64, P, 64, P, 64, P, 64, NULL, NULL, P, NULL) == lib.ERR_UNSUPPORTED
+    assert L.lrbi_residual_norm_backward(residual(lib, rows=most), P, 64, P, 64, P, 64, P, 64, P, P, 64, P, 64, P, P, P, P, P, P, 1 << 40, NULL) == lib.ERR_UNSUPPORTED
+    assert lib.launch_count() == before
 
 
 def test_python_refusals(lib):
