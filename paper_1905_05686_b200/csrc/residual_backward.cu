@@ -307,21 +307,22 @@ lrbi_status backward_types(const JoinCut &k, bool vector, cudaStream_t s, const 
 
 }  // namespace
 
-// Enough for any types.
+// Enough for any types and vectors.
 size_t join_backward_workspace(int rows, int cols)
 {
     size_t most = 16;
     for (int f : {LRBI_Y_BF16, LRBI_Y_F32})
-        for (int x : {f, (int)LRBI_Y_F32}) {
-            const JoinCut k = backward_cut(rows, cols, x, f);
-            most = std::max(most, (size_t)k.groups * 16 * k.width() * k.split);
-        }
+        for (int x : {f, (int)LRBI_Y_F32})
+            for (bool level : {false, true}) {
+                const JoinCut k = backward_cut(rows, cols, x, f, level);
+                most = std::max(most, (size_t)k.groups * 16 * k.width() * k.split);
+            }
     return most;
 }
 
 lrbi_status launch_join_backward(const JoinArgs &a, float *workspace, cudaStream_t s)
 {
-    const JoinCut k = backward_cut(a.rows, a.cols, a.x_dtype, a.f_dtype);
+    const JoinCut k = backward_cut(a.rows, a.cols, a.x_dtype, a.f_dtype, join_level(a));
     const bool sums = a.dgamma || a.dbeta || a.dpost_gamma || a.dpost_beta || a.dgate, vector = join_vector(a);
     const Join j = make_join(a, k, sums ? workspace : nullptr);
     if (a.rows > 0) {

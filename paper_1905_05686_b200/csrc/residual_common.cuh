@@ -217,16 +217,16 @@ struct JoinCut {
     int width() const { return threads / 32 * each * SPAN; }
 };
 
+// most_each: spans of a warp where there are more rows than `few`.  A warp that has more of a row has fewer others to wait for, and
+// more rows are under way side by side; few rows are better spread over many warps.
 // row: bytes of a column of a row in shared memory; vectors: of the vectors' columns; meet: of the places to meet, an entry.
-// may_direct: rows of a block may do without the vectors in shared memory (2048 x 16384, root mean square, forward: 118 us as two
-// blocks that share a row).
-inline JoinCut join_cut(int rows, int cols, int most_each, int row, int vectors, int meet, bool may_direct)
+// may_direct: rows of a block may do without the vectors in shared memory (2048 x 16384, root mean square, forward: 96 us; as two
+// blocks that share a row 118).
+inline JoinCut join_cut(int rows, int cols, int most_each, int few, int row, int vectors, int meet, bool may_direct)
 {
     JoinCut k = {};
     const int spans = (cols + SPAN - 1) / SPAN;
-    // A warp that has more of a row has fewer others to wait for, and more rows are under way side by side; few rows are better
-    // spread over many warps.
-    k.each = spans > 1 && (rows > 2 * NORM_SMS || spans > JOIN_WARPS) ? most_each : 1;
+    k.each = spans > 1 && (rows > std::max(2 * NORM_SMS, few) || spans > JOIN_WARPS) ? most_each : 1;
     for (k.split = 1;; k.split *= 2) {
         const int warps = ((spans + k.split - 1) / k.split + k.each - 1) / k.each;
         k.threads = 32 * warps;
@@ -244,8 +244,21 @@ inline JoinCut join_cut(int rows, int cols, int most_each, int row, int vectors,
     return k;
 }
 inline int type_bytes(int dtype) { return dtype == LRBI_Y_F32 ? 4 : 2; }
-inline JoinCut forward_cut(const JoinArgs &a) { return join_cut(a.rows, a.cols, 4, type_bytes(a.x_dtype) + type_bytes(a.f_dtype), 16, 8, true); }
-inline JoinCut backward_cut(int rows, int cols, int x_dtype, int f_dtype) { return join_cut(rows, cols, 2, 2 * (type_bytes(x_dtype) + type_bytes(f_dtype)), 8, 32, false); }
+// Rows that the blocks of all SMs take at a time, with `each` spans a warp.
+inline int rows_at_once(int cols, int each) { return NORM_SMS * std::max(1, JOIN_WARPS / ((cols + SPAN * each - 1) / (SPAN * each))); }
+// Forward: 300 x 1000 3.9 us with one span a warp, 5.0 with four; 1003 x 801 6.7 and 6.4, 2000 x 1024 8.4 and 5.2.
+inline JoinCut forward_cut(const JoinArgs &a)
+{
+    return join_cut(a.rows, a.cols, 4, rows_at_once(a.cols, 4) / 4, type_bytes(a.x_dtype) + type_bytes(a.f_dtype), 16, 8, true);
+}
+// Backward: with one row for each team or less, 1003 x 801 12.0 us, with two spans a warp 13.9; 2000 x 1024 12.4 and 11.4, 700 x 1500
+// (three rows a team with one span) 13.8 and 10.2.  level (the kernel that then runs is short of registers with two spans):
+// 1000 x 4096 21.3 and 23.4, 5000 x 333 21.7 and 26.0, 2048 x 4096 alike.
+inline JoinCut backward_cut(int rows, int cols, int x_dtype, int f_dtype, bool level)
+{
+    const int few = level ? 5 * rows_at_once(cols, 2) : std::min(rows_at_once(cols, 2), 2 * rows_at_once(cols, 1));
+    return join_cut(rows, cols, 2, few, 2 * (type_bytes(x_dtype) + type_bytes(f_dtype)), 8, 32, false);
+}
 
 template <class Kernel>
 lrbi_status join_launch(Kernel kernel, const JoinCut &k, cudaStream_t s, const Join &j)
