@@ -749,7 +749,8 @@ def lrbi_residual_norm(x: torch.Tensor, f: torch.Tensor, gamma: torch.Tensor | N
         u = norm(out) * gamma + beta           (norm: kind "layer" or "rms")
 
     Returns (out, u, stats): out in x's type, u in f's (None without gamma), stats float32 [4, rows] for the backward pass.  With
-    tokens=True u comes as I8Tokens for the next layer's 8-bit product, and stats is None."""
+    tokens=True u comes as I8Tokens for the next layer's 8-bit product, and stats is None.  Small results (256 KB together) lie in one
+    allocation: clone one to keep or save it by itself."""
     out, u, stats, q, scale = _native().residual_norm(x, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, eps, _kind(kind), tokens, stream)
     return out, (I8Rows._of(q, scale, *x.shape) if tokens else u), stats
 
@@ -760,7 +761,8 @@ def lrbi_residual_norm_backward(du: torch.Tensor | None, dout: torch.Tensor | No
                                 stats: torch.Tensor | None = None, kind: str = "layer", stream=None):
     """Gradients of lrbi_residual_norm from those of u (None without gamma) and of out (None: nothing else reads it), with the out
     and stats that it returned and the arguments that it was given.  Returns (dx, df, grads): dx in out's type, df in f's, and
-    fp32 gradients of the vectors that were given, by name ("gamma", "beta", "post_gamma", "post_beta", "gate"; one allocation)."""
+    fp32 gradients of the vectors that were given, by name ("gamma", "beta", "post_gamma", "post_beta", "gate"; one allocation, and
+    small results all in one)."""
     dx, df, *vectors = _native().residual_norm_backward(du, dout, out, f, gamma, beta, post_gamma, post_beta, gate, residual_scale, stats, _kind(kind), stream)
     return dx, df, {name: g for name, g in zip(("gamma", "beta", "post_gamma", "post_beta", "gate"), vectors) if g is not None}
 

@@ -13,9 +13,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
-#include <tuple>
 #include <utility>
 
 #include "lrbi.h"
@@ -152,6 +152,25 @@ struct Call {
         t.unsafeGetTensorImpl()->set_storage_offset(offset);
         return t;
     }
+    // New arrays: out of one allocation where they are small (allocations cost more than the checks of a call), else each its own.
+    struct Wanted { at::Tensor &tensor; at::DimVector sizes; at::ScalarType type; };
+    void make_all(std::initializer_list<Wanted> wanted) const
+    {
+        int64_t total = 0;
+        for (const Wanted &w : wanted) total += room(w);
+        if (total > SMALL) {
+            for (const Wanted &w : wanted) w.tensor = make(w.sizes, w.type);
+            return;
+        }
+        const at::Tensor all = make({total}, at::kByte);
+        int64_t at_byte = 0;
+        for (const Wanted &w : wanted) {
+            w.tensor = part(all, at_byte / (int64_t)c10::elementSize(w.type), w.sizes, w.type);
+            at_byte += room(w);
+        }
+    }
+    static constexpr int64_t SMALL = 1 << 18;
+    static int64_t room(const Wanted &w) { return (c10::multiply_integers(w.sizes) * (int64_t)c10::elementSize(w.type) + 31) / 32 * 32; }      // rows in vectors start on 32-byte boundaries
     void *handle() const { return stream.stream(); }
 };
 
@@ -505,12 +524,9 @@ PyObject *residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (tokens && !how.gamma) throw BadValue("tokens come from the second norm: give gamma");
         const Call c(x.device, a[11]);
         at::Tensor t[5];      // out, u, stats, q, scale
-        t[0] = c.make({x.rows, x.cols}, x.type);
-        if (tokens) std::tie(t[3], t[4]) = make_rows8(c, x.rows, x.cols);
-        else {
-            if (how.gamma) t[1] = c.make({x.rows, x.cols}, f.type);
-            t[2] = c.make({4, x.rows}, at::kFloat);
-        }
+        if (tokens) c.make_all({{t[0], {x.rows, x.cols}, x.type}, {t[3], {x.rows, lrbi_i8_pitch(x.cols)}, at::kChar}, {t[4], {x.rows}, at::kFloat}});
+        else if (how.gamma) c.make_all({{t[0], {x.rows, x.cols}, x.type}, {t[1], {x.rows, x.cols}, f.type}, {t[2], {4, x.rows}, at::kFloat}});
+        else c.make_all({{t[0], {x.rows, x.cols}, x.type}, {t[2], {4, x.rows}, at::kFloat}});
         auto at = [](const at::Tensor &v) { return v.defined() ? v.data_ptr() : nullptr; };
         check(lrbi_residual_norm(&how, x.data, x.stride, f.data, f.stride, at(t[0]), x.cols, at(t[1]), x.cols, static_cast<int8_t *>(at(t[3])),
                                  static_cast<float *>(at(t[4])), static_cast<float *>(at(t[2])), c.handle()),
@@ -545,18 +561,17 @@ PyObject *residual_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         const Call c(f.device, a[12]);
         at::Tensor t[7];      // dx, df, and the vectors' gradients out of one allocation
-        t[0] = c.make({f.rows, f.cols}, x.type);
-        t[1] = c.make({f.rows, f.cols}, f.type);
         const void *vectors[5] = {how.gamma, how.beta, how.post_gamma, how.post_beta, how.gate};
         float *to[5] = {};
         int count = 0;
         for (const void *v : vectors) count += v != nullptr;
+        const int64_t pitch = (f.cols + 3) / 4 * 4;
+        at::Tensor all;
+        c.make_all({{t[0], {f.rows, f.cols}, x.type}, {t[1], {f.rows, f.cols}, f.type}, {all, {count * pitch}, at::kFloat}});
         if (count) {
-            const int64_t pitch = (f.cols + 3) / 4 * 4;
-            const at::Tensor all = c.make({count * pitch}, at::kFloat);
             for (int i = 0, k = 0; i < 5; ++i) {
                 if (!vectors[i]) continue;
-                t[2 + i] = Call::part(all, k++ * pitch, {f.cols}, at::kFloat);
+                t[2 + i] = Call::part(all, all.storage_offset() + k++ * pitch, {f.cols}, at::kFloat);
                 to[i] = static_cast<float *>(t[2 + i].data_ptr());
             }
         }
