@@ -13,6 +13,11 @@
 // so a gate that is the same for all rows costs no sum of its own.  The two means of df hang on those of ds, but only linearly:
 // with p = dout + rstd g, ds = p - rstd (mean(g) + n mean(g n)), and mean(w ds), mean(w ds nf) follow from the sums of g, g n, w p,
 // w n, w nf p, w nf and w nf n, which are taken together: the threads of a row meet once.
+//
+// Bound: memory where there are many rows (stream in fp32, f in bf16, root mean square, 16384 x 4096: forward 129 us of 125,
+// backward 215 of 187; bf16 97 of 83 with layer norms, 89 without means).  Behind layer norms with betas the backward pass has four
+// sums a column in registers and is bound by issue and what does not fit (186 of 125).  Few rows: 5 us of launch, vectors and
+// first rows.  One span a thread and loads straight into registers, the first form, took 75 and 102 us for 4096 x 4096, now 28 and 56.
 #pragma once
 #include <algorithm>
 
