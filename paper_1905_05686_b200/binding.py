@@ -706,6 +706,8 @@ def lrbi_i8_quantize(layer, W: torch.Tensor, ip: torch.Tensor | None = None, iz:
         raise ValueError("packed factor sizes do not match the layout")
     w = _dev(W, torch.bfloat16, "W")
     factors = [None if t is None else _dev(t, torch.int32, what) for t, what in ((ip, "ip"), (iz, "iz"))]
+    if W.device.index != torch.cuda.current_device() or any(t is not None and t.device != W.device for t in (ip, iz)):
+        raise ValueError("the call's tensors must be on the current CUDA device")
     q = _empty((lay.rows, L.lrbi_i8_pitch(lay.cols)), torch.int8, W.device, stream)
     scale = _empty((lay.rows,), torch.float32, W.device, stream)
     rc = L.lrbi_i8_quantize(ctypes.byref(lay), w, *factors, q.data_ptr(), scale.data_ptr(), _stream_ptr(stream))

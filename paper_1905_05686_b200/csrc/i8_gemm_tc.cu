@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
                     const int at = o0 + c + h * 16;      // first channel of the 64 bytes
                     char *const to = static_cast<char *>(p.y) + ((long long)b0 * p.rows + at) * size;
                     const long long pitch = (long long)p.rows * size;
-                    const int width = min(64, (p.rows - at) * size);      // bytes that are there
+                    const int width = min(64 / size, p.rows - at) * size;      // bytes that are there
                     if (p.vector == 16) {                // eight rows at a time
                         const int piece = lane & 3;
 #pragma unroll

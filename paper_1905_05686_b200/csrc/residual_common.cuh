@@ -35,7 +35,7 @@ struct Join {
     int width;                 // columns of a block: whole spans
     bool whole;                // the vectors start on 16-byte boundaries
     float per;                 // 1 / cols
-    float *parts;              // backward: [groups][4][cols], or null
+    float *parts;              // backward: [groups][4][split * width], or null
 };
 
 __device__ __forceinline__ uint32_t join_rank()
