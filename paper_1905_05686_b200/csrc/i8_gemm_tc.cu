@@ -533,7 +533,7 @@ lrbi_status launch_i8_split(const I8Product &p, int tokens, int split, cudaStrea
     const int stage = I8_A_BYTES + t.tokens * I8_KB;
     const long long tiles = (long long)((p.batch + t.tokens - 1) / t.tokens) * ((p.rows + 127) / 128);
     if (tiles * split > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
-    const bool two = t.tokens <= 128 && tiles * split > NORM_SMS;      // three stages or more in half of an SM's shared memory
+    const bool two = t.tokens <= 128 && tiles * split > i8_at_once(split);      // three stages or more in half of an SM's shared memory
     t.stages = std::min(8, (int)(((two ? I8_SHARED / 2 : I8_SHARED) - sizeof(I8Ctl)) / stage));
     const size_t smem = (size_t)t.stages * stage + sizeof(I8Ctl);      // in all cases more than the 512 bytes a token that the sums take
     CUtensorMap x_map, w_map;

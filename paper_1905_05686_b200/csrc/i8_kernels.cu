@@ -279,9 +279,9 @@ struct Estimate {
     double split(int tokens, int split) const
     {
         const long long ctas = (long long)((batch + tokens - 1) / tokens) * ((rows + 127) / 128) * split;
-        const double turns = rounds(ctas, tokens <= 128 ? 2 * NORM_SMS : NORM_SMS) * (split == 8 && tokens > 128 ? 2. : 1.);
+        const double turns = rounds(ctas, i8_at_once(split)), inner = rounds(ctas, (tokens <= 128 ? 2 : 1) * i8_at_once(split)) * (split == 8 && tokens > 128 ? 2. : 1.);
         const double tile = split == 1 ? 0.3 + 0.013 * tokens : 1. + 0.35 * (split > 2) + 0.35 * (split > 4) + 0.0185 * tokens;
-        const double inside = std::max(turns * ((blocks + split - 1) / split) * (tokens <= 192 ? 0.216 : 0.284), (double)ctas * blocks / split * (16384 + 128 * tokens) / 12e6);
+        const double inside = std::max(inner * ((blocks + split - 1) / split) * (tokens <= 128 ? 0.22 : tokens <= 192 ? 0.25 : 0.34), (double)ctas * blocks / split * (16384 + 128 * tokens) / 12e6);
         return 2. + turns * tile + std::max(inside, memory);
     }
 };

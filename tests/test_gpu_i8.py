@@ -52,7 +52,8 @@ def random_rows8(B, rows, cols, seed=0, most=127):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (3, 7, 0), (1, 4096, 0), (5, 801, 3), (33, 256, 8), (130, 257, 0), (17, 4104, 0), (9, 9216, 0),
-                                           (4, 16384, 1), (3, 20000, 0), (2, 40003, 0), (2, 131072, 0), (1000, 64, 0)])
+                                           (4, 16384, 1), (3, 20000, 0), (2, 40003, 0), (2, 131072, 0), (1000, 64, 0), (1000, 4096, 0), (900, 4097, 0),
+                                           (600, 16384, 8), (250, 20001, 3), (3000, 1000, 0)])
 def test_tokens_are_the_definition(B, rows, cols, pad, dtype):
     x = activations(rows, cols, dtype, pad)
     t = B.lrbi_i8_tokens(x)
@@ -81,7 +82,8 @@ def test_tokens_of_odd_rows(B, cols):
 
 
 @pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
-@pytest.mark.parametrize("rows,cols,dtype", [(5, 800, torch.bfloat16), (7, 1157, torch.float32), (3, 16384, torch.bfloat16), (2, 20001, torch.bfloat16)])
+@pytest.mark.parametrize("rows,cols,dtype", [(5, 800, torch.bfloat16), (7, 1157, torch.float32), (3, 16384, torch.bfloat16), (2, 20001, torch.bfloat16),
+                                             (1100, 4096, torch.bfloat16), (700, 5000, torch.float32), (300, 18000, torch.bfloat16)])
 def test_tokens_of_the_nonlinearity(B, act, rows, cols, dtype):
     x = activations(rows, cols, dtype, pad=2)
     t = B.lrbi_i8_tokens(x, act=act)

@@ -147,14 +147,32 @@ def test_sizes(B, rows, cols, kind):
         check_backward(c, out, stats, True, *c.backward(B, out, stats))
 
 
+# More rows: a warp has four spans (forward) or two (backward) of a row, all of them there or not; rows in one block whose vectors stay
+# in memory; rows shared by two, four and eight blocks.
+MANY = [(400, 1024), (650, 1030), (900, 4096), (640, 4104), (620, 4099), (500, 8192), (330, 9216), (310, 12345), (300, 16384), (300, 20000), (299, 32760), (3000, 512),
+        (6000, 200), (2500, 777)]
+
+
+@pytest.mark.parametrize("kind,beta", [("layer", True), ("rms", False), ("layer", False), ("rms", True)])
+@pytest.mark.parametrize("rows,cols", MANY)
+def test_many_rows(B, rows, cols, kind, beta):
+    for x, f in ((BF16, BF16), (F32, BF16), (F32, F32)):
+        c = Case(rows, cols, x, f, kind, beta=beta)
+        out, u, stats = c.forward(B)
+        check_forward(c, out, u, stats)
+        check_backward(c, out, stats, True, *c.backward(B, out, stats))
+    out, t, _ = c.forward(B, tokens=True)
+    assert (t.q[:, :cols].abs().amax(1) == 127).all() and not t.q[:, cols:].any()
+
+
 @pytest.mark.parametrize("post", [False, True])
 @pytest.mark.parametrize("gate", [False, True])
 @pytest.mark.parametrize("beta", [False, True])
 @pytest.mark.parametrize("pre", [False, True])
 def test_parts(B, post, gate, beta, pre):
-    for cols, pad, params in ((500, 0, BF16), (512, 8, F32), (777, 5, BF16)):
+    for rows, cols, pad, params in ((40, 500, 0, BF16), (40, 512, 8, F32), (40, 777, 5, BF16), (2600, 1024, 0, F32), (600, 16000, 0, BF16)):
         for x, f, kind in ((BF16, BF16, "layer"), (F32, F32, "rms")):
-            c = Case(40, cols, x, f, kind, post, gate, beta, pre, pad, params)
+            c = Case(rows, cols, x, f, kind, post, gate, beta, pre, pad, params)
             out, u, stats = c.forward(B)
             check_forward(c, out, u, stats)
             for dout in (True, False) if pre else (True,):
