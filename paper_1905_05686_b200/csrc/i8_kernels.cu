@@ -275,14 +275,15 @@ struct Estimate {
     double few(int cols) const { return 1.5 + 0.0006 * cols + rows * (0.0004 + 1e-7 * cols); }
     // Pairs: a launch and the last tile's stores; 128 columns of a tile.
     double many() const { return 6. + std::max(rounds((long long)((batch + 255) / 256) * ((rows + 255) / 256), NORM_SMS / 2) * blocks * 0.28, memory); }
-    // Clusters: a launch, the sums and stores of a tile's tokens; 128 columns of a CTA one after the other, or what all of them read of L2.
+    // Clusters: a launch, 10 ns more for each CTA that has to start beside others, the sums and stores of a tile's tokens; 128 columns of a
+    // CTA one after the other, or what all of them read of L2.
     double split(int tokens, int split) const
     {
         const long long ctas = (long long)((batch + tokens - 1) / tokens) * ((rows + 127) / 128) * split;
         const double turns = rounds(ctas, i8_at_once(split)), inner = rounds(ctas, (tokens <= 128 ? 2 : 1) * i8_at_once(split)) * (split == 8 && tokens > 128 ? 2. : 1.);
         const double tile = split == 1 ? 0.3 + 0.013 * tokens : 1. + 0.35 * (split > 2) + 0.35 * (split > 4) + 0.0185 * tokens;
-        const double inside = std::max(inner * ((blocks + split - 1) / split) * (tokens <= 128 ? 0.22 : tokens <= 192 ? 0.25 : 0.34), (double)ctas * blocks / split * (16384 + 128 * tokens) / 12e6);
-        return 2. + turns * tile + std::max(inside, memory);
+        const double inside = std::max(inner * ((blocks + split - 1) / split) * (tokens <= 128 ? 0.22 : tokens <= 192 ? 0.25 : 0.34), (double)ctas * blocks / split * (16384 + 128 * tokens) / 15e6);
+        return 2. + (split > 1 ? 0.01 * ctas : 0.) + turns * tile + std::max(inside, memory);
     }
 };
 

@@ -238,8 +238,9 @@ lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *
 lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s);
 lrbi_status launch_i8_long(const I8Product &p, cudaStream_t s);
 lrbi_status launch_i8_split(const I8Product &p, int tokens, int split, cudaStream_t s);
-// CTAs of the split kernel that run at once where each has an SM: clusters of four or eight leave some of the GPCs' SMs over.
-constexpr int i8_at_once(int split) { return split >= 4 ? 128 : 148; }
+// CTAs of the split kernel that run at once where each has an SM: clusters of four or eight leave some of the GPCs' SMs over (33 and 15
+// of them fit).
+constexpr int i8_at_once(int split) { return split >= 8 ? 120 : split >= 4 ? 132 : 148; }
 
 // Between two blocks: out = scale * x + gate * norm(f), u = norm(out), and the backward pass; null pointers for what a call
 // does not have.
