@@ -3,7 +3,7 @@
 // tcgen05.mma kind::i8, K-major operands with the 128-byte swizzle (a stage is 128 columns of both), sums in tensor memory as
 // 32-bit whole numbers: exact, in any order.  Two kernels:
 //
-//   long   many tokens.  CTA pairs (cta_group::2) of 256 tokens x 256 channels walk the output tiles; two accumulators, so that
+//   long   many tokens.  CTA pairs (cta_group::2) of 256 tokens x 128 to 256 channels walk the output tiles; two accumulators, so that
 //          eight warps scale and store one tile while the next one is computed.  Bound: the tensor cores (pipe 94% busy; 4096
 //          tokens, 16384 x 4096: 167 us, 3.3 Pop/s, twice what bf16 products of that size reach), at smaller sizes the last round of
 //          tiles (1000 tokens, 4096 x 16384: 64 tiles on 74 pairs, 47 us of 40).
@@ -43,6 +43,7 @@ struct I8Tc {
     int rows, batch;                 // channels, tokens
     int blocks;                      // of columns: stages of a tile
     int stages;
+    int channels;                    // long: of a tile, a multiple of 32 from 128 to 256
     int tokens;                      // split: of a tile
     int split;
     int vector;                      // bytes that an access to Y may have: 16, 8, 4 or 2
@@ -140,12 +141,12 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
 
     // Tiles run fastest along the smaller operand: the pairs at work at any time share all of it, and the larger one streams
     // from memory once.
-    const int token_tiles = (p.batch + 255) / 256, channel_tiles = (p.rows + 255) / 256, tiles = token_tiles * channel_tiles;
+    const int token_tiles = (p.batch + 255) / 256, channel_tiles = (p.rows + p.channels - 1) / p.channels, tiles = token_tiles * channel_tiles;
     const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
     const bool tokens_fast = p.batch <= p.rows;
     auto tile_at = [&](int t, int &b0, int &o0) {
         b0 = (tokens_fast ? t % token_tiles : t / channel_tiles) * 256;
-        o0 = (tokens_fast ? t / token_tiles : t % channel_tiles) * 256;
+        o0 = (tokens_fast ? t / token_tiles : t % channel_tiles) * p.channels;
     };
 
     if (warp == 0) {
@@ -159,11 +160,11 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
                 for (int k = 0; k < p.blocks; ++k) {
                     ok = mbar_wait(&ctl->empty[s], parity, abort_flag, p.status, DEV_TIMEOUT_EMPTY);
                     if (!ok) break;
-                    if (rank == 0) mbar_arrive_expect_tx(&ctl->full[s], 2 * I8_LONG_STAGE);       // of both CTAs
+                    if (rank == 0) mbar_arrive_expect_tx(&ctl->full[s], 2 * I8_A_BYTES + p.channels * I8_KB);       // of both CTAs
                     const uint32_t bar = in_cta(smem_u32(&ctl->full[s]), 0);
                     uint8_t *a = smem + (size_t)s * I8_LONG_STAGE;
                     tma_load_2d_pair(a, &x_map, bar, k * I8_KB, b0 + (int)rank * 128);
-                    tma_load_2d_pair(a + I8_A_BYTES, &w_map, bar, k * I8_KB, o0 + (int)rank * 128);
+                    tma_load_2d_pair(a + I8_A_BYTES, &w_map, bar, k * I8_KB, o0 + (int)rank * (p.channels / 2));
                     if (++s == p.stages) { s = 0; parity ^= 1; }
                 }
             }
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t idesc = i8_idesc(256, 256);
+            const uint32_t idesc = i8_idesc(256, p.channels);
             int s = 0, n = 0;
             uint32_t parity = 0;
             bool ok = true;
@@ -198,6 +199,7 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
         const int quad = warp & 3, half = (warp - 2) >> 2;
         uint8_t *stage = epi + (warp - 2) * I8_EPI_BYTES;
         float *scale = reinterpret_cast<float *>(stage + 32 * 64);
+        const int mine0 = (p.channels + 32) / 64 * 32, mine = half ? p.channels - mine0 : mine0;      // channels of the warp
         const bool f32 = p.y_dtype == LRBI_Y_F32;
         const int size = f32 ? 4 : 2;
         bool ok = true;
@@ -206,23 +208,24 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
             int b0, o0;
             tile_at(t, b0, o0);
             b0 += (int)rank * 128 + quad * 32;
-            o0 += half * 128;
+            const int end = min(o0 + p.channels, p.rows);
+            o0 += half * mine0;
             const int left = min(32, p.batch - b0);      // rows of Y that the warp has
             const float token = lane < left ? __ldg(p.x_scale + b0 + lane) : 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) scale[i * 32 + lane] = o0 + i * 32 + lane < p.rows ? __ldg(p.w_scale + o0 + i * 32 + lane) : 0.f;
+            for (int i = 0; i < 4; ++i) scale[i * 32 + lane] = o0 + i * 32 + lane < end ? __ldg(p.w_scale + o0 + i * 32 + lane) : 0.f;
             ok = mbar_wait(&ctl->accum[n & 1], n >> 1 & 1, abort_flag, p.status, DEV_TIMEOUT_ACCUM);
             __syncwarp();                                // the loads below are the whole warp's: one verdict for all lanes
             if (!ok || *abort_flag) break;
             tc_fence_after();
-            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (n & 1) * 256 + half * 128;
+            const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (n & 1) * 256 + half * mine0;
             uint4 *own = reinterpret_cast<uint4 *>(stage + lane * 64);
             const int swap = lane >> 1 & 3;
-            for (int c = 0; c < 128; c += 32) {
+            for (int c = 0; c < mine; c += 32) {
                 int v[32];
                 tmem_ld32(from + c, v);
                 tmem_ld_wait();
-                if (c == 96) {                           // read: the accumulator may be overwritten
+                if (c == mine - 32) {                    // read: the accumulator may be overwritten
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
@@ -256,7 +259,7 @@ __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __gri
                     const int at = o0 + c + h * 16;      // first channel of the 64 bytes
                     char *const to = static_cast<char *>(p.y) + ((long long)b0 * p.rows + at) * size;
                     const long long pitch = (long long)p.rows * size;
-                    const int width = min(64 / size, p.rows - at) * size;      // bytes that are there
+                    const int width = min(64 / size, end - at) * size;      // bytes that are there
                     if (p.vector == 16) {                // eight rows at a time
                         const int piece = lane & 3;
 #pragma unroll
@@ -509,17 +512,18 @@ I8Tc i8_args(const I8Product &p)
 
 }  // namespace
 
-lrbi_status launch_i8_long(const I8Product &p, cudaStream_t s)
+lrbi_status launch_i8_long(const I8Product &p, int channels, cudaStream_t s)
 {
     I8Tc t = i8_args(p);
+    t.channels = channels;
     t.stages = 6;
     const size_t smem = (size_t)t.stages * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl);
     static_assert((size_t)6 * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl) <= I8_SHARED, "");
     CUtensorMap x_map, w_map;
     lrbi_status rc = i8_map(&x_map, p.x, p.batch, p.cols, p.pitch, 128);
-    if (rc == LRBI_OK) rc = i8_map(&w_map, p.w, p.rows, p.cols, p.pitch, 128);
+    if (rc == LRBI_OK) rc = i8_map(&w_map, p.w, p.rows, p.cols, p.pitch, channels / 2);
     if (rc != LRBI_OK) return rc;
-    const long long tiles = (long long)((p.batch + 255) / 256) * ((p.rows + 255) / 256);
+    const long long tiles = (long long)((p.batch + 255) / 256) * ((p.rows + channels - 1) / channels);
     if (tiles > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
     const int pairs = (int)(tiles < NORM_SMS / 2 ? tiles : NORM_SMS / 2);
     return launch_kernel(i8_long_kernel, dim3(2 * pairs), dim3(I8_LONG_THREADS), smem, s, 2, x_map, w_map, t);

@@ -273,17 +273,23 @@ struct Estimate {
     static double rounds(long long units, int at_once) { return (double)((units + at_once - 1) / at_once); }
     // 9 to 16 tokens without tensor memory
     double few(int cols) const { return 1.5 + 0.0006 * cols + rows * (0.0004 + 1e-7 * cols); }
-    // Pairs: a launch and the last tile's stores; 128 columns of a tile.
-    double many() const { return 6. + std::max(rounds((long long)((batch + 255) / 256) * ((rows + 255) / 256), NORM_SMS / 2) * blocks * 0.28, memory); }
-    // Clusters: a launch, 10 ns more for each CTA that has to start beside others, the sums and stores of a tile's tokens; 128 columns of a
-    // CTA one after the other, or what all of them read of L2.
+    // Pairs: a launch and the last tile's stores; 128 columns of a tile, in proportion to what a pair reads of both operands.  Tiles of
+    // fewer channels where they fill the last round better (11049 x 7389, 1606 tokens: 256 channels 110 us, 224 101; 8192 x 8192, 700:
+    // 256 43.8, 192 40.0; 4096 x 16384, 1000: 256 47, 224 82).
+    double many(int channels) const
+    {
+        const double turns = rounds((long long)((batch + 255) / 256) * ((rows + channels - 1) / channels), NORM_SMS / 2);
+        return 6. + std::max(turns * blocks * 0.28 * (256 + channels) / 512, memory);
+    }
+    // Clusters: a launch, 8 ns more for each CTA that has to start beside others, the sums and stores of a tile's tokens; 128 columns of a
+    // CTA one after the other, or what all of them read of L2 (a block takes as long as 4000 bytes more would).
     double split(int tokens, int split) const
     {
         const long long ctas = (long long)((batch + tokens - 1) / tokens) * ((rows + 127) / 128) * split;
         const double turns = rounds(ctas, i8_at_once(split)), inner = rounds(ctas, (tokens <= 128 ? 2 : 1) * i8_at_once(split)) * (split == 8 && tokens > 128 ? 2. : 1.);
-        const double tile = split == 1 ? 0.3 + 0.013 * tokens : 1. + 0.35 * (split > 2) + 0.35 * (split > 4) + 0.0185 * tokens;
-        const double inside = std::max(inner * ((blocks + split - 1) / split) * (tokens <= 128 ? 0.22 : tokens <= 192 ? 0.25 : 0.34), (double)ctas * blocks / split * (16384 + 128 * tokens) / 15e6);
-        return 2. + (split > 1 ? 0.01 * ctas : 0.) + turns * tile + std::max(inside, memory);
+        const double tile = split == 1 ? 0.3 + 0.009 * tokens : 1. + 0.2 * (split > 2) + 0.35 * (split > 4) + 0.0145 * tokens;
+        const double inside = std::max(inner * ((blocks + split - 1) / split) * (tokens <= 128 ? 0.22 : tokens <= 192 ? 0.25 : 0.34), (double)ctas * blocks / split * (20384 + 128 * tokens) / 16e6);
+        return 2. + 0.008 * ctas + turns * tile + std::max(inside, memory);
     }
 };
 
@@ -308,8 +314,10 @@ lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
 {
     if (p.batch <= 8) return launch_few(p, s);
     const Estimate e(p);
-    double best = e.many();
-    int tokens = 0, split = 0;
+    double best = e.many(256);
+    int channels = 256, tokens = 0, split = 0;
+    for (int n = 224; n >= 128; n -= 32)
+        if (e.many(n) < best) { best = e.many(n); channels = n; }
     for (int n : {16, 32, 64, 128, 192, 256})
         for (int k = 1; k <= 8 && k <= e.blocks; k *= 2) {
             const int each = std::min(n, (p.batch + 15) / 16 * 16);
@@ -317,7 +325,7 @@ lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
             if (t < best) { best = t; tokens = each; split = k; }
         }
     if (p.batch <= 16 && e.few(p.cols) < best) return launch_few(p, s);
-    return split ? launch_i8_split(p, tokens, split, s) : launch_i8_long(p, s);
+    return split ? launch_i8_split(p, tokens, split, s) : launch_i8_long(p, channels, s);
 }
 
 }  // namespace lrbi

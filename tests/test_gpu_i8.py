@@ -117,6 +117,16 @@ def test_every_size_of_batch(B, batch):
     assert same(B.lrbi_i8_gemm(w, x), product(w, x, torch.bfloat16))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,batch", [(4490, 65, 1028), (4491, 65, 1028), (3180, 281, 1325), (3181, 281, 1325), (3140, 679, 987), (3141, 679, 987),
+                                             (3974, 598, 780), (3975, 598, 780), (3976, 598, 780), (4098, 577, 808), (4100, 577, 808)])
+def test_sizes_between_rounds_of_tiles(B, rows, cols, batch, dtype):
+    """Many tokens, the outputs cut into 128 to 256 channels for the last round's sake."""
+    w, x = random_rows8(B, rows, cols, 9), random_rows8(B, batch, cols, 10)
+    assert same(B.lrbi_i8_gemm(w, x, y_dtype=dtype), product(w, x, dtype))
+    assert B.device_status() == 0
+
+
 @pytest.mark.parametrize("batch", [3, 40, 300, 600])
 def test_largest_sums(B, batch):
     """131072 columns of 127 * 127 on top of one another stay in 32 bits."""
