@@ -21,9 +21,57 @@ struct TokenArgs {
     int rows, cols, pitch;
 };
 
+__device__ __forceinline__ float not_below(float v, float least)      // a NaN stays
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(least));
+    return r;
+}
+
+// gelu of bf16 values: max(h, 0) - |h| Phi(-|h|), the tail as 2 to a polynomial in n = -min(|h|, 13.25) (there it has left fp32's
+// range), with one of the two special functions of the form in activation.cuh.  The polynomial was fitted to log2 Phi(n) (least
+// squares, reweighted by the errors over those allowed): 4e-7 absolutely and 2^-14 of the tail, rounding in fp32 included.
+__device__ __forceinline__ F2 gelu_bf16(F2 h)
+{
+    float a, b, x, y;
+    split(h, a, b);
+    split(h * f2(0.f), x, y);         // a NaN for infinities, so that -inf does not come as 0
+    const F2 n = f2(not_below(-fabsf(a), -13.25f), not_below(-fabsf(b), -13.25f));
+    F2 p = fma2(n, f2(2.1539401e-09f), f2(1.5457624e-07f));
+    p = fma2(n, p, f2(4.8707334e-06f));
+    p = fma2(n, p, f2(8.925598e-05f));
+    p = fma2(n, p, f2(0.001066364f));
+    p = fma2(n, p, f2(0.008884988f));
+    p = fma2(n, p, f2(0.054551717f));
+    p = fma2(n, p, f2(-0.4579603f));
+    p = fma2(n, p, f2(1.151456f));
+    p = fma2(n, p, f2(-0.99996823f));
+    return fma2(n, exp2_2(p), f2(fmaxf(a, x), fmaxf(b, y)));
+}
+
+// The nonlinearity of values of a row; 0 stays 0 in all of them.
+template <int ACT, int SRC> __device__ __forceinline__ F2 token_act(F2 v)
+{
+    if constexpr (ACT == ACT_NONE) return v;
+    else if constexpr (ACT == LRBI_ACT_GELU && SRC == SRC_BF16) return gelu_bf16(v);
+    else if constexpr (ACT == LRBI_ACT_RELU) {
+        float a, b;
+        split(v, a, b);
+        return f2(not_below(a, 0.f), not_below(b, 0.f));
+    } else {
+        F2 slope;
+        activate<ACT, false, SRC == SRC_F32, false>(v, v, slope);
+        return v;
+    }
+}
+
+// Whether values are taken out of what was loaded twice, and relu again, rather than kept in fp32 between the maximum and the bytes:
+// fewer registers, so twice the chunks a thread (4096 x 4096 of relu 9.6 us, kept 10.1).  Rows that are not whole vectors, and other
+// nonlinearities, take longer again than the registers cost (gelu 21.4 and 14.7).
+__host__ __device__ constexpr bool taken_again(int act, bool strided) { return !strided && (act == ACT_NONE || act == LRBI_ACT_RELU); }
 // blockDim = (threads of a row, rows of a block).  A thread has up to K chunks of its row in registers between the maximum and the
-// bytes: as they were loaded, or as results of the nonlinearity in fp32.  Rows of more chunks are read, and activated, twice.
-// 4096 x 4096 bf16 9.2 us (floor 7.8); 1000 x 16384 of gelu 16.7 (7.6): about two thirds of that is the arithmetic of gelu.
+// bytes: as they were loaded, or as results in fp32 (taken_again()).  Rows of more chunks are read, and activated, twice.
+// 4096 x 4096 bf16 8.3 us (floor 7.8); 1000 x 16384 of gelu 15.3 (7.6): half of that is the arithmetic of gelu.
 template <int SRC, int ACT, bool STRIDED, int K>
 __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_kernel(TokenArgs a)
 {
@@ -37,7 +85,8 @@ __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_
     const int rounds = (a.cols + warps * SPAN * K - 1) / (warps * SPAN * K);
     const char *x = static_cast<const char *>(a.x.data) + row * a.x.stride * SIZE;
     Raw<SRC, STRIDED> raw[K];
-    F2 results[ACT == ACT_NONE ? 1 : K][PAIRS];
+    constexpr bool AGAIN = taken_again(ACT, STRIDED);
+    F2 results[AGAIN ? 1 : K][PAIRS];
     auto load = [&](int round) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -45,25 +94,21 @@ __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_
             raw[k].clear();
             if (there && c < a.cols) raw[k].load_at(x + (long long)c * SIZE, a.cols - c, STRIDED && c0 + SPAN <= a.cols);
         }
-        if constexpr (ACT != ACT_NONE) {
+        if constexpr (!AGAIN) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 raw[k].get(results[k]);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) {
-                    F2 slope;
-                    activate<ACT, false, SRC == SRC_F32, false>(results[k][i], results[k][i], slope);      // 0 stays 0 in all of them
-                }
+                for (int i = 0; i < PAIRS; ++i) results[k][i] = token_act<ACT, SRC>(results[k][i]);
             }
         }
     };
     auto get = [&](int k, F2 (&v)[PAIRS]) {
-        if constexpr (ACT == ACT_NONE) raw[k].get(v);
-        else
+        if constexpr (AGAIN) raw[k].get(v);
 #pragma unroll
-            for (int i = 0; i < PAIRS; ++i) v[i] = results[k][i];
+        for (int i = 0; i < PAIRS; ++i) v[i] = AGAIN ? token_act<ACT, SRC>(v[i]) : results[AGAIN ? 0 : k][i];
     };
-    uint32_t top = 0;
+    float most = 0.f;
     for (int r = 0; r < rounds; ++r) {
         load(r);
 #pragma unroll
@@ -74,11 +119,11 @@ __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_
             for (int i = 0; i < PAIRS; ++i) {
                 float lo, hi;
                 split(v[i], lo, hi);
-                top = max(top, max(__float_as_uint(lo) & 0x7FFFFFFFu, __float_as_uint(hi) & 0x7FFFFFFFu));      // a NaN is above infinity
+                most = not_below(fabsf(hi), not_below(fabsf(lo), most));
             }
         }
     }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    uint32_t top = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));      // a NaN is above infinity
     if (warps > 1) {
         if (lane == 0) part[team * warps + warp] = top;
         __syncthreads();
@@ -221,9 +266,9 @@ lrbi_status tokens_chunks(const TokenArgs &a, cudaStream_t s)
 {
     const int spans = (a.cols + SPAN - 1) / SPAN;
     // Many rows: a thread has more chunks of its row, all of them under way at once, and few others to wait for (4096 x 4096 bf16: one
-    // 17.9 us, four 10.4, eight 9.2).
+    // 17.9 us, four 10.4, eight 9.2, all with a slower maximum than now).
     if (spans > 2 && (long long)a.rows * spans > 64 * NORM_SMS) {
-        if constexpr (SRC == SRC_BF16 && ACT == ACT_NONE && !STRIDED) return tokens_launch<SRC, ACT, STRIDED, 8>(a, 32 * std::min(8, (spans + 7) / 8), s);
+        if constexpr (SRC == SRC_BF16 && taken_again(ACT, STRIDED)) return tokens_launch<SRC, ACT, STRIDED, 8>(a, 32 * std::min(8, (spans + 7) / 8), s);
         return tokens_launch<SRC, ACT, STRIDED, 4>(a, 32 * std::min(16, (spans + 3) / 4), s);
     }
     if (spans <= 16) return tokens_launch<SRC, ACT, STRIDED, 1>(a, 32 * (spans <= 1 ? 1 : spans <= 2 ? 2 : spans <= 4 ? 4 : spans <= 8 ? 8 : 16), s);

@@ -403,20 +403,21 @@ __device__ __forceinline__ void store_i8(int8_t *to, int left, const F2 (&v)[PAI
     for (int i = 0; i < PAIRS; ++i) {
         float lo, hi;
         split(v[i] * f2(factor), lo, hi);
-        b[2 * i] = fine ? __float_as_uint(__fadd_rn(lo, 12582912.f)) : 0;
-        b[2 * i + 1] = fine ? __float_as_uint(__fadd_rn(hi, 12582912.f)) : 0;
+        b[2 * i] = __float_as_uint(__fadd_rn(lo, 12582912.f));      // (added in pairs, the compiler makes one rounding of the two)
+        b[2 * i + 1] = __float_as_uint(__fadd_rn(hi, 12582912.f));
     }
+    const uint32_t keep = fine ? 0xFFFFFFFFu : 0;
     if constexpr (STRIDED) {
         if (whole) {
 #pragma unroll
-            for (int e = 0; e < CHUNK; ++e) to[32 * e] = (int8_t)b[e];
+            for (int e = 0; e < CHUNK; ++e) to[32 * e] = (int8_t)(b[e] & keep);
         } else {
 #pragma unroll
-            for (int e = 0; e < CHUNK; ++e) if (32 * e < left) to[32 * e] = (int8_t)b[e];
+            for (int e = 0; e < CHUNK; ++e) if (32 * e < left) to[32 * e] = (int8_t)(b[e] & keep);
         }
     } else if (left > 0) {
-        *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
-                                                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+        *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) & keep,
+                                                    __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410) & keep);
     }
 }
 

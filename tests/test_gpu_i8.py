@@ -96,6 +96,31 @@ def test_tokens_of_the_nonlinearity(B, act, rows, cols, dtype):
     assert (t.q[:, :cols].abs().amax(1) == 127).all()
 
 
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_nonlinearity_of_every_16_bit_value(B, act):
+    """Rows of one value: 127 times the scale is the value's magnitude.  Off by 2^-20 (1 + h^2 / 8) and 2^-13 of it, and by three
+    roundings of 2^-24; rows below 2^-118 are zeros.  No finite result comes of an infinity or a NaN, but relu's of -inf."""
+    x = torch.arange(65536, device="cuda", dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(-1, 1)
+    t = B.lrbi_i8_tokens(x, act=act)
+    h, got = x.double()[:, 0], 127 * t.scale.double()
+    want = {"relu": h.clamp(min=0), "gelu": -h.abs() * 0.5 * torch.erfc(h.abs() * 0.5 ** 0.5) + h.clamp(min=0), "silu": h * torch.special.expit(h)}[act].abs()
+    finite = torch.isfinite(h)
+    near = finite & (want >= 2.0 ** -100)
+    assert ((got - want).abs() <= want * (2.0 ** -13 + 2.0 ** -20 * (1 + h * h / 8) + 2.0 ** -22))[near].all()
+    assert (got <= 2.0 ** -99)[finite & ~near].all()
+    assert (t.q[:, 0].double() == torch.where(t.scale > 0, torch.where(h < 0, -127., 127.), 0.))[finite].all()
+    lost = torch.isnan(h) | (torch.isinf(h) & (h > 0 if act == "relu" else True))
+    assert torch.isnan(t.scale[lost]).all() and not t.q[lost].any()
+    # the same among many columns, in rows that are and are not whole vectors
+    for cols in (2048, 2049):
+        y = torch.zeros((64, cols), dtype=torch.bfloat16, device="cuda")
+        values = x[finite & (h.abs() < 60)][:, 0]
+        y[:, :1024] = values[torch.randint(0, values.numel(), (64, 1024), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda")]
+        big = B.lrbi_i8_tokens(y.repeat(200, 1), act=act)
+        one = B.lrbi_i8_tokens(y, act=act)
+        assert same(big.q, one.q.repeat(200, 1)) and same(big.scale, one.scale.repeat(200))
+
+
 SHAPES = [(1, 1, 1), (16, 64, 1), (500, 800, 1), (500, 801, 3), (33, 17, 9), (4096, 9216, 1), (4096, 9216, 8), (1000, 4096, 16), (129, 1000, 17), (500, 801, 333),
           (256, 2304, 40), (640, 320, 64), (100, 129, 100), (4096, 512, 128), (300, 3000, 129), (2000, 1024, 200), (1024, 640, 256), (130, 16, 257),
           (4097, 384, 300), (1000, 257, 1000), (257, 4096, 511), (3000, 144, 2000), (8192, 1040, 1500), (16384, 128, 520), (64, 16384, 700), (12, 131072, 5),
