@@ -175,6 +175,8 @@ class PrunedStack:
     def __init__(self, blocks: list[PrunedFFN], joints: list[Joint], residual_scale: float = 1.0):
         if not blocks or len(blocks) != len(joints):
             raise ValueError("a stack has one joint for each of its blocks")
+        if any(block.eps != blocks[0].eps or block.gamma.shape != blocks[0].gamma.shape for block in blocks):
+            raise ValueError("the blocks of a stack have one width and one eps")
         self.blocks, self.joints, self.residual_scale = blocks, joints, residual_scale
 
     def _between(self, i):

@@ -150,3 +150,32 @@ def test_wrong_stacks():
         ffn.PrunedStack([block], [])
     with pytest.raises(ValueError):
         ffn.PrunedStack([], [])
+
+
+def test_blocks_of_a_stack_are_alike():
+    from paper_1905_05686_b200 import ffn
+    joint = ffn.synthetic_stack(256, 512, 1, 128).joints[0]
+    wide, other = ffn.synthetic_block(512, 512, 128), ffn.synthetic_block(256, 512, 128)
+    other.eps = 1e-3
+    for second in (wide, other):
+        with pytest.raises(ValueError):
+            ffn.PrunedStack([ffn.synthetic_block(256, 512, 128), second], [joint, joint])
+
+
+def test_a_block_twice():
+    """A stack that goes through the same block twice: the gradients of both uses, apart, are those of two equal blocks."""
+    from paper_1905_05686_b200 import ffn
+    one, two = ffn.synthetic_stack(256, 512, 1, 128), ffn.synthetic_stack(256, 512, 2, 128)
+    shared = ffn.PrunedStack(one.blocks * 2, one.joints * 2)
+    for block, joint in zip(two.blocks, two.joints):
+        for a, b in ((block.up.W, one.blocks[0].up.W), (block.down.W, one.blocks[0].down.W)):
+            a.copy_(b)
+        block.up.refresh()
+        block.down.refresh()
+    x = torch.randn((70, 256), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    results = []
+    for stack in (shared, two):
+        out, kept = stack.forward(x)
+        dx, grads = stack.backward(torch.ones_like(out), kept)
+        results.append([out, dx, stack.prompts()(x)] + [g[name] for g in grads for name in sorted(g)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
