@@ -248,13 +248,19 @@ inline JoinCut join_cut(int rows, int cols, int most_each, int few, int row, int
     k.groups = std::min((rows + k.teams - 1) / k.teams, NORM_SMS / k.split);
     return k;
 }
+// Vectors of the forward pass in shared memory: gate * post_gamma, gamma, beta, gate * post_beta, up to the last that there is.
+__host__ __device__ inline int join_vectors(const JoinArgs &a) { return a.post_beta ? 4 : a.beta ? 3 : a.gamma ? 2 : 1; }
 inline int type_bytes(int dtype) { return dtype == LRBI_Y_F32 ? 4 : 2; }
 // Rows that the blocks of all SMs take at a time, with `each` spans a warp.
 inline int rows_at_once(int cols, int each) { return NORM_SMS * std::max(1, JOIN_WARPS / ((cols + SPAN * each - 1) / (SPAN * each))); }
-// Forward: 300 x 1000 3.9 us with one span a warp, 5.0 with four; 1003 x 801 6.7 and 6.4, 2000 x 1024 8.4 and 5.2.
+// Forward.  Room for the vectors that there are (2000 x 12896 bf16, gamma alone: 54 us, with room for all four none fit, 90).  A row whose
+// vectors have no room reads up to six: more than three, and two blocks that share the row, beside the vectors, are faster (2000 x 12891
+// fp32: three 173 us and 160, six 263 and 161; in whole vectors, 12896, 117 and 124, 180 and 128; 100 rows 13 and 16, 20 and 17).
+// 300 x 1000 3.9 us with one span a warp, 5.0 with four; 1003 x 801 6.7 and 6.4, 2000 x 1024 8.4 and 5.2.
 inline JoinCut forward_cut(const JoinArgs &a)
 {
-    return join_cut(a.rows, a.cols, 4, rows_at_once(a.cols, 4) / 4, type_bytes(a.x_dtype) + type_bytes(a.f_dtype), 16, 8, true);
+    const int reads = (a.post_gamma != nullptr) + (a.gate != nullptr) * (a.post_beta ? 2 : 1) + (a.post_beta != nullptr) + (a.gamma != nullptr) + (a.beta != nullptr);
+    return join_cut(a.rows, a.cols, 4, rows_at_once(a.cols, 4) / 4, type_bytes(a.x_dtype) + type_bytes(a.f_dtype), 4 * join_vectors(a), 8, reads <= 3);
 }
 // Backward: with one row for each team or less, 1003 x 801 12.0 us, with two spans a warp 13.9; 2000 x 1024 12.4 and 11.4, 700 x 1500
 // (three rows a team with one span) 13.8 and 10.2.  level (the kernel that then runs is short of registers with two spans):

@@ -84,8 +84,8 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
     constexpr int SLOT = XS::SLOT + FS::SLOT, XSIZE = XS::SIZE, FSIZE = FS::SIZE;
     Team t(j.split);
     const int block0 = t.rank * j.width, w0 = t.warp * K * SPAN, c0 = block0 + w0, left = a.cols - c0;      // first columns of the block, of the warp
-    float *vectors = shared;                                 // gate * post_gamma, gate * post_beta, gamma, beta
-    float *part = vectors + (DIRECT ? 0 : 4 * j.width);
+    float *vectors = shared;                                 // gate * post_gamma, gamma, beta, gate * post_beta, up to the last that there is
+    float *part = vectors + (DIRECT ? 0 : join_vectors(a) * j.width);
     char *ring = reinterpret_cast<char *>(part + blockDim.y * 2 * t.entries() * 2) + (threadIdx.y * t.warps + t.warp) * 2 * SLOT;
     begin();
     const XS x(a.x, a.x_stride, c0, a.cols);
@@ -101,9 +101,9 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
         const float4 pb = four_of(a.post_beta, a.param_dtype, j.whole, from, a.cols, 0.f), g = four_of(a.gamma, a.param_dtype, j.whole, from, a.cols, 0.f);
         const float4 b = four_of(a.beta, a.param_dtype, j.whole, from, a.cols, 0.f);
         to[0] = gate * pg;
-        if (a.post_beta) to[pitch] = gate * pb;
-        if (a.gamma) to[2 * pitch] = g;
-        if (a.beta) to[3 * pitch] = b;
+        if (a.post_beta) to[3 * pitch] = gate * pb;
+        if (a.gamma) to[pitch] = g;
+        if (a.beta) to[2 * pitch] = b;
     }
     __syncthreads();
     if (j.split > 1) t.meet();       // blocks write to one another once all of them have begun
@@ -112,13 +112,13 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
     char *const out = static_cast<char *>(a.out) + (long long)c * XSIZE, *const u = static_cast<char *>(a.u) + (long long)c * FSIZE;
     const float *own = vectors + w0;
     const Params p = {nullptr, nullptr, a.param_dtype, j.whole};
-    // Chunk k of a vector: gate * post_gamma, gate * post_beta, gamma, beta.
+    // Chunk k of a vector: gate * post_gamma, gamma, beta, gate * post_beta.
     auto vector = [&](int which, int k, F2 (&w)[PAIRS]) {
         if constexpr (!DIRECT) get_vector<STRIDED>(own + which * j.width, k, t.lane, w);
         else {
-            const void *const all[4] = {a.post_gamma, a.post_beta, a.gamma, a.beta};
+            const void *const all[4] = {a.post_gamma, a.gamma, a.beta, a.post_beta};
             load_param<STRIDED>(all[which], p, c + k * SPAN, a.cols, all[which] ? 0.f : 1.f, w);
-            if (which < 2 && a.gate) {
+            if ((which == 0 || which == 3) && a.gate) {
                 F2 gate[PAIRS];
                 load_param<STRIDED>(a.gate, p, c + k * SPAN, a.cols, 0.f, gate);
 #pragma unroll
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) v[k][i] = fma2(b[i], f2(a.residual_scale), fma2(v[k][i], scale, shift) * w[i]);
             if (a.post_beta) {
-                vector(1, k, b);
+                vector(3, k, b);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[k][i] = v[k][i] + b[i];
             }
@@ -182,9 +182,9 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (!FULL && left <= k * SPAN) break;
-            vector(2, k, w);
+            vector(1, k, w);
             if (a.beta) {
-                vector(3, k, b);
+                vector(2, k, b);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[k][i] = fma2(fma2(v[k][i], scale, shift), w[i], b[i]);
             } else {

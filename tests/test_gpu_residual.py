@@ -179,6 +179,19 @@ def test_parts(B, post, gate, beta, pre):
                 check_backward(c, out, stats, dout, *c.backward(B, out, stats, dout))
 
 
+@pytest.mark.parametrize("post,gate,beta,pre", [(False, False, False, True), (True, False, False, True), (True, True, False, True), (False, False, True, True),
+                                               (True, False, True, False), (False, True, False, False), (True, True, True, True), (True, True, True, False)])
+@pytest.mark.parametrize("rows,cols,x", [(310, 8704, F32), (150, 8701, F32), (310, 12896, BF16), (305, 12891, BF16), (160, 16381, F32)])
+def test_vectors_that_leave_room(B, rows, cols, x, post, gate, beta, pre):
+    """Long rows in one block beside few vectors, without them, or shared by blocks."""
+    c = Case(rows, cols, x, BF16, "rms", post, gate, beta, pre)
+    out, u, stats = c.forward(B)
+    check_forward(c, out, u, stats)
+    if pre:
+        again, t, _ = c.forward(B, tokens=True)
+        assert torch.equal(again, out) and (t.q[:, :cols].abs().amax(1) == 127).all() and not t.q[:, cols:].any()
+
+
 def test_values_far_from_zero(B):
     """A mean a thousand times the spread: squares are summed about it."""
     c = Case(30, 1000, F32, F32, offset=1000.0)
