@@ -437,7 +437,7 @@ LRBI_API lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, 
  *           ones are exactly zero, and what the array holds at their places is not looked at.
  * lrbi_i8_tokens    x [rows][cols] (bf16 or fp32, rows x_stride elements apart) -> q, scale of the rows of act(x); act: LRBI_ACT_*,
  *           or LRBI_ACT_NONE for x itself.  act(x) is taken in fp32 (as far off as
- *           lrbi_activation states, for x in bf16 as for outputs in bf16; below 2^-118 it may come as 0) and not rounded.
+ *           lrbi_activation states for outputs in fp32; below 2^-118 it may come as 0) and not rounded.
  * lrbi_i8_gemm      Y [batch][rows], contiguous, overlapping none of the inputs.  batch may be 0.
  */
 #define LRBI_I8_MAX_COLS (1 << 17)

@@ -28,50 +28,30 @@ __device__ __forceinline__ float not_below(float v, float least)      // a NaN s
     return r;
 }
 
-// gelu of bf16 values: max(h, 0) - |h| Phi(-|h|), the tail as 2 to a polynomial in n = -min(|h|, 13.25) (there it has left fp32's
-// range), with one of the two special functions of the form in activation.cuh.  The polynomial was fitted to log2 Phi(n) (least
-// squares, reweighted by the errors over those allowed): 4e-7 absolutely and 2^-14 of the tail, rounding in fp32 included.
-__device__ __forceinline__ F2 gelu_bf16(F2 h)
-{
-    float a, b, x, y;
-    split(h, a, b);
-    split(h * f2(0.f), x, y);         // a NaN for infinities, so that -inf does not come as 0
-    const F2 n = f2(not_below(-fabsf(a), -13.25f), not_below(-fabsf(b), -13.25f));
-    F2 p = fma2(n, f2(2.1539401e-09f), f2(1.5457624e-07f));
-    p = fma2(n, p, f2(4.8707334e-06f));
-    p = fma2(n, p, f2(8.925598e-05f));
-    p = fma2(n, p, f2(0.001066364f));
-    p = fma2(n, p, f2(0.008884988f));
-    p = fma2(n, p, f2(0.054551717f));
-    p = fma2(n, p, f2(-0.4579603f));
-    p = fma2(n, p, f2(1.151456f));
-    p = fma2(n, p, f2(-0.99996823f));
-    return fma2(n, exp2_2(p), f2(fmaxf(a, x), fmaxf(b, y)));
-}
-
-// The nonlinearity of values of a row; 0 stays 0 in all of them.
-template <int ACT, int SRC> __device__ __forceinline__ F2 token_act(F2 v)
+// The nonlinearity of values of a row, as for results in fp32; 0 stays 0 in all of them.  (gelu with a tail off by 2^-14, as results in
+// bf16 allow, moved ten times the bytes to the other side of a tie that roundings in fp32 move.)
+template <int ACT> __device__ __forceinline__ F2 token_act(F2 v)
 {
     if constexpr (ACT == ACT_NONE) return v;
-    else if constexpr (ACT == LRBI_ACT_GELU && SRC == SRC_BF16) return gelu_bf16(v);
     else if constexpr (ACT == LRBI_ACT_RELU) {
         float a, b;
         split(v, a, b);
         return f2(not_below(a, 0.f), not_below(b, 0.f));
     } else {
         F2 slope;
-        activate<ACT, false, SRC == SRC_F32, false>(v, v, slope);
+        activate<ACT, false, true, false>(v, v, slope);
         return v;
     }
 }
 
 // Whether values are taken out of what was loaded twice, and relu again, rather than kept in fp32 between the maximum and the bytes:
 // fewer registers, so twice the chunks a thread (4096 x 4096 of relu 9.6 us, kept 10.1).  Rows that are not whole vectors, and other
-// nonlinearities, take longer again than the registers cost (gelu 21.4 and 14.7).
+// nonlinearities, take longer again than the registers cost (a gelu of fewer steps than this one 21.4 and 14.7).
 __host__ __device__ constexpr bool taken_again(int act, bool strided) { return !strided && (act == ACT_NONE || act == LRBI_ACT_RELU); }
 // blockDim = (threads of a row, rows of a block).  A thread has up to K chunks of its row in registers between the maximum and the
 // bytes: as they were loaded, or as results in fp32 (taken_again()).  Rows of more chunks are read, and activated, twice.
-// 4096 x 4096 bf16 8.3 us (floor 7.8); 1000 x 16384 of gelu 15.3 (7.6): half of that is the arithmetic of gelu.
+// 4096 x 4096 bf16 8.2 us (floor 7.8), fp32 12.6 (13.0); of gelu 15.7 and 17.8, of silu 16.5 and 14.0; 1000 x 16384 bf16 of gelu 17.0 (7.6): more
+// than half of that is the arithmetic of gelu.
 template <int SRC, int ACT, bool STRIDED, int K>
 __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_kernel(TokenArgs a)
 {
@@ -99,14 +79,14 @@ __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_
             for (int k = 0; k < K; ++k) {
                 raw[k].get(results[k]);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) results[k][i] = token_act<ACT, SRC>(results[k][i]);
+                for (int i = 0; i < PAIRS; ++i) results[k][i] = token_act<ACT>(results[k][i]);
             }
         }
     };
     auto get = [&](int k, F2 (&v)[PAIRS]) {
         if constexpr (AGAIN) raw[k].get(v);
 #pragma unroll
-        for (int i = 0; i < PAIRS; ++i) v[i] = AGAIN ? token_act<ACT, SRC>(v[i]) : results[AGAIN ? 0 : k][i];
+        for (int i = 0; i < PAIRS; ++i) v[i] = AGAIN ? token_act<ACT>(v[i]) : results[AGAIN ? 0 : k][i];
     };
     float most = 0.f;
     for (int r = 0; r < rounds; ++r) {
