@@ -32,11 +32,13 @@ __device__ __forceinline__ void row_two(float &p, float &q, Team &t, float *part
     }
 }
 
-// 1 / root over a row of the values v (zeros where there is no column), and the mean.  Squares are summed beside the values, as
-// long as the mean's square is at most the variance (the difference then loses one bit at most); else once more about the mean,
-// however far that is from zero.  left: columns from the warp's first one on.
+// Mean and 1 / root over a row of the values v (zeros where there is no column).  Squares are summed beside the values, as long as
+// the mean's square is at most the variance (the difference then loses one bit at most).  Else the mean is taken off the values, and
+// what is left of them is summed once more with its squares: its mean corrects the first one, whose own error, roundings of a sum of
+// large values, would be a part of the spread (values 1e5 times their spread from zero: 2e-2 of it).  centre: what is left to take off v.
+// left: columns from the warp's first one on.
 template <int K, bool STRIDED, bool RMS, bool FULL>
-__device__ __forceinline__ void row_statistics(const F2 (&v)[K][PAIRS], int left, const Join &j, Team &t, float *part, float &mean, float &rstd)
+__device__ __forceinline__ void row_statistics(F2 (&v)[K][PAIRS], int left, const Join &j, Team &t, float *part, float &mean, float &centre, float &rstd)
 {
     F2 s = f2(0.f), q = f2(0.f);
 #pragma unroll
@@ -48,25 +50,30 @@ __device__ __forceinline__ void row_statistics(const F2 (&v)[K][PAIRS], int left
         }
     float sum = RMS ? 0.f : sum2(s), square = sum2(q);
     row_two(sum, square, t, part);
-    mean = RMS ? 0.f : sum * j.per;
+    mean = centre = RMS ? 0.f : sum * j.per;
     float variance = square * j.per;
     if (!RMS) {
         variance = fmaf(-mean, mean, variance);
         if (!(mean * mean <= variance)) {          // the same in all threads of the row
-            q = f2(0.f);
+            s = q = f2(0.f);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                F2 d[PAIRS];
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) d[i] = v[k][i] + f2(-mean);
-                keep_there<STRIDED, FULL>(d, left - k * SPAN, t.lane);
+                for (int i = 0; i < PAIRS; ++i) v[k][i] = v[k][i] + f2(-mean);
+                keep_there<STRIDED, FULL>(v[k], left - k * SPAN, t.lane);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) q = fma2(d[i], d[i], q);
+                for (int i = 0; i < PAIRS; ++i) {
+                    s = s + v[k][i];
+                    q = fma2(v[k][i], v[k][i], q);
+                }
             }
+            sum = sum2(s);
             square = sum2(q);
-            float off = 0.f;
-            row_two(off, square, t, part);
-            variance = square * j.per;
+            row_two(sum, square, t, part);
+            centre = sum * j.per;
+            mean += centre;
+            variance = fmaf(-centre, centre, square * j.per);
+            if (variance < 0.f) variance = 0.f;    // (a NaN stays)
         }
     }
     rstd = inverse_root(variance + j.a.eps);
@@ -141,10 +148,10 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
         F2 v[K][PAIRS], w[PAIRS], b[PAIRS];
 #pragma unroll
         for (int k = 0; k < K; ++k) f.template get<FULL>(slot, row, k, max(left - k * SPAN, 0), t.lane, v[k]);
-        float mean = 0.f, rstd = 1.f;
-        if (a.post_gamma) row_statistics<K, STRIDED, RMS, FULL>(v, left, j, t, part, mean, rstd);
+        float mean = 0.f, centre = 0.f, rstd = 1.f;
+        if (a.post_gamma) row_statistics<K, STRIDED, RMS, FULL>(v, left, j, t, part, mean, centre, rstd);
         if (tells) { a.stats[2ll * a.rows + row] = mean; a.stats[3ll * a.rows + row] = rstd; }
-        F2 scale = f2(rstd), shift = f2(-mean * rstd);
+        F2 scale = f2(rstd), shift = f2(-centre * rstd);
         char *to = out + row * a.out_stride * XSIZE;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -170,13 +177,13 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_forward_kernel(Join j)
             store_at<XSIZE, STRIDED>(to + k * SPAN * XSIZE, FULL ? SPAN : a.cols - c - k * SPAN, v[k], STRIDED && (FULL || left >= (k + 1) * SPAN));
             keep_there<STRIDED, FULL>(v[k], left - k * SPAN, t.lane);
         }
-        mean = 0.f;
+        mean = centre = 0.f;
         rstd = 1.f;
-        if (a.gamma) row_statistics<K, STRIDED, RMS, FULL>(v, left, j, t, part, mean, rstd);
+        if (a.gamma) row_statistics<K, STRIDED, RMS, FULL>(v, left, j, t, part, mean, centre, rstd);
         if (tells) { a.stats[row] = mean; a.stats[a.rows + row] = rstd; }
         if (!a.gamma) continue;
         scale = f2(rstd);
-        shift = f2(-mean * rstd);
+        shift = f2(-centre * rstd);
         to = u + row * a.u_stride * FSIZE;
         uint32_t top = 0;
 #pragma unroll

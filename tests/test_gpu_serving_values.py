@@ -54,3 +54,53 @@ def test_bytes_of_the_nonlinearity(B, act, rows, cols, pad):
     exact = want * (127 / top)
     slack = exact.abs() * (bound + bound.gather(1, at) + 2.0 ** -23)
     assert ((t.q[:, :cols].double() - exact).abs() <= 0.5 + slack).all()
+
+
+def norm64(v, eps):
+    mean = v.mean(1, keepdim=True)
+    rstd = ((v - mean).square().mean(1, keepdim=True) + eps) ** -0.5
+    return (v - mean) * rstd, mean[:, 0], rstd[:, 0]
+
+
+@pytest.mark.parametrize("which", ["x", "f"])
+@pytest.mark.parametrize("rows,cols", [(30, 1000), (7, 801), (900, 4096), (620, 4099), (300, 16384), (300, 20000), (300, 32760), (5, 32768)])
+def test_rows_far_from_zero(B, rows, cols, which):
+    """Means 1e5 times the spread, of the stream (the second norm) or of f (the first).
+
+    A sum over a row is a chain of at most 31 additions for any one value: 16 in a thread (four spans, two values at a time), 1 for its
+    pair, 5 in the warp, 9 over a row's warps.  The mean that is subtracted first is off by up to 31 roundings of 1e5, a fifth of the
+    spread; what is left is summed anew, in magnitudes of the spread: a normalised value n is off by 31 roundings of the mean, 20 of the
+    root and a few of its own, together below 2^-18 (|n| + 1).  The mean that is kept is off by its own rounding and by less than
+    another."""
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    rand = lambda *shape: torch.randn(shape, generator=g, device="cuda")
+    x, f = rand(rows, cols) + (1e5 if which == "x" else 0), rand(rows, cols) * 0.7 - (7e4 if which == "f" else 0)
+    gamma, post, gate = 1 + 0.2 * rand(cols), 1 + 0.2 * rand(cols), 0.5 + 0.1 * rand(cols)
+    beta, post_beta = 0.2 * rand(cols), 0.2 * rand(cols)
+    how = dict(post_gamma=post, post_beta=post_beta, gate=gate, residual_scale=0.75, eps=1e-5)
+    out, u, stats = B.lrbi_residual_norm(x, f, gamma, beta, **how)
+    n, mean, rstd = norm64(f.double(), 1e-5)
+    assert ((stats[2] - mean).abs() <= 2.0 ** -23 * mean.abs() + 2.0 ** -18).all() and ((stats[3] / rstd - 1).abs() <= 2.0 ** -18).all()
+    z, size = n * post.double() + post_beta.double(), (n.abs() + 1) * post.abs() + post_beta.abs()
+    want = 0.75 * x.double() + gate.double() * z
+    assert ((out - want).abs() <= 2.0 ** -18 * gate.abs() * size + 2.0 ** -24 * (want.abs() + 0.75 * x.abs() + (gate * z).abs())).all()
+    n, mean, rstd = norm64(out.double(), 1e-5)
+    assert ((stats[0] - mean).abs() <= 2.0 ** -23 * mean.abs() + 2.0 ** -18).all() and ((stats[1] / rstd - 1).abs() <= 2.0 ** -18).all()
+    want, size = n * gamma.double() + beta.double(), (n.abs() + 1) * gamma.abs() + beta.abs()
+    assert ((u - want).abs() <= 2.0 ** -18 * size).all()
+    again, t, _ = B.lrbi_residual_norm(x, f, gamma, beta, tokens=True, **how)
+    step = t.scale.double()[:, None]
+    assert torch.equal(again, out)
+    assert ((t.q[:, :cols] * step - want).abs() <= step * (0.5 + 2.0 ** -16) + 2.0 ** -18 * size).all()
+
+
+def test_rows_of_one_value(B):
+    """A spread of nothing: n is 0 but for what the mean is off, and the root is that of eps."""
+    for cols in (40, 1000, 4096, 12891):
+        value = torch.tensor([1000.0, -3.3, 1e6, 1 / 3], device="cuda")[:, None]
+        x = value.expand(4, cols).contiguous()
+        gamma = torch.ones(cols, device="cuda")
+        out, u, stats = B.lrbi_residual_norm(x, torch.zeros_like(x), gamma)
+        assert torch.equal(out, x) and ((stats[0] - value[:, 0]).abs() <= 2.0 ** -23 * value[:, 0].abs()).all()
+        # what is left of a value, some 31 roundings, is taken off to 2^-18 of itself
+        assert (u.abs() <= 2.0 ** -18 * 31 * 2.0 ** -24 * value.abs() / 1e-5 ** 0.5).all() and ((stats[1] * 1e-5 ** 0.5 - 1).abs() <= 2.0 ** -18 + (31 * 2.0 ** -24 * value[:, 0]) ** 2 * 2.0 ** -18 / 1e-5).all()
