@@ -439,6 +439,7 @@ LRBI_API lrbi_status lrbi_w4_gemv(const uint32_t *packed, const uint32_t *meta, 
  *           or LRBI_ACT_NONE for x itself.  act(x) is taken in fp32 (as far off as
  *           lrbi_activation states for outputs in fp32; below 2^-118 it may come as 0) and not rounded.
  * lrbi_i8_gemm      Y [batch][rows], contiguous, overlapping none of the inputs.  batch may be 0.
+ * lrbi_i8_gemm_plan how lrbi_i8_gemm runs a product of that size, batch 1 or more (nothing is launched, no device is needed).
  */
 #define LRBI_I8_MAX_COLS (1 << 17)
 enum { LRBI_ACT_NONE = -1 };
@@ -449,6 +450,17 @@ LRBI_API lrbi_status lrbi_i8_tokens(const void *x, int32_t x_dtype, int64_t x_st
                                     int8_t *q, float *scale, void *stream);
 LRBI_API lrbi_status lrbi_i8_gemm(const int8_t *w_q, const float *w_scale, int32_t rows, int32_t cols, const int8_t *x_q,
                                   const float *x_scale, int32_t batch, void *Y, int32_t y_dtype, void *stream);
+enum { LRBI_I8_FEW = 0, LRBI_I8_SPLIT = 1, LRBI_I8_LONG = 2 };
+typedef struct {
+    int32_t kernel;        /* LRBI_I8_FEW warp-level products, _SPLIT tensor memory and clusters, _LONG pairs of CTAs      */
+    int32_t tokens;        /* of an output tile                                                                           */
+    int32_t channels;      /* of an output tile                                                                           */
+    int32_t split;         /* LRBI_I8_SPLIT: CTAs of a cluster that share the columns (1: no cluster); else 1              */
+    int32_t stages;        /* steps of the columns that are under way at once                                             */
+    int32_t threads;       /* of a CTA                                                                                    */
+    int32_t per_sm;        /* LRBI_I8_SPLIT: CTAs that an SM has room for; else 1                                          */
+} lrbi_i8_plan;
+LRBI_API lrbi_status lrbi_i8_gemm_plan(int32_t rows, int32_t cols, int32_t batch, int32_t y_dtype, lrbi_i8_plan *plan);
 
 /*
  * Between two blocks: the norm behind a block, its gate, the residual scale and the norm before the next block, in one pass.

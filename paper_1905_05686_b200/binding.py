@@ -46,6 +46,11 @@ class GemmPlan(ctypes.Structure):
                 ("scratch_bytes", ctypes.c_uint64)]
 
 
+class I8Plan(ctypes.Structure):
+    """lrbi_i8_plan: how lrbi_i8_gemm would run a product."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("kernel", "tokens", "channels", "split", "stages", "threads", "per_sm")]
+
+
 class TileRanks(ctypes.Structure):
     """lrbi_tile_ranks: device arrays with one rank and two word offsets per tile."""
     _fields_ = [("ranks", ctypes.c_void_p), ("ip_offset", ctypes.c_void_p), ("iz_offset", ctypes.c_void_p)]
@@ -165,6 +170,8 @@ def lib():
         L.lrbi_i8_tokens.restype = i32
         L.lrbi_i8_gemm.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, i32, vp]
         L.lrbi_i8_gemm.restype = i32
+        L.lrbi_i8_gemm_plan.argtypes = [i32, i32, i32, i32, ctypes.POINTER(I8Plan)]
+        L.lrbi_i8_gemm_plan.restype = i32
         rp = ctypes.POINTER(Residual)
         L.lrbi_residual_norm.argtypes = [rp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp]
         L.lrbi_residual_norm.restype = i32
@@ -730,6 +737,20 @@ def lrbi_i8_gemm(weights: I8Weights, tokens: I8Tokens, y_dtype=torch.bfloat16, s
     if weights.cols != tokens.cols:
         raise ValueError("the tokens must have as many columns as the weights")
     return _native().i8_gemm(weights.q, weights.scale, weights.rows, weights.cols, tokens.q, tokens.scale, tokens.rows, y_dtype, stream)
+
+
+I8_FEW, I8_SPLIT, I8_LONG = range(3)
+
+
+def i8_gemm_plan(rows: int, cols: int, batch: int, y_dtype=torch.bfloat16) -> I8Plan:
+    """The kernel that lrbi_i8_gemm would run for [rows, cols] weights and `batch` tokens (nothing is launched)."""
+    if y_dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("y_dtype must be torch.bfloat16 or torch.float32")
+    plan = I8Plan()
+    rc = lib().lrbi_i8_gemm_plan(rows, cols, batch, Y_F32 if y_dtype == torch.float32 else Y_BF16, ctypes.byref(plan))
+    if rc != OK:
+        raise LrbiError(rc, "lrbi_i8_gemm_plan")
+    return plan
 
 
 NORMS = {"layer": 0, "rms": 1}

@@ -269,6 +269,14 @@ lrbi_status lrbi_i8_gemm(const int8_t *w_q, const float *w_scale, int32_t rows, 
     return launch_i8_gemm({w_q, w_scale, x_q, x_scale, Y, y_dtype, rows, cols, i8_pitch(cols), batch}, static_cast<cudaStream_t>(stream));
 }
 
+lrbi_status lrbi_i8_gemm_plan(int32_t rows, int32_t cols, int32_t batch, int32_t y_dtype, lrbi_i8_plan *plan)
+{
+    if (rows < 1 || !i8_cols_ok(cols) || batch < 1 || !dtype_ok(y_dtype) || !plan) return LRBI_ERR_INVALID_ARG;
+    if (rows > MOST_ROWS || batch > MOST_ROWS) return LRBI_ERR_UNSUPPORTED;
+    *plan = i8_gemm_plan(rows, cols, batch, y_dtype);
+    return LRBI_OK;
+}
+
 lrbi_status lrbi_residual_norm(const lrbi_residual *how, const void *x, int64_t x_stride, const void *f, int64_t f_stride, void *out, int64_t out_stride,
                                void *u, int64_t u_stride, int8_t *u_q, float *u_scale, float *stats, void *stream)
 {

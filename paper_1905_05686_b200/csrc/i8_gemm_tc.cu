@@ -107,7 +107,7 @@ __device__ __forceinline__ void let_copies_land()
 // The tile's M is the token (a lane of tensor memory), its N the channel: a thread has neighbouring outputs of one row of Y.
 // They go through 2 KB a warp, 32 rows x 64 bytes with the pieces of a row in an order that keeps the banks apart, and out as
 // whole sectors.
-constexpr int I8_LONG_STAGE = 2 * I8_A_BYTES, I8_EPI_BYTES = 32 * 64 + 128 * 4;
+constexpr int I8_LONG_STAGES = 6, I8_LONG_STAGE = 2 * I8_A_BYTES, I8_EPI_BYTES = 32 * 64 + 128 * 4;
 __global__ void __launch_bounds__(I8_LONG_THREADS, 1) i8_long_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, I8Tc p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -512,13 +512,15 @@ I8Tc i8_args(const I8Product &p)
 
 }  // namespace
 
-lrbi_status launch_i8_long(const I8Product &p, int channels, cudaStream_t s)
+lrbi_i8_plan i8_long_plan(int channels) { return {LRBI_I8_LONG, 256, channels, 1, I8_LONG_STAGES, I8_LONG_THREADS, 1}; }
+
+lrbi_status launch_i8_long(const I8Product &p, const lrbi_i8_plan &plan, cudaStream_t s)
 {
     I8Tc t = i8_args(p);
-    t.channels = channels;
-    t.stages = 6;
+    const int channels = t.channels = plan.channels;
+    t.stages = plan.stages;
     const size_t smem = (size_t)t.stages * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl);
-    static_assert((size_t)6 * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl) <= I8_SHARED, "");
+    static_assert((size_t)I8_LONG_STAGES * I8_LONG_STAGE + I8_EPI_WARPS * I8_EPI_BYTES + sizeof(I8Ctl) <= I8_SHARED, "");
     CUtensorMap x_map, w_map;
     lrbi_status rc = i8_map(&x_map, p.x, p.batch, p.cols, p.pitch, 128);
     if (rc == LRBI_OK) rc = i8_map(&w_map, p.w, p.rows, p.cols, p.pitch, channels / 2);
@@ -529,16 +531,27 @@ lrbi_status launch_i8_long(const I8Product &p, int channels, cudaStream_t s)
     return launch_kernel(i8_long_kernel, dim3(2 * pairs), dim3(I8_LONG_THREADS), smem, s, 2, x_map, w_map, t);
 }
 
-lrbi_status launch_i8_split(const I8Product &p, int tokens, int split, cudaStream_t s)      // tokens of a tile: a multiple of 16, up to 256
+namespace {
+long long split_tiles(int rows, int batch, int tokens) { return (long long)((batch + tokens - 1) / tokens) * ((rows + 127) / 128); }
+}  // namespace
+
+lrbi_i8_plan i8_split_plan(int rows, int batch, int tokens, int split)
+{
+    const bool two = tokens <= 128 && split_tiles(rows, batch, tokens) * split > i8_at_once(split);      // three stages or more in half of an SM's shared memory
+    const int stages = std::min(8, (int)(((two ? I8_SHARED / 2 : I8_SHARED) - sizeof(I8Ctl)) / (I8_A_BYTES + tokens * I8_KB)));
+    return {LRBI_I8_SPLIT, tokens, 128, split, stages, 32 * I8_SPLIT_WARPS, two ? 2 : 1};
+}
+
+lrbi_status launch_i8_split(const I8Product &p, const lrbi_i8_plan &plan, cudaStream_t s)
 {
     I8Tc t = i8_args(p);
-    t.tokens = tokens;
-    t.split = split;
+    t.tokens = plan.tokens;
+    const int split = t.split = plan.split;
+    t.stages = plan.stages;
     const int stage = I8_A_BYTES + t.tokens * I8_KB;
-    const long long tiles = (long long)((p.batch + t.tokens - 1) / t.tokens) * ((p.rows + 127) / 128);
+    const long long tiles = split_tiles(p.rows, p.batch, t.tokens);
     if (tiles * split > INT32_MAX) return LRBI_ERR_UNSUPPORTED;
-    const bool two = t.tokens <= 128 && tiles * split > i8_at_once(split);      // three stages or more in half of an SM's shared memory
-    t.stages = std::min(8, (int)(((two ? I8_SHARED / 2 : I8_SHARED) - sizeof(I8Ctl)) / stage));
+    const bool two = plan.per_sm == 2;
     const size_t smem = (size_t)t.stages * stage + sizeof(I8Ctl);      // in all cases more than the 512 bytes a token that the sums take
     CUtensorMap x_map, w_map;
     lrbi_status rc = i8_map(&x_map, p.x, p.batch, p.cols, p.pitch, t.tokens);

@@ -279,11 +279,16 @@ lrbi_status few_launch(const I8Product &p, cudaStream_t s)
 
 // One token, us: 4096 x 9216 with 8 warps 8.9, 16 11.1; 16384 x 4096 12.6 and 18.1; layers of fewer tiles than SMs: 64 x 16384 5.6 and
 // 4.3, 1000 x 4096 2.9 and 2.5.  Short rows, two steps at a time: 16384 x 500 3.9, four 4.9.
-lrbi_status launch_few(const I8Product &p, cudaStream_t s)
+lrbi_i8_plan few_plan(int rows, int cols, int batch)
 {
-    if (p.batch > 8) return few_launch<2, 16, 4>(p, s);
-    if (p.rows <= 16 * NORM_SMS) return few_launch<1, 16, 4>(p, s);
-    return p.cols <= 1024 ? few_launch<1, 8, 2>(p, s) : few_launch<1, 8, 4>(p, s);
+    const int warps = batch > 8 || rows <= 16 * NORM_SMS ? 16 : 8;
+    return {LRBI_I8_FEW, batch > 8 ? 16 : 8, 16, 1, warps == 8 && cols <= 1024 ? 2 : 4, 32 * warps, 1};
+}
+lrbi_status launch_few(const I8Product &p, const lrbi_i8_plan &plan, cudaStream_t s)
+{
+    if (plan.tokens > 8) return few_launch<2, 16, 4>(p, s);
+    if (plan.threads == 512) return few_launch<1, 16, 4>(p, s);
+    return plan.stages == 2 ? few_launch<1, 8, 2>(p, s) : few_launch<1, 8, 4>(p, s);
 }
 
 // Times in microseconds, as fitted to those measured (64 .. 16384 rows, 500 .. 16384 columns, 16 .. 4096 tokens).
@@ -291,9 +296,9 @@ struct Estimate {
     int rows, batch, blocks;      // blocks: of 128 columns
     double memory;                // what the arrays take
 
-    explicit Estimate(const I8Product &p) : rows(p.rows), batch(p.batch), blocks((p.cols + 127) / 128)
+    Estimate(int rows_, int cols, int batch_, int y_dtype) : rows(rows_), batch(batch_), blocks((cols + 127) / 128)
     {
-        memory = ((double)rows * p.cols + (double)batch * p.cols + (p.y_dtype == LRBI_Y_F32 ? 4. : 2.) * batch * rows) / 5.7e6;
+        memory = ((double)rows * cols + (double)batch * cols + (y_dtype == LRBI_Y_F32 ? 4. : 2.) * batch * rows) / 5.7e6;
     }
     static double rounds(long long units, int at_once) { return (double)((units + at_once - 1) / at_once); }
     // 9 to 16 tokens without tensor memory
@@ -335,22 +340,28 @@ lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *
     return LRBI_OK;
 }
 
-lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
+lrbi_i8_plan i8_gemm_plan(int rows, int cols, int batch, int y_dtype)
 {
-    if (p.batch <= 8) return launch_few(p, s);
-    const Estimate e(p);
+    if (batch <= 8) return few_plan(rows, cols, batch);
+    const Estimate e(rows, cols, batch, y_dtype);
     double best = e.many(256);
     int channels = 256, tokens = 0, split = 0;
     for (int n = 224; n >= 128; n -= 32)
         if (e.many(n) < best) { best = e.many(n); channels = n; }
     for (int n : {16, 32, 64, 128, 192, 256})
         for (int k = 1; k <= 8 && k <= e.blocks; k *= 2) {
-            const int each = std::min(n, (p.batch + 15) / 16 * 16);
+            const int each = std::min(n, (batch + 15) / 16 * 16);
             const double t = e.split(each, k);
             if (t < best) { best = t; tokens = each; split = k; }
         }
-    if (p.batch <= 16 && e.few(p.cols) < best) return launch_few(p, s);
-    return split ? launch_i8_split(p, tokens, split, s) : launch_i8_long(p, channels, s);
+    if (batch <= 16 && e.few(cols) < best) return few_plan(rows, cols, batch);
+    return split ? i8_split_plan(rows, batch, tokens, split) : i8_long_plan(channels);
+}
+
+lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s)
+{
+    const lrbi_i8_plan plan = i8_gemm_plan(p.rows, p.cols, p.batch, p.y_dtype);
+    return plan.kernel == LRBI_I8_FEW ? launch_few(p, plan, s) : plan.kernel == LRBI_I8_SPLIT ? launch_i8_split(p, plan, s) : launch_i8_long(p, plan, s);
 }
 
 }  // namespace lrbi

@@ -236,8 +236,11 @@ struct I8Product {
 lrbi_status launch_i8_tokens(const void *x, int dtype, long long stride, int rows, int cols, int act, int8_t *q, float *scale, cudaStream_t s);
 lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *ip, const uint32_t *iz, int8_t *q, float *scale, cudaStream_t s);
 lrbi_status launch_i8_gemm(const I8Product &p, cudaStream_t s);
-lrbi_status launch_i8_long(const I8Product &p, int channels, cudaStream_t s);
-lrbi_status launch_i8_split(const I8Product &p, int tokens, int split, cudaStream_t s);
+lrbi_i8_plan i8_gemm_plan(int rows, int cols, int batch, int y_dtype);      // which kernel a product runs on; no device is asked
+lrbi_i8_plan i8_long_plan(int channels);
+lrbi_i8_plan i8_split_plan(int rows, int batch, int tokens, int split);     // tokens of a tile: a multiple of 16, up to 256
+lrbi_status launch_i8_long(const I8Product &p, const lrbi_i8_plan &plan, cudaStream_t s);
+lrbi_status launch_i8_split(const I8Product &p, const lrbi_i8_plan &plan, cudaStream_t s);
 // CTAs of the split kernel that run at once where each has an SM: clusters of four or eight leave some of the GPCs' SMs over (33 and 15
 // of them fit).
 constexpr int i8_at_once(int split) { return split >= 8 ? 120 : split >= 4 ? 132 : 148; }
