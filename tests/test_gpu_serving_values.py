@@ -104,3 +104,38 @@ def test_rows_of_one_value(B):
         assert torch.equal(out, x) and ((stats[0] - value[:, 0]).abs() <= 2.0 ** -23 * value[:, 0].abs()).all()
         # what is left of a value, some 31 roundings, is taken off to 2^-18 of itself
         assert (u.abs() <= 2.0 ** -18 * 31 * 2.0 ** -24 * value.abs() / 1e-5 ** 0.5).all() and ((stats[1] * 1e-5 ** 0.5 - 1).abs() <= 2.0 ** -18 + (31 * 2.0 ** -24 * value[:, 0]) ** 2 * 2.0 ** -18 / 1e-5).all()
+
+
+# Rows with one span a warp and with four; whole vectors and not; in one block, with the vectors in shared memory or read for every row;
+# shared by two, four and eight blocks.
+TOKEN_ROWS = [(3, 520), (70, 801), (400, 1024), (650, 1030), (900, 4096), (640, 4104), (620, 4099), (500, 8192), (310, 8704), (330, 9216), (310, 12345), (310, 12896), (300, 16384),
+              (160, 16381), (300, 20000), (299, 32760), (70, 32761), (3000, 512), (6000, 200), (2500, 777)]
+
+
+@pytest.mark.parametrize("post,gate,beta", [(True, True, True), (True, True, False), (False, False, False), (True, False, True), (False, True, False)])
+@pytest.mark.parametrize("rows,cols", TOKEN_ROWS)
+def test_tokens_between_blocks(B, rows, cols, post, gate, beta):
+    """u as 8-bit tokens, value by value: off by half a step and 2^-18 of the magnitudes that go into u (64 roundings: sums over a row of
+    31 additions at most, the root's 20, a few of its own); in fp32 the bytes and scales of u itself."""
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    rand = lambda *shape: torch.randn(shape, generator=g, device="cuda")
+    gamma, vec = 1 + 0.2 * rand(cols), 0.2 * rand(cols)
+    how = dict(post_gamma=1 + vec if post else None, post_beta=vec if post and beta else None, gate=0.4 + vec if gate else None, residual_scale=0.8, eps=1e-5)
+    for x, f in ((BF16, BF16), (F32, BF16), (F32, F32)):
+        for kind in ("layer", "rms"):
+            a, b = (rand(rows, cols) + 0.3).to(x), (0.7 * rand(rows, cols) - 0.3).to(f)
+            out, t, stats = B.lrbi_residual_norm(a, b, gamma, vec if beta else None, kind=kind, tokens=True, **how)
+            plain, u, _ = B.lrbi_residual_norm(a, b, gamma, vec if beta else None, kind=kind, **how)
+            assert torch.equal(out, plain) and stats is None and not t.q[:, cols:].any() and (t.q.abs().amax(1) == 127).all()
+            o = out.double()
+            mean = o.mean(1, keepdim=True) if kind == "layer" else 0.0
+            rstd = ((o - mean).square().mean(1, keepdim=True) + 1e-5) ** -0.5
+            offset = vec.double() if beta else 0.0
+            want = (o - mean) * rstd * gamma.double() + offset
+            size = (o.abs() + o.abs().mean(1, keepdim=True)) * rstd * gamma.double().abs() + abs(offset)
+            step, top = t.scale.double()[:, None], want.abs().amax(1)
+            assert ((t.q[:, :cols] * step - want).abs() <= step * (0.5 + 2.0 ** -16) + size * 2.0 ** -18).all()
+            assert ((127 * step[:, 0] - top).abs() <= 2.0 ** -18 * size.amax(1) + 2.0 ** -23 * top).all()
+            if f == F32:
+                same = B.lrbi_i8_tokens(u)
+                assert torch.equal(t.q, same.q) and torch.equal(t.scale, same.scale)
