@@ -342,6 +342,9 @@ lrbi_status launch_i8_quantize(const Geo &g, const uint16_t *W, const uint32_t *
 
 lrbi_i8_plan i8_gemm_plan(int rows, int cols, int batch, int y_dtype)
 {
+    // Up to 8 tokens, few blocks or many: over 12 .. 8192 rows and 512 .. 131072 columns warp-level products take as long as clusters that
+    // share the columns or up to half of it (us, one token: 12 x 4096 2.0 and 4.1, 12 x 131072 29.6 and 30.8, 64 x 16384 4.9 and 6.7,
+    // 4096 x 9216 8.4 and 10.3), but for rows of 65536 columns and more, where they take up to 14% longer (1000 x 131072 39.4 and 34.5).
     if (batch <= 8) return few_plan(rows, cols, batch);
     const Estimate e(rows, cols, batch, y_dtype);
     double best = e.many(256);
