@@ -214,7 +214,6 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) join_backward_kernel(Join j)
         float *mine = columns + threadIdx.y * SUMS * j.width;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (w0 + k * SPAN >= j.width) break;
 #pragma unroll
             for (int s = 0; s < SUMS; ++s) {
                 float v[CHUNK];
