@@ -5,8 +5,9 @@
 //
 //   long   many tokens.  CTA pairs (cta_group::2) of 256 tokens x 128 to 256 channels walk the output tiles; two accumulators, so that
 //          eight warps scale and store one tile while the next one is computed.  Bound: the tensor cores (pipe 94% busy; 4096
-//          tokens, 16384 x 4096: 167 us, 3.3 Pop/s, twice what bf16 products of that size reach), at smaller sizes the last round of
-//          tiles (1000 tokens, 4096 x 16384: 64 tiles on 74 pairs, 47 us of 40).
+//          tokens, 16384 x 4096: 167 us by itself, 3.3 Pop/s, twice what bf16 products of that size reach; call after call, each
+//          with its tokens, the power cap: 195 us for both, 2.8 Pop/s), at smaller sizes the last round of tiles (1000 tokens,
+//          4096 x 16384: 64 tiles on 74 pairs, 47 us of 40).
 //   split  fewer.  128 channels x up to 256 tokens a CTA; the CTAs of a cluster share the columns and add their sums to one another
 //          by bulk copies that add (whole numbers: the same bits however they are cut), so that all SMs stream the weights.
 //          Bound: memory, with 2 us of set-up before and 2 to 5 us of sums and stores behind it (4096 x 9216: 16 tokens 10.6 us,

@@ -129,7 +129,8 @@ __global__ void __launch_bounds__(K == 8 ? 256 : 512, K == 8 ? 4 : 2) i8_tokens_
 // Weights
 // ---------------------------------------------------------------------------------------------------------------------
 // A block has a row.  The range is that of the kept weights; pruned ones are stored as zeros whatever the array holds there.
-// The index of a weight is decoded on its own, twice: a layer is quantised once.
+// A value an access, and the index of a weight decoded on its own, twice: a layer is quantised once, before it serves (4096 x 9216
+// 134 us, with an index of rank 32 330; floor 17.5).
 __global__ void __launch_bounds__(256) i8_quantize_kernel(Geo geo, const uint16_t *__restrict__ W, const uint32_t *__restrict__ ip,
                                                           const uint32_t *__restrict__ iz, int8_t *__restrict__ q, float *__restrict__ scale, int pitch)
 {

@@ -16,8 +16,9 @@
 //
 // Bound: memory where there are many rows (stream in fp32, f in bf16, root mean square, 16384 x 4096: forward 129 us of 125,
 // backward 215 of 187; bf16 97 of 83 with layer norms, 89 without means).  Behind layer norms with betas the backward pass has four
-// sums a column in registers and is bound by issue and what does not fit (186 of 125).  Few rows: 5 us of launch, vectors and
-// first rows.  One span a thread and loads straight into registers, the first form, took 75 and 102 us for 4096 x 4096, now 28 and 56.
+// sums a column in the registers of its 512 threads and is bound by issue and what does not fit there (186 of 125).  Few rows: 5 us of
+// launch, vectors and first rows.  Rows that are not whole vectors: an access a value (forward, 4096 x 4097 bf16 50 us of 21, 4096 x 801
+// 13 of 4).  Means larger than the spread cost a row another sum (4096 x 4096 bf16 28 -> 36 us).  One span a thread and loads straight into registers, the first form, took 75 and 102 us for 4096 x 4096, now 28 and 56.
 #pragma once
 #include <algorithm>
 
